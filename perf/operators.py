@@ -1,0 +1,464 @@
+"""Attention over caches that are bounded or shared by a ragged batch, and the calls that bound them.
+
+Three operators of a serving loop, each through the public entry points:
+  attend   a batch of sequences, each with its own queries (one token of several agents, or a chunk of new
+           tokens of one) over contiguous or paged caches, with a sliding window and sink tokens or without
+  weights  what every cached token received of the queries' attention, added to a running sum per token
+  evict    which tokens stay by that sum, and their rows moved to the caches that hold only them
+
+Sizes are those of the layers below; lengths follow from the case alone (`length_seed`), values from the seed.
+"""
+from __future__ import annotations
+
+import math
+import random
+
+import torch
+
+own = False
+
+ROPE_THETA = 500000.0
+BLOCK = 16
+
+# Attention layers: query heads, kv heads, head dimension.
+LAYERS = {
+    "llama3_8b": (32, 8, 128),
+    "qwen25_7b": (28, 4, 128),
+    "tiny": (4, 4, 64),
+}
+
+
+def _case(name, op, layer, n, *, rank=16, seqs=1, shortest=0, queries=1, causal=False, window=0, sinks=0,
+          key_side=True, rope=False, paged=False, dtype="bf16", decay=0.0, budget=0, recent=0, length_seed=0):
+    """n: cached tokens of the longest sequence, the new ones included; queries: the most a sequence has (agents
+    that decode one token each, or with `causal` the new tokens of one agent)."""
+    c = {"op": op, "layer": layer, "n": n, "rank": rank, "seqs": seqs, "shortest": shortest or n, "queries": queries,
+         "causal": causal, "window": window, "sinks": sinks, "key_side": key_side, "rope": rope, "paged": paged,
+         "dtype": dtype, "decay": decay, "budget": budget, "recent": recent, "length_seed": length_seed}
+    return dict(c, name=name) if name else c
+
+
+def listed():
+    return [
+        # The smallest attention call: two agents of a small fp32 model behind a short window, all latency.
+        _case("attend_fp32_tiny", "attend", "tiny", 700, rank=8, queries=2, window=256, sinks=4, dtype="fp32"),
+        # A decode step of four agents whose shared 32k trajectory is seen through a window of 4k and four sinks.
+        _case("attend_window_a4_n32768", "attend", "llama3_8b", 32768, queries=4, window=4096, sinks=4),
+        # Serving: sixteen trajectories of 4k to 64k tokens on pages, four agents each, a wide window.
+        _case("attend_window_batch", "attend", "qwen25_7b", 65536, rank=32, seqs=16, shortest=4096, queries=4,
+              window=8192, sinks=16, paged=True, length_seed=11),
+        # Continuous batching: some sequences decode one token, others take a chunk of their prompt; no window.
+        _case("attend_mixed_chunks", "attend", "llama3_8b", 8000, seqs=12, shortest=500, queries=256, causal=True,
+              paged=True, length_seed=3),
+        # Two long prompts advance by a chunk of up to 2048 tokens, full causal attention on pages.
+        _case("attend_chunk_2048", "attend", "llama3_8b", 18432, seqs=2, shortest=8000, queries=2048, causal=True,
+              paged=True, length_seed=7),
+        # Tools' answers of a few hundred tokens, keys with a rotated adapter, a narrow window of odd size.
+        _case("attend_chunk_rotary", "attend", "qwen25_7b", 5333, rank=8, seqs=4, shortest=700, queries=333, causal=True,
+              window=1000, sinks=4, rope=True, paged=True, length_seed=7),
+        # The smallest weights call.
+        _case("weights_fp32_tiny", "weights", "tiny", 700, rank=8, queries=2, decay=1.0, dtype="fp32"),
+        # Four agents' decode step on one 8k context adds to the running sums.
+        _case("weights_a4_n8192", "weights", "llama3_8b", 8192, queries=4, decay=1.0),
+        # The same for a ragged batch on pages, with sums that fade.
+        _case("weights_batch", "weights", "qwen25_7b", 65536, rank=32, seqs=16, shortest=4096, queries=4, decay=0.98,
+              paged=True, length_seed=11),
+        # A prompt is judged once, by its last 64 tokens.
+        _case("weights_observe_64", "weights", "llama3_8b", 18432, queries=64, causal=True),
+        # One long context is cut to a quarter.
+        _case("evict_16384_to_4096", "evict", "llama3_8b", 16384, budget=4096, sinks=4, recent=512),
+        # A ragged batch on pages is cut to 8k tokens each; some sequences are shorter and stay whole.
+        _case("evict_batch", "evict", "qwen25_7b", 65536, rank=32, seqs=16, shortest=4096, budget=8192, sinks=16,
+              recent=1001, paged=True, length_seed=11),
+    ]
+
+
+def _log(rng, lo, hi):
+    """An integer of [lo, hi], spread over its logarithm."""
+    return min(hi, max(lo, int(round(lo * (hi / lo) ** rng.random()))))
+
+
+def _draw_once(rng):
+    op = rng.choice(("attend", "attend", "attend", "weights", "weights", "evict"))
+    layer = rng.choice(("llama3_8b", "llama3_8b", "qwen25_7b", "tiny"))
+    rank = rng.choice((8, 16, 16, 24, 32, 64))
+    fp32 = layer == "tiny" and rng.random() < 0.5
+    if fp32:
+        rank = rng.choice((8, 12, 16))
+    seqs = rng.choice((1, _log(rng, 2, 16)))
+    longest = _log(rng, 40, 65536 if op != "attend" or seqs > 1 else 32768)
+    shortest = max(1, int(longest * rng.uniform(0.05, 1.0))) if seqs > 1 else longest
+    same = dict(rank=rank, seqs=seqs, shortest=shortest, paged=seqs > 1 or rng.random() < 0.3,
+                dtype="fp32" if fp32 else "bf16", length_seed=rng.randrange(1 << 20))
+    if op == "evict":
+        budget = max(2, int(longest * rng.uniform(0.1, 1.1)))
+        recent = rng.randrange(0, budget // 2 + 1)
+        return _case(None, "evict", layer, longest, budget=budget, recent=recent,
+                     sinks=rng.choice((0, 1, 4, 16)) if budget - recent >= 16 else 0, **same)
+    causal = rng.random() < 0.5
+    queries = min(shortest, _log(rng, 1, 1500 if op == "attend" else 128) if causal else _log(rng, 1, 8))
+    window = _log(rng, 16, 16384) if rng.random() < 0.6 else 0
+    same.update(queries=queries, causal=causal, window=window, sinks=rng.choice((0, 1, 4, 16, 64)) if window else 0,
+                key_side=rng.random() < 0.75)
+    if op == "weights":
+        return _case(None, "weights", layer, longest, decay=rng.choice((0.0, 0.9, 1.0)), **same)
+    return _case(None, "attend", layer, longest, rope=causal and same["key_side"] and rng.random() < 0.25, **same)
+
+
+def draw(rng):
+    """Cases whose padded batch costs the plain form no more than the listed ones."""
+    while True:
+        c = _draw_once(rng)
+        hq, hkv, d = LAYERS[c["layer"]]
+        lengths, _ = _sizes(c)
+        keys = _span(c) if c["op"] != "evict" else c["n"]
+        scores = c["seqs"] * hq * c["queries"] * keys
+        rows = c["seqs"] * keys * hkv * d * (c["queries"] if c["rope"] and not c["causal"] else 1)
+        if scores <= 1 << 30 and rows <= 1 << 29 and sum(lengths) <= 600000:
+            return c
+
+
+def _sizes(case):
+    """Lengths and query counts of the sequences."""
+    rng = random.Random(case["length_seed"])
+    n, seqs = case["n"], case["seqs"]
+    lengths = [n] + [rng.randint(case["shortest"], n) for _ in range(seqs - 1)]
+    most = case["queries"]
+    counts = [most] + [min(lengths[t], _log(rng, 1, most)) if case["causal"] else most for t in range(1, seqs)]
+    return lengths, counts
+
+
+def _seen(case, n, c):
+    """Sinks before the window, and the first key of the window of a sequence's first query."""
+    first = n - c if case["causal"] else n - 1
+    lo = max(0, first - case["window"] + 1) if case["window"] else 0
+    return min(case["sinks"], lo) if case["window"] else 0, lo
+
+
+def _span(case):
+    """The most keys that any sequence's queries see together."""
+    lengths, counts = _sizes(case)
+    return max(s + n - lo for n, c in zip(lengths, counts) for s, lo in (_seen(case, n, c),))
+
+
+class _State:
+    """Tensors and descriptors that a serving program holds for one layer."""
+
+
+def _inputs(case, seed):
+    dev = torch.device("cuda")
+    gen = torch.Generator(device=dev).manual_seed(seed)
+    dt = torch.bfloat16 if case["dtype"] == "bf16" else torch.float32
+    hq, hkv, d = LAYERS[case["layer"]]
+    r = case["rank"]
+
+    def randn(*shape, std=1.0):
+        return torch.randn(*shape, generator=gen, device=dev, dtype=dt).mul_(std)
+
+    s = _State()
+    lengths, counts = _sizes(case)
+    seqs = case["seqs"]
+    s.n_adapters = 5
+    s.seq_lens = torch.tensor(lengths, dtype=torch.int32, device=dev)
+    s.block_table = None
+    kv_shape, l_shape = (lengths[0], hkv, d), (lengths[0], r)
+    if case["paged"]:
+        per_seq = torch.tensor([-(-n // BLOCK) for n in lengths], device=dev)
+        blocks = sum(-(-n // BLOCK) for n in lengths)
+        order = torch.randperm(blocks, generator=gen, device=dev).to(torch.int32)
+        at = torch.arange(-(-max(lengths) // BLOCK), device=dev)
+        index = (torch.cumsum(per_seq, 0) - per_seq)[:, None] + at
+        s.block_table = torch.where(at < per_seq[:, None], order[index.clamp(max=blocks - 1)], -1).to(torch.int32).contiguous()
+        kv_shape, l_shape = (blocks, hkv, BLOCK, d), (blocks, BLOCK, r)
+    s.k, s.v, s.l = randn(*kv_shape), randn(*kv_shape), randn(*l_shape)
+    s.b_k = randn(s.n_adapters, r, hkv * d, std=0.02) if case["key_side"] else None
+    s.b_v = randn(s.n_adapters, r, hkv * d, std=0.02)
+    total = sum(counts)
+    s.q = randn(total, hq, d)
+    s.start = torch.tensor([sum(counts[:t]) for t in range(seqs + 1)], dtype=torch.int32, device=dev)
+    per = torch.tensor(counts, device=dev)
+    s.query_adapter = (torch.arange(seqs, device=dev).repeat_interleave(per) % s.n_adapters if case["causal"]
+                       else torch.arange(total, device=dev) % s.n_adapters).to(torch.int32)
+    if case["op"] == "weights":
+        # sums of about what one more call adds
+        s.weights = torch.rand(seqs, max(lengths), generator=gen, device=dev).clamp_(min=1e-6).log_().mul_(-hq * max(counts) / max(lengths))
+    elif case["op"] == "evict":
+        # running sums of attention weight: a few tokens hold most of it
+        s.weights = torch.rand(seqs, max(lengths), generator=gen, device=dev).clamp_(min=1e-6).pow_(-1.2)
+    return s
+
+
+def prepare(case, seed):
+    s = _inputs(case, seed)
+    s.case = case
+    dev = s.q.device
+    hq, hkv, d = LAYERS[case["layer"]]
+    lengths, counts = _sizes(case)
+    s.most, s.keys, s.n_max = max(counts), _span(case) if case["op"] != "evict" else 0, max(lengths)
+    s.out = torch.empty_like(s.q)
+    if case["op"] == "evict":
+        budget, seqs = case["budget"], case["seqs"]
+        s.kept = torch.full((seqs, budget), -1, dtype=torch.int32, device=dev)
+        s.new_lens = torch.zeros(seqs, dtype=torch.int32, device=dev)
+        s.dst_weights = torch.zeros(seqs, budget, device=dev)
+        s.dst_table = None
+        kv_shape, l_shape = (budget, hkv, d), (budget, case["rank"])
+        if case["paged"]:
+            per = -(-budget // BLOCK)
+            s.dst_table = torch.arange(seqs * per, dtype=torch.int32, device=dev).view(seqs, per).flip(0).contiguous()
+            kv_shape, l_shape = (seqs * per, hkv, BLOCK, d), (seqs * per, BLOCK, case["rank"])
+        s.dst = [torch.zeros(shape, dtype=s.k.dtype, device=dev) for shape in (kv_shape, kv_shape, l_shape)]
+    if own:
+        import paper_2602_01053_amd as lra
+        s.lra = lra
+        s.shape = lra.make_shape(s.q, hkv, case["rank"], 0.0, ROPE_THETA if case["rope"] else 0.0)
+        s.cache = lra.make_cache(s.k, s.v, s.l, s.seq_lens, max(lengths), s.block_table, seq_lens_host=lengths)
+        if case["op"] == "evict":
+            s.dst_cache = lra.make_cache(*s.dst, s.new_lens, case["budget"], s.dst_table)
+            need = lra.lra_evict_workspace_bytes(s.cache, case["budget"])
+        else:
+            s.batch = lra.make_batch(s.start, s.query_adapter, s.most, causal=case["causal"], window=case["window"],
+                                     sinks=case["sinks"])
+            size = lra.lra_batch_workspace_bytes if case["op"] == "attend" else lra.lra_key_weights_workspace_bytes
+            need = size(s.shape, s.cache, s.batch)
+        s.workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+    return s
+
+
+def run(s):
+    case = s.case
+    if own:
+        lra = s.lra
+        if case["op"] == "attend":
+            lra.lra_attn_batch(s.shape, s.cache, s.b_k, s.b_v, s.n_adapters, s.batch, s.q, s.out, s.workspace)
+            return s.out
+        if case["op"] == "weights":
+            lra.lra_key_weights(s.shape, s.cache, s.b_k, s.n_adapters, s.batch, s.q, case["decay"], s.weights, s.workspace)
+            return s.weights
+        lra.lra_evict_select(s.cache, s.weights, case["budget"], case["sinks"], case["recent"], s.kept, s.new_lens, s.workspace)
+        lra.lra_cache_gather(s.shape, s.cache, s.kept, s.dst_cache, weights=s.weights, dst_weights=s.dst_weights)
+    elif case["op"] == "attend":
+        return _plain_attend(s)
+    elif case["op"] == "weights":
+        return _plain_weights(s)
+    else:
+        _plain_evict(s)
+    return {"kept": s.kept, "new_lens": s.new_lens, "k": s.dst[0], "v": s.dst[1], "l": s.dst[2], "weights": s.dst_weights}
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# The plain forms: padded batches, 32 bits, rounded once.
+# ---------------------------------------------------------------------------------------------------------------
+def _places(s, token):
+    """(block, slot) or row of token [seqs][...] of every sequence, for indexing the caches."""
+    if s.block_table is None:
+        return token
+    row = torch.arange(token.shape[0], device=token.device)[:, None]
+    return s.block_table[row, token // BLOCK].long(), token % BLOCK
+
+
+def _rows(s, cache, token):
+    at = _places(s, token)
+    if s.block_table is None:
+        return cache[at].float()
+    return (cache[at[0], :, at[1]] if cache.dim() == 4 else cache[at[0], at[1]]).float()
+
+
+def _plain_scores(s):
+    """Scores [seqs][A][Hkv][M * G][keys] of the padded batch (queries = A adapters of M tokens each), minus infinity
+    where nothing is seen; with them the padded queries' indices, keys' tokens and the keys' low-rank rows."""
+    case, dev = s.case, s.q.device
+    hq, hkv, d = LAYERS[case["layer"]]
+    r, g, seqs, most = case["rank"], hq // hkv, case["seqs"], s.most
+    n = s.seq_lens.long()
+    start = s.start.long()
+    count = start[1:] - start[:-1]
+    k_of = torch.arange(most, device=dev)
+    query = torch.minimum(start[:-1, None] + k_of, start[1:, None] - 1)                                # [T][C]
+    pos = (n - count)[:, None] + k_of if case["causal"] else (n - 1)[:, None].expand(seqs, most)
+    first = pos[:, :1]
+    lo = (first - case["window"] + 1).clamp(min=0) if case["window"] else torch.zeros_like(first)
+    sinks = torch.minimum(torch.full_like(lo, case["sinks"]), lo) if case["window"] else lo
+    u = torch.arange(s.keys, device=dev)
+    token = torch.where(u < sinks, u, u - sinks + lo)                                                  # [T][U]
+    live = token < n[:, None]
+    token = torch.minimum(token, n[:, None] - 1)
+    a, m = (1, most) if case["causal"] else (most, 1)
+    adapter = s.query_adapter[query[:, ::m]].long()                                                    # [T][A]
+    q = s.q[query].float().view(seqs, a, m, hkv, g, d).permute(0, 1, 3, 2, 4, 5).reshape(seqs, a, hkv, m * g, d)
+    keys = _rows(s, s.k, token).permute(0, 2, 3, 1).unsqueeze(1)                                       # [T][1][Hkv][d][U]
+    low = _rows(s, s.l, token)                                                                         # [T][U][r]
+    if s.b_k is not None:
+        b = s.b_k[adapter].float().view(seqs, a, r, hkv, d).permute(0, 1, 3, 2, 4)                     # [T][A][Hkv][r][d]
+        if case["rope"]:
+            add = torch.matmul(low[:, None, None], b)                                                  # [T][A][Hkv][U][d]
+            rate = ROPE_THETA ** (-torch.arange(0, d, 2, device=dev, dtype=torch.float64) / d)
+            angle = token[..., None].double() * rate
+            cos, sin = torch.cos(angle).float()[:, None, None], torch.sin(angle).float()[:, None, None]
+            x, y = add[..., :d // 2], add[..., d // 2:]
+            keys = keys + torch.cat((x * cos - y * sin, y * cos + x * sin), -1).transpose(-1, -2)
+            scores = torch.matmul(q, keys)
+        else:
+            scores = torch.matmul(q, keys)
+            scores += torch.matmul(torch.matmul(q, b.transpose(-1, -2)), low.transpose(-1, -2)[:, None, None])
+    else:
+        scores = torch.matmul(q, keys)
+    scores *= 1.0 / math.sqrt(d)
+    seen = live[:, None] & (token[:, None] <= pos[..., None])
+    if case["window"]:
+        seen &= (token[:, None] > pos[..., None] - case["window"]) | (token[:, None] < case["sinks"])
+    seen = seen.view(seqs, a, 1, m, 1, s.keys).expand(-1, -1, hkv, -1, g, -1).reshape(seqs, a, hkv, m * g, s.keys)
+    scores.masked_fill_(~seen, -math.inf)
+    return scores, adapter, token, live, low, count
+
+
+def _plain_attend(s):
+    case = s.case
+    hq, hkv, d = LAYERS[case["layer"]]
+    r, g, seqs, most = case["rank"], hq // hkv, case["seqs"], s.most
+    scores, adapter, token, _, low, count = _plain_scores(s)
+    a, m = scores.shape[1], scores.shape[3] // g
+    scores -= scores.amax(-1, keepdim=True).clamp(min=-1e30)
+    p = scores.exp_()
+    total = p.sum(-1, keepdim=True)
+    values = _rows(s, s.v, token).permute(0, 2, 1, 3).unsqueeze(1)                                     # [T][1][Hkv][U][d]
+    b = s.b_v[adapter].float().view(seqs, a, r, hkv, d).permute(0, 1, 3, 2, 4)
+    o = torch.matmul(p, values) + torch.matmul(torch.matmul(p, low[:, None, None]), b)
+    o /= total
+    o = o.view(seqs, a, hkv, m, g, d).permute(0, 1, 3, 2, 4, 5).reshape(seqs, most, hq, d)
+    ours = torch.arange(most, device=o.device) < count[:, None]
+    return o[ours].to(s.q.dtype)
+
+
+def _plain_weights(s):
+    case = s.case
+    scores, _, token, live, _, count = _plain_scores(s)
+    seqs, a, hkv, rows, keys = scores.shape
+    scores -= scores.amax(-1, keepdim=True).clamp(min=-1e30)
+    p = scores.exp_()
+    p /= p.sum(-1, keepdim=True)
+    ours = torch.arange(s.most, device=p.device) < count[:, None]
+    p *= ours.view(seqs, a, 1, s.most // a, 1, 1).expand(-1, -1, hkv, -1, rows * a // s.most, -1).reshape(seqs, a, hkv, rows, 1)
+    got = p.sum((1, 2, 3)) * live
+    inside = torch.arange(s.n_max, device=p.device) < s.seq_lens[:, None]
+    w = torch.where(inside, s.weights * case["decay"], s.weights)
+    w.scatter_add_(1, token, got)
+    s.weights.copy_(w)
+    return s.weights
+
+
+def _plain_evict(s):
+    case = s.case
+    n = s.seq_lens.long()[:, None]
+    j = torch.arange(s.n_max, device=s.weights.device)
+    held = (j < case["sinks"]) | (j >= n - case["recent"])
+    rank_by = torch.where(held, math.inf, s.weights).masked_fill(j >= n, -math.inf)
+    order = torch.sort(rank_by, dim=1, descending=True, stable=True).indices[:, :case["budget"]]
+    i = torch.arange(order.shape[1], device=j.device)
+    new = torch.minimum(n, torch.full_like(n, case["budget"]))
+    kept = torch.sort(torch.where(i < new, order, s.n_max), dim=1).values
+    ours = i < new
+    kept = torch.where(ours, kept, 0)
+    t, at = torch.nonzero(ours, as_tuple=True)
+    src = kept[t, at]
+    s.kept[t, at] = src.int()
+    s.new_lens.copy_(new[:, 0])
+    s.dst_weights[t, at] = s.weights[t, src]
+    if s.block_table is None:
+        s.dst[0][at], s.dst[1][at], s.dst[2][at] = s.k[src], s.v[src], s.l[src]
+    else:
+        b, c = s.block_table[t, src // BLOCK].long(), src % BLOCK
+        e, f = s.dst_table[t, at // BLOCK].long(), at % BLOCK
+        s.dst[0][e, :, f], s.dst[1][e, :, f], s.dst[2][e, f] = s.k[b, :, c], s.v[b, :, c], s.l[b, c]
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# The definition in 64 bits, sequence by sequence and head by head: keys and values are formed, nothing is padded.
+# ---------------------------------------------------------------------------------------------------------------
+def exact(case, seed):
+    s = _inputs(case, seed)
+    hq, hkv, d = LAYERS[case["layer"]]
+    g, r = hq // hkv, case["rank"]
+    lengths, counts = _sizes(case)
+    if case["op"] == "evict":
+        return None
+    out = torch.zeros(s.q.shape, dtype=torch.float64, device=s.q.device)
+    weights = s.weights.double() if case["op"] == "weights" else None
+    if weights is not None:
+        for t, n in enumerate(lengths):
+            weights[t, :n] *= case["decay"]
+    at = 0
+    for t, (n, c) in enumerate(zip(lengths, counts)):
+        j = torch.arange(n, device=s.q.device)
+        if s.block_table is not None:
+            blk = s.block_table[t, j // BLOCK].long()
+            k, v, low = s.k[blk, :, j % BLOCK], s.v[blk, :, j % BLOCK], s.l[blk, j % BLOCK].double()
+        else:
+            k, v, low = s.k, s.v, s.l.double()
+        groups = [(at, c)] if case["causal"] else [(at + i, 1) for i in range(c)]
+        for first, m in groups:
+            a = int(s.query_adapter[first])
+            p_of = n - m + torch.arange(m, device=j.device)
+            mask = j[None, :] <= p_of[:, None]
+            if case["window"] > 0:
+                mask &= (p_of[:, None] - j[None, :] < case["window"]) | (j[None, :] < case["sinks"])
+            some = torch.nonzero(mask.any(0))[:, 0]
+            mask = mask[:, some]
+            for h in range(hkv):
+                cols = slice(h * d, (h + 1) * d)
+                key = k[some, h].double()
+                if s.b_k is not None:
+                    extra = low[some] @ s.b_k[a, :, cols].double()
+                    if case["rope"]:
+                        turn = some[:, None].double() / ROPE_THETA ** (torch.arange(d // 2, device=j.device).double() * 2 / d)
+                        z = torch.polar(torch.ones_like(turn), turn) * torch.complex(extra[:, :d // 2], extra[:, d // 2:])
+                        extra = torch.cat((z.real, z.imag), 1)
+                    key = key + extra
+                if weights is None:
+                    val = v[some, h].double() + low[some] @ s.b_v[a, :, cols].double()
+                for x in range(h * g, (h + 1) * g):
+                    z = s.q[first:first + m, x].double() @ key.T / math.sqrt(d)
+                    pr = torch.softmax(z.masked_fill(~mask, -math.inf), 1)
+                    if weights is None:
+                        out[first:first + m, x] = pr @ val
+                    else:
+                        weights[t].index_add_(0, some, pr.sum(0))
+        at += c
+    return out if weights is None else weights
+
+
+def work(case):
+    """Bytes: the rows that any query of a sequence sees, its queries, outputs and the adapters in use once; for an
+    eviction the weights, and the kept rows read and written.  Operations: per pair of a query row and a key it sees
+    2d for the score, 2d + 2r for the values (2r more with a key-side adapter, or 2rd per key and head where it is
+    rotated), and the rank-r projections of each row."""
+    hq, hkv, d = LAYERS[case["layer"]]
+    es = 2 if case["dtype"] == "bf16" else 4
+    r, causal, win, sinks = case["rank"], case["causal"], case["window"], case["sinks"]
+    lengths, counts = _sizes(case)
+    if case["op"] == "evict":
+        kept = sum(min(n, case["budget"]) for n in lengths)
+        return {"bytes": 4 * sum(lengths) + kept * (2 * es * (2 * hkv * d + r) + 16), "flops": 0}
+    pairs = keys = 0
+    for n, c in zip(lengths, counts):
+        s0, lo = _seen(case, n, c)
+        keys += s0 + n - lo
+        for p in (range(n - c, n) if causal else [n - 1] * c):
+            first = max(0, p - win + 1) if win else 0
+            pairs += p + 1 - first + (min(sinks, first) if win else 0)
+    rows = sum(counts) * hq
+    pairs *= hq
+    used = min(5, case["seqs"] if causal else sum(counts))
+    sides = (1 if case["key_side"] else 0) + (1 if case["op"] == "attend" else 0)
+    nbytes = es * (rows * d + sides * used * r * hkv * d)
+    flops = pairs * 2 * d
+    if case["key_side"] and case["rope"]:
+        flops += 2 * keys * hkv * r * d * (1 if causal else max(counts))
+    elif case["key_side"]:
+        flops += pairs * 2 * r + 2 * rows * d * r
+    if case["op"] == "attend":
+        nbytes += es * (keys * (2 * hkv * d + r) + rows * d)
+        flops += pairs * (2 * d + 2 * r) + 2 * rows * d * r
+    else:
+        nbytes += es * keys * (hkv * d + (r if case["key_side"] else 0)) + 4 * sum(lengths) * (2 if case["decay"] else 1)
+    return {"bytes": nbytes, "flops": flops}
