@@ -398,6 +398,54 @@ lra_status lra_cache_append(const lra_shape* shape, const lra_cache* cache, cons
 size_t lra_append_workspace_bytes(const lra_shape* shape, const lra_cache* cache,
                                   const lra_projection* proj, int32_t n_new, const lra_tuning* tuning);
 
+/*
+ * A batch of queries with a mask of their own, for lra_attn_batch and lra_key_weights.
+ *
+ * Queries are grouped by sequence as in lra_attn_decode: sequence t owns queries seq_query_start[t] ..
+ * seq_query_start[t+1]-1, c_t of them (none is fine).  The token that query k of them (from 0) stands for is
+ *   causal == 0   the last one of its sequence, position seq_lens[t] - 1: one new token of each of c_t agents;
+ *   causal != 0   position seq_lens[t] - c_t + k: the queries are the last c_t tokens of the sequence, a chunk
+ *                 of new tokens of ONE agent, whose adapter is that of the chunk's first query (the adapter
+ *                 ids of the others are not read).  Sequences with one query and sequences with a long chunk
+ *                 can share a batch.
+ * A query at position i sees the tokens j with
+ *     0 <= j <= i   and   (window == 0  or  j > i - window  or  j < sinks):
+ * all before it, or the last `window` tokens (its own among them) and the first `sinks` of the sequence.
+ * Attention over a window bounds what a growing trajectory costs per token; its first tokens stay visible
+ * because trained models put much of their weight there whatever they hold.  A query that sees nothing (its
+ * sequence holds no token, or a chunk is longer than its sequence) gives zeros.
+ * Rows that no query of the call sees are not read: they may hold anything, NaN included, and block-table
+ * entries of blocks that hold no visible token may be out of range (pages behind the window can be given back).
+ * Rows that some queries of a sequence see and others do not must be finite (a weight of zero times NaN is NaN).
+ */
+typedef struct {
+  const int32_t* seq_query_start; /* DEVICE int32 [n_seqs+1], non-decreasing, [0] = 0, [n_seqs] = n_queries */
+  const int32_t* query_adapter;   /* DEVICE int32 [n_queries], clamped into [0, n_adapters) */
+  int32_t n_queries;              /* >= 1 */
+  int32_t max_queries_per_seq;    /* HOST-known upper bound of every c_t */
+  int32_t causal;
+  int32_t window;                 /* 0: no window */
+  int32_t sinks;                  /* 0 <= sinks; of no effect without a window */
+} lra_batch;
+
+/*
+ * Attention of such a batch, with the scores, adapters, rotary key side and caches of lra_attn_decode and
+ * lra_attn_prefill: decode steps of several agents behind a window, chunks of new tokens of many sequences over
+ * one paged cache, or both kinds in one call (causal, chunks of one token).  In lra_cache, seq_lens[t] may be 0
+ * for a sequence without queries or whose queries see nothing, and seq_lens_host is not used.
+ *
+ *   q    DEVICE [n_queries][Hq][d]        out  DEVICE [n_queries][Hq][d]
+ *   workspace  DEVICE, 256-byte aligned, >= lra_batch_workspace_bytes(...) bytes; contents undefined afterwards;
+ *              calls that overlap in time, captured graphs among them, need separate ones
+ *   tuning     kernel_variant (1: vector-ALU kernels), decode_split_keys (keys per workgroup)
+ */
+lra_status lra_attn_batch(const lra_shape* shape, const lra_cache* cache, const lra_adapters* adapters,
+                          const lra_batch* batch, const void* q, void* out, void* workspace, size_t workspace_bytes,
+                          const lra_tuning* tuning, void* stream);
+/* (size_t)-1 when the arguments would be rejected. */
+size_t lra_batch_workspace_bytes(const lra_shape* shape, const lra_cache* cache, const lra_batch* batch,
+                                 const lra_tuning* tuning);
+
 /* Static, NUL-terminated description of a status code. */
 const char* lra_status_string(lra_status status);
 

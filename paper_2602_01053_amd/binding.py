@@ -21,7 +21,8 @@ LRA_BF16, LRA_F32 = 0, 1
 STATIC_WORKSPACE_BYTES = 64 << 20   # LRA_STATIC_WORKSPACE_BYTES of the header
 
 EXPORTS = ("lra_workspace_bytes", "lra_attn_decode", "lra_attn_decode_static", "lra_attn_prefill", "lra_status_string",
-           "lra_cache_append", "lra_append_workspace_bytes", "lra_probe_stream_read", "lra_probe_mfma_bf16")
+           "lra_cache_append", "lra_append_workspace_bytes", "lra_probe_stream_read", "lra_probe_mfma_bf16",
+           "lra_attn_batch", "lra_batch_workspace_bytes")
 
 
 class LraShape(ctypes.Structure):
@@ -47,6 +48,12 @@ class LraAdapters(ctypes.Structure):
 
 class LraProjection(ctypes.Structure):
     _fields_ = [("w", ctypes.c_void_p), ("d_model", ctypes.c_int32), ("rope_theta", ctypes.c_float)]
+
+
+class LraBatch(ctypes.Structure):
+    _fields_ = [("seq_query_start", ctypes.c_void_p), ("query_adapter", ctypes.c_void_p), ("n_queries", ctypes.c_int32),
+                ("max_queries_per_seq", ctypes.c_int32), ("causal", ctypes.c_int32), ("window", ctypes.c_int32),
+                ("sinks", ctypes.c_int32)]
 
 
 class LraTuning(ctypes.Structure):
@@ -145,6 +152,11 @@ def load_library() -> ctypes.CDLL:
     lib.lra_append_workspace_bytes.argtypes = [sp, cp, ctypes.POINTER(LraProjection), i32, tp]
     lib.lra_status_string.restype = ctypes.c_char_p
     lib.lra_status_string.argtypes = [ctypes.c_int]
+    bp = ctypes.POINTER(LraBatch)
+    lib.lra_attn_batch.restype = ctypes.c_int
+    lib.lra_attn_batch.argtypes = [sp, cp, ap, bp, vp, vp, vp, ctypes.c_size_t, tp, vp]
+    lib.lra_batch_workspace_bytes.restype = ctypes.c_size_t
+    lib.lra_batch_workspace_bytes.argtypes = [sp, cp, bp, tp]
     lib.lra_probe_stream_read.restype = ctypes.c_int
     lib.lra_probe_stream_read.argtypes = [vp, ctypes.c_size_t, vp, vp]
     lib.lra_probe_mfma_bf16.restype = ctypes.c_int
@@ -380,3 +392,45 @@ def lra_attn_prefill(shape: LraShape, cache: LraCache, b_k: Optional[torch.Tenso
                                                  stream)
     if status:
         _check(status)
+
+
+def make_batch(seq_query_start: torch.Tensor, query_adapter: torch.Tensor, max_queries_per_seq: int, causal: bool = False,
+               window: int = 0, sinks: int = 0) -> LraBatch:
+    """Queries grouped by sequence (int32 tensors on the device, see lra_batch of the header): each the last token of its
+    sequence (several agents' decode step), or with `causal` the last tokens of it in order (a chunk of one agent); seen
+    through a window of the last `window` tokens and the first `sinks`, or without one (0)."""
+    for t in (seq_query_start, query_adapter):
+        if t.dtype != torch.int32 or not t.is_contiguous() or t.dim() != 1:
+            raise LraError(2, "seq_query_start and query_adapter must be dense int32 vectors")
+    batch = LraBatch(_ptr(seq_query_start), _ptr(query_adapter), query_adapter.numel(), int(max_queries_per_seq), int(bool(causal)),
+                     int(window), int(sinks))
+    batch._tensors = (seq_query_start, query_adapter)  # the struct holds raw pointers into them
+    return batch
+
+
+def lra_batch_workspace_bytes(shape: LraShape, cache: LraCache, batch: LraBatch) -> int:
+    n = load_library().lra_batch_workspace_bytes(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(batch), _tuning_ref)
+    if n == ctypes.c_size_t(-1).value:
+        raise LraError(2, "lra_batch_workspace_bytes rejected the arguments")
+    return int(n)
+
+
+def _workspace_args(workspace: Optional[torch.Tensor]):
+    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+
+
+def _check_rows(batch: LraBatch, shape: LraShape, *tensors: torch.Tensor) -> None:
+    want = (batch.n_queries, shape.n_q_heads, shape.head_dim)
+    for t in tensors:
+        if tuple(t.shape) != want or not t.is_contiguous() or _dtype_code(t) != shape.dtype:
+            raise LraError(2, f"q and out must be dense {want} tensors of the shape's dtype")
+
+
+def lra_attn_batch(shape: LraShape, cache: LraCache, b_k: Optional[torch.Tensor], b_v: Optional[torch.Tensor], n_adapters: int,
+                   batch: LraBatch, q: torch.Tensor, out: torch.Tensor, workspace: Optional[torch.Tensor], stream=None) -> None:
+    """Attention of a ragged batch (make_batch): decode steps of several agents or chunks of new tokens, with a sliding
+    window and sinks or without.  q, out: [n_queries][Hq][d]."""
+    _check_rows(batch, shape, q, out)
+    ad = LraAdapters(_ptr(b_k), _ptr(b_v), int(n_adapters))
+    _check(load_library().lra_attn_batch(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(ad), ctypes.byref(batch), _ptr(q),
+                                         _ptr(out), *_workspace_args(workspace), _tuning_ref, _stream_ptr(stream)))

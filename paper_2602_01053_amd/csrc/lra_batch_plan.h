@@ -1,0 +1,19 @@
+// Host-side checks and launch planning of the batch entry points.  Plain C++ with no HIP dependency, like lra_plan.h.
+#pragma once
+
+#include "lra_plan.h"
+
+namespace lra {
+
+lra_status check_batch(const lra_shape* sh, const lra_cache* c, const lra_batch* b);
+
+struct BatchPlan {
+  int rows;        // n_queries x Hq
+  int split_keys;  // keys per share, of those that a row sees
+  int n_splits;
+  size_t off_ml, off_o, off_lr, off_adapter, bytes;
+  bool launchable;  // false: LRA_ERR_UNSUPPORTED
+};
+BatchPlan plan_batch(const lra_shape* sh, const lra_cache* c, const lra_batch* b, const Tuning& tune);
+
+}  // namespace lra

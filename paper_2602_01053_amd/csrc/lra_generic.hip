@@ -10,6 +10,7 @@
 // the merge kernel, after the per-split states are combined.
 #include <type_traits>
 
+#include "lra_batch.h"
 #include "lra_common.h"
 #include "lra_decode_util.h"
 #include "lra_plan.h"
@@ -38,17 +39,6 @@ __device__ __forceinline__ float dot_row(const T* __restrict__ row, const float*
   }
   for (int c = 0; c < len; ++c) acc = fmaf(to_f32<T>(row[c]), vec[c], acc);
   return acc;
-}
-
-// Sequence of query `tok`: the last t with seq_query_start[t] <= tok.
-__device__ __forceinline__ int sequence_of_query(const Params& p, int tok) {
-  int lo = 0, hi = p.n_seqs - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (p.seq_query_start[mid] <= tok) lo = mid;
-    else hi = mid - 1;
-  }
-  return lo;
 }
 
 // The elements of a 16-byte piece as floats.
@@ -139,8 +129,10 @@ constexpr int kGenericRowBits = 23;
 // keys, 4 agents, 91, 59; 700 new bf16 tokens of rank 12 578, 294.
 // K and V rows are 16-byte aligned (bases and strides are checked); L rows of a rank that is no multiple of four
 // are not, and are read element by element.
-template <typename T, int D, bool PAGED, int RB>
-__global__ __launch_bounds__(256, 3) void generic_partial_kernel(Params p) {
+// P = BatchParams: rows of a batch with a window (lra_batch.h), keys numbered among those that the row sees.
+template <typename T, int D, bool PAGED, int RB, typename P = Params>
+__global__ __launch_bounds__(256, 3) void generic_partial_kernel(P p) {
+  constexpr bool BATCH = std::is_same_v<P, BatchParams>;
   constexpr int E = 16 / static_cast<int>(sizeof(T));  // elements per piece
   constexpr int CG = D / E;                            // pieces per row
   constexpr int PK = CG / 4;                           // pieces of a K row per lane; V rows per lane and step
@@ -173,7 +165,15 @@ __global__ __launch_bounds__(256, 3) void generic_partial_kernel(Params p) {
 
   // (scalar loads, both requested before either is waited for)
   int t, a, n_vis;
-  if (p.is_prefill) {
+  [[maybe_unused]] int n_sinks = 0, gap = 0;
+  if constexpr (BATCH) {
+    const BatchRow b = batch_row(p, tok);
+    t = b.t;
+    a = b.adapter;
+    n_vis = b.n_keys;
+    n_sinks = b.n_sinks;
+    gap = b.gap;
+  } else if (p.is_prefill) {
     t = p.seq_index;
     a = p.adapter_index;
     n_vis = min(CONST_I32(p.seq_lens)[t], p.max_seq_len) - p.n_new + tok + 1;
@@ -209,21 +209,25 @@ __global__ __launch_bounds__(256, 3) void generic_partial_kernel(Params p) {
 
   uint4 kp[PK], vp[PK];
   T lv[LN];
+  auto token = [&](int key) __attribute__((always_inline)) -> int {
+    if constexpr (BATCH) return key < n_sinks ? key : key + gap;
+    else return key;
+  };
   // (rows past the end: the last one again, weighted zero)
   auto request_v = [&](int jb) __attribute__((always_inline)) {
     int jk = jb + 16 * wave + kg;
     if constexpr (RB > 16) asm volatile("" : "+v"(jk));  // (row numbers formed again in each step, not held in registers)
 #pragma unroll
     for (int i = 0; i < PK; ++i)
-      vp[i] = reinterpret_cast<const uint4*>(vb + kv_row<PAGED>(p, t, min(jk + KGW * i, j1 - 1), h))[cg];
+      vp[i] = reinterpret_cast<const uint4*>(vb + kv_row<PAGED>(p, t, token(min(jk + KGW * i, j1 - 1)), h))[cg];
   };
   auto request_k = [&](int jb) __attribute__((always_inline)) {
-    const uint4* krow = reinterpret_cast<const uint4*>(kb + kv_row<PAGED>(p, t, min(jb + key_k, j1 - 1), h));
+    const uint4* krow = reinterpret_cast<const uint4*>(kb + kv_row<PAGED>(p, t, token(min(jb + key_k, j1 - 1)), h));
 #pragma unroll
     for (int i = 0; i < PK; ++i) kp[i] = krow[quarter + 4 * i];
   };
   auto request_l = [&](int jb) __attribute__((always_inline)) {
-    const T* lrow = lr + l_row<PAGED>(p, t, min(jb + key_k, j1 - 1), a);
+    const T* lrow = lr + l_row<PAGED>(p, t, token(min(jb + key_k, j1 - 1)), a);
     int q4 = quarter;
     if constexpr (!L_EARLY) asm volatile("" : "+v"(q4));  // (sixteen offsets formed again in each step, not held in registers)
 #pragma unroll
@@ -411,8 +415,9 @@ __global__ __launch_bounds__(256, 3) void generic_partial_kernel(Params p) {
 // pairs.  r * d multiply-adds per (row, key) instead of d + r: the price of the rotation
 // without materialising the keys.  Angles as in the cache-append producer: rates in double
 // precision and revolutions, fractional part, v_sin_f32 / v_cos_f32.
-template <typename T>
-__global__ __launch_bounds__(kWave) void generic_partial_rope_kernel(Params p) {
+template <typename T, typename P = Params>
+__global__ __launch_bounds__(kWave) void generic_partial_rope_kernel(P p) {
+  constexpr bool BATCH = std::is_same_v<P, BatchParams>;
   const int row = blockIdx.x;
   const int split = blockIdx.y;
   const int lane = threadIdx.x;
@@ -422,7 +427,15 @@ __global__ __launch_bounds__(kWave) void generic_partial_rope_kernel(Params p) {
   const int h = g / p.group;
 
   int t, a, n_vis;
-  if (p.is_prefill) {
+  [[maybe_unused]] int n_sinks = 0, gap = 0;
+  if constexpr (BATCH) {
+    const BatchRow b = batch_row(p, tok);
+    t = b.t;
+    a = b.adapter;
+    n_vis = b.n_keys;
+    n_sinks = b.n_sinks;
+    gap = b.gap;
+  } else if (p.is_prefill) {
     t = p.seq_index;
     a = p.adapter_index;
     const int n_t = min(p.seq_lens[t], p.max_seq_len);
@@ -462,9 +475,13 @@ __global__ __launch_bounds__(kWave) void generic_partial_rope_kernel(Params p) {
   const T* lr = static_cast<const T*>(p.l);
 
   float m = -INFINITY, ell = 0.f, o0 = 0.f, o1 = 0.f, olr = 0.f;
+  auto token = [&](int key) __attribute__((always_inline)) -> int {
+    if constexpr (BATCH) return key < n_sinks ? key : key + gap;
+    else return key;
+  };
   for (int jb = j0; jb < j1; jb += kWave) {
-    const int j = jb + lane;
-    const bool valid = j < j1;
+    const bool valid = jb + lane < j1;
+    const int j = token(jb + lane);
     // this lane's L row, as floats, where the lane can index it with a loop variable
     if (valid) {
       const T* lrow = lr + l_offset(p, t, j, a);
@@ -491,7 +508,7 @@ __global__ __launch_bounds__(kWave) void generic_partial_rope_kernel(Params p) {
     }
     const float m_new = fmaxf(m, wave_max(s));  // finite: lane 0 is always valid here
     const float alpha = (m == -INFINITY) ? 0.f : expf(m - m_new);
-    const float pj = valid ? expf(s - m_new) : 0.f;
+    const float pj = valid && !(BATCH && s == -INFINITY) ? expf(s - m_new) : 0.f;
     ell = alpha * ell + wave_sum(pj);
     o0 *= alpha;
     o1 *= alpha;
@@ -503,7 +520,7 @@ __global__ __launch_bounds__(kWave) void generic_partial_rope_kernel(Params p) {
       float v0[8], v1[8];
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        const T* v = vb + kv_offset(p, t, jb + min(jj0 + u, cnt - 1), h);
+        const T* v = vb + kv_offset(p, t, token(jb + min(jj0 + u, cnt - 1)), h);
         v0[u] = to_f32<T>(v[c0]);
         v1[u] = to_f32<T>(v[c1]);
       }
@@ -1151,11 +1168,12 @@ static void launch_merge_rows(const Params& p, int rows, hipStream_t s) {
   else by_rank(std::integral_constant<int, 64>{});
 }
 
-hipError_t launch_generic_partials(const Params& p, bool is_bf16, int rows, hipStream_t s) {
+template <typename P>
+static hipError_t launch_partials(const P& p, bool is_bf16, int rows, hipStream_t s) {
   const dim3 grid(rows, p.n_splits), block(kWave);
   if (p.key_rope_theta > 0.f && p.b_k != nullptr) {
-    if (is_bf16) hipLaunchKernelGGL(generic_partial_rope_kernel<bf16_t>, grid, block, 0, s, p);
-    else hipLaunchKernelGGL(generic_partial_rope_kernel<float>, grid, block, 0, s, p);
+    if (is_bf16) hipLaunchKernelGGL((generic_partial_rope_kernel<bf16_t, P>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((generic_partial_rope_kernel<float, P>), grid, block, 0, s, p);
     return hipGetLastError();
   }
   const int x = rows < (1 << kGenericRowBits) ? rows : (1 << kGenericRowBits);
@@ -1164,11 +1182,11 @@ hipError_t launch_generic_partials(const Params& p, bool is_bf16, int rows, hipS
     constexpr bool PAGED = decltype(paged_c)::value;
     constexpr int RB = decltype(rb_c)::value;
     if (p.head_dim == 128) {
-      if (is_bf16) hipLaunchKernelGGL((generic_partial_kernel<bf16_t, 128, PAGED, RB>), rgrid, dim3(256), 0, s, p);
-      else hipLaunchKernelGGL((generic_partial_kernel<float, 128, PAGED, RB>), rgrid, dim3(256), 0, s, p);
+      if (is_bf16) hipLaunchKernelGGL((generic_partial_kernel<bf16_t, 128, PAGED, RB, P>), rgrid, dim3(256), 0, s, p);
+      else hipLaunchKernelGGL((generic_partial_kernel<float, 128, PAGED, RB, P>), rgrid, dim3(256), 0, s, p);
     } else {
-      if (is_bf16) hipLaunchKernelGGL((generic_partial_kernel<bf16_t, 64, PAGED, RB>), rgrid, dim3(256), 0, s, p);
-      else hipLaunchKernelGGL((generic_partial_kernel<float, 64, PAGED, RB>), rgrid, dim3(256), 0, s, p);
+      if (is_bf16) hipLaunchKernelGGL((generic_partial_kernel<bf16_t, 64, PAGED, RB, P>), rgrid, dim3(256), 0, s, p);
+      else hipLaunchKernelGGL((generic_partial_kernel<float, 64, PAGED, RB, P>), rgrid, dim3(256), 0, s, p);
     }
   };
   auto by_rank = [&](auto paged_c) {
@@ -1179,6 +1197,9 @@ hipError_t launch_generic_partials(const Params& p, bool is_bf16, int rows, hipS
   else by_rank(std::false_type{});
   return hipGetLastError();
 }
+
+hipError_t launch_generic_partials(const Params& p, bool is_bf16, int rows, hipStream_t s) { return launch_partials(p, is_bf16, rows, s); }
+hipError_t launch_batch_partials(const BatchParams& p, bool is_bf16, int rows, hipStream_t s) { return launch_partials(p, is_bf16, rows, s); }
 
 template <typename T>
 static void launch_merge_t(const Params& p, bool is_bf16, int rows, hipStream_t s) {

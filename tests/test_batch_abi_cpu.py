@@ -1,0 +1,89 @@
+"""What the batch entry points refuse, before anything is launched (no GPU here)."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2602_01053_amd as lra
+from paper_2602_01053_amd.binding import LraAdapters, LraBatch, LraCache, LraShape
+
+NULL, SHAPE, DTYPE, UNSUP, WS = 1, 2, 3, 4, 5
+FAKE = 0x1000  # never dereferenced
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return lra.load_library()
+
+
+def good():
+    return (LraShape(32, 8, 128, 16, 0, 0.0), LraCache(FAKE, FAKE, FAKE, 1024, 128, 0, 0, 0, 0, 1, 0, 0, None, FAKE, 8192),
+            LraAdapters(FAKE, FAKE, 4), LraBatch(FAKE, FAKE, 4, 4, 0, 0, 0))
+
+
+def attend(lib, sh, c, ad, b, q=FAKE, out=FAKE, ws=FAKE, ws_bytes=0):
+    ref = lambda x: None if x is None else ctypes.byref(x)  # noqa: E731
+    return lib.lra_attn_batch(ref(sh), ref(c), ref(ad), ref(b), q, out, ws, ws_bytes, None, None)
+
+
+def test_attention_refuses_before_launch(lib):
+    sh, c, ad, b = good()
+    assert attend(lib, None, c, ad, b) == NULL and attend(lib, sh, None, ad, b) == NULL
+    assert attend(lib, sh, c, None, b) == NULL and attend(lib, sh, c, ad, None) == NULL
+    assert attend(lib, sh, c, ad, b, q=None) == NULL and attend(lib, sh, c, ad, b, out=None) == NULL
+    assert attend(lib, sh, c, ad, b, q=FAKE + 8) == SHAPE and attend(lib, sh, c, ad, b, out=FAKE + 2) == SHAPE
+    assert attend(lib, sh, c, ad, b) == WS                               # too small
+    assert attend(lib, sh, c, ad, b, ws=None, ws_bytes=1 << 40) == WS
+    assert attend(lib, sh, c, ad, b, ws=FAKE + 16, ws_bytes=1 << 40) == WS
+    for field, bad in (("n_queries", 0), ("n_queries", -3), ("max_queries_per_seq", 0), ("max_queries_per_seq", 5), ("window", -1),
+                       ("sinks", -1)):
+        sh, c, ad, b = good()
+        setattr(b, field, bad)
+        assert attend(lib, sh, c, ad, b) == SHAPE, field
+    for field in ("seq_query_start", "query_adapter"):
+        sh, c, ad, b = good()
+        setattr(b, field, None)
+        assert attend(lib, sh, c, ad, b) == NULL, field
+    for field, bad, want in (("dtype", 7, DTYPE), ("rank", 65, UNSUP), ("head_dim", 96, UNSUP), ("n_q_heads", 30, SHAPE),
+                             ("key_rope_theta", -1.0, SHAPE), ("scale", float("nan"), SHAPE)):
+        sh, c, ad, b = good()
+        setattr(sh, field, bad)
+        assert attend(lib, sh, c, ad, b) == want, field
+    sh, c, ad, b = good()
+    ad.n_adapters = 0
+    assert attend(lib, sh, c, ad, b) == SHAPE
+    sh, c, ad, b = good()
+    b.n_queries, b.max_queries_per_seq = 1 << 28, 1 << 28
+    assert attend(lib, sh, c, ad, b) == UNSUP
+
+
+def test_workspace_size_says_what_is_refused(lib):
+    refused = ctypes.c_size_t(-1).value
+    size = lambda sh, c, b: lib.lra_batch_workspace_bytes(ctypes.byref(sh), ctypes.byref(c), ctypes.byref(b), None)  # noqa: E731
+    sh, c, _, b = good()
+    assert 0 < size(sh, c, b) < refused
+    b.window = -1
+    assert size(sh, c, b) == refused
+    sh, c, _, b = good()
+    sh.rank = 65
+    assert size(sh, c, b) == refused
+    for window, sinks in ((1, 0), (2 ** 31 - 1, 2 ** 31 - 1), (2 ** 31 - 1, 0), (0, 2 ** 31 - 1)):  # sums stay in range
+        sh, c, _, b = good()
+        b.window, b.sinks, b.causal = window, sinks, 1
+        assert 0 < size(sh, c, b) < refused
+
+
+def test_binding_refuses_what_the_library_cannot_see():
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32)  # noqa: E731
+    with pytest.raises(lra.LraError):
+        lra.make_batch(i32(0, 2).long(), i32(0, 1), 2)
+    with pytest.raises(lra.LraError):
+        lra.make_batch(i32(0, 2), torch.zeros(4, dtype=torch.int32)[::2], 2)
+    batch = lra.make_batch(i32(0, 2), i32(0, 1), 2, window=8, sinks=1)
+    assert (batch.n_queries, batch.window, batch.sinks, batch.causal) == (2, 8, 1, 0)
+    q = torch.zeros(2, 4, 64)
+    sh = lra.make_shape(q, 2, 8)
+    _, c, _, _ = good()
+    for bad_q, bad_out in ((q[:1], q), (q, q.bfloat16()), (q.transpose(0, 1).contiguous().transpose(0, 1), q)):
+        with pytest.raises(lra.LraError):
+            lra.lra_attn_batch(sh, c, None, None, 1, batch, bad_q, bad_out, None)
