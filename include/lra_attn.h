@@ -446,6 +446,31 @@ lra_status lra_attn_batch(const lra_shape* shape, const lra_cache* cache, const 
 size_t lra_batch_workspace_bytes(const lra_shape* shape, const lra_cache* cache, const lra_batch* batch,
                                  const lra_tuning* tuning);
 
+/*
+ * The attention weight that every cached token received from a batch of queries, added to a running sum: what a
+ * cache that may not grow goes by when it lets tokens go.  For j < seq_lens[t]
+ *     weights[t][j] = decay * weights[t][j] + sum over the queries of sequence t and the Hq heads of P[j],
+ * P the softmax of the query's scores (as lra_attn_batch has them: same mask, scale and key-side adapters; zero where
+ * the query does not see j).  One sum per token and not per head: the L row of a token serves every head and every
+ * agent, so a token leaves the cache for all of them or for none.  For a prompt, the queries may be its last few
+ * tokens only (causal): the batch need not hold every new token.
+ *
+ *   adapters   b_v is not used
+ *   decay      finite; 0: the old values are not read, so they may hold anything
+ *   weights    DEVICE float [n_seqs][weights_stride], weights_stride >= max_seq_len; entries at and past
+ *              seq_lens[t] are left as they are.  Held in fp32 whatever the caches' type, and the scores of bf16
+ *              caches are formed from q B_K^T in 16 bits of mantissa, so that small sums keep their order.
+ *   workspace  DEVICE, 256-byte aligned, >= lra_key_weights_workspace_bytes(...), as for lra_attn_batch
+ * A rotated key-side adapter (key_rope_theta > 0 with a b_k) is LRA_ERR_UNSUPPORTED: its keys depend on the token's
+ * index, which an eviction changes.
+ */
+lra_status lra_key_weights(const lra_shape* shape, const lra_cache* cache, const lra_adapters* adapters,
+                           const lra_batch* batch, const void* q, float decay, float* weights, int64_t weights_stride,
+                           void* workspace, size_t workspace_bytes, const lra_tuning* tuning, void* stream);
+/* (size_t)-1 when the arguments would be rejected. */
+size_t lra_key_weights_workspace_bytes(const lra_shape* shape, const lra_cache* cache, const lra_batch* batch,
+                                       const lra_tuning* tuning);
+
 /* Static, NUL-terminated description of a status code. */
 const char* lra_status_string(lra_status status);
 

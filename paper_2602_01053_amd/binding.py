@@ -22,7 +22,7 @@ STATIC_WORKSPACE_BYTES = 64 << 20   # LRA_STATIC_WORKSPACE_BYTES of the header
 
 EXPORTS = ("lra_workspace_bytes", "lra_attn_decode", "lra_attn_decode_static", "lra_attn_prefill", "lra_status_string",
            "lra_cache_append", "lra_append_workspace_bytes", "lra_probe_stream_read", "lra_probe_mfma_bf16",
-           "lra_attn_batch", "lra_batch_workspace_bytes")
+           "lra_attn_batch", "lra_batch_workspace_bytes", "lra_key_weights", "lra_key_weights_workspace_bytes")
 
 
 class LraShape(ctypes.Structure):
@@ -157,6 +157,10 @@ def load_library() -> ctypes.CDLL:
     lib.lra_attn_batch.argtypes = [sp, cp, ap, bp, vp, vp, vp, ctypes.c_size_t, tp, vp]
     lib.lra_batch_workspace_bytes.restype = ctypes.c_size_t
     lib.lra_batch_workspace_bytes.argtypes = [sp, cp, bp, tp]
+    lib.lra_key_weights.restype = ctypes.c_int
+    lib.lra_key_weights.argtypes = [sp, cp, ap, bp, vp, ctypes.c_float, vp, ctypes.c_int64, vp, ctypes.c_size_t, tp, vp]
+    lib.lra_key_weights_workspace_bytes.restype = ctypes.c_size_t
+    lib.lra_key_weights_workspace_bytes.argtypes = [sp, cp, bp, tp]
     lib.lra_probe_stream_read.restype = ctypes.c_int
     lib.lra_probe_stream_read.argtypes = [vp, ctypes.c_size_t, vp, vp]
     lib.lra_probe_mfma_bf16.restype = ctypes.c_int
@@ -434,3 +438,33 @@ def lra_attn_batch(shape: LraShape, cache: LraCache, b_k: Optional[torch.Tensor]
     ad = LraAdapters(_ptr(b_k), _ptr(b_v), int(n_adapters))
     _check(load_library().lra_attn_batch(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(ad), ctypes.byref(batch), _ptr(q),
                                          _ptr(out), *_workspace_args(workspace), _tuning_ref, _stream_ptr(stream)))
+
+
+def lra_key_weights_workspace_bytes(shape: LraShape, cache: LraCache, batch: LraBatch) -> int:
+    n = load_library().lra_key_weights_workspace_bytes(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(batch), _tuning_ref)
+    if n == ctypes.c_size_t(-1).value:
+        raise LraError(2, "lra_key_weights_workspace_bytes rejected the arguments")
+    return int(n)
+
+
+def _check_weights(cache: LraCache, weights: torch.Tensor) -> None:
+    if weights.dtype != torch.float32 or weights.dim() != 2 or weights.size(0) != cache.n_seqs or weights.stride(1) != 1:
+        raise LraError(2, f"weights must be float32 [{cache.n_seqs}][tokens], unit stride on the tokens")
+    if weights.size(1) < cache.max_seq_len:
+        raise LraError(2, f"weights must have room for {cache.max_seq_len} tokens of each sequence")
+
+
+def _row_stride(t: torch.Tensor) -> int:
+    return t.stride(0) if t.size(0) > 1 else t.size(1)
+
+
+def lra_key_weights(shape: LraShape, cache: LraCache, b_k: Optional[torch.Tensor], n_adapters: int, batch: LraBatch, q: torch.Tensor,
+                    decay: float, weights: torch.Tensor, workspace: Optional[torch.Tensor], stream=None) -> None:
+    """weights[t][j] = decay * weights[t][j] + the attention weight that token j of sequence t receives from the batch's
+    queries, all heads together.  weights: float32 [n_seqs][>= max_seq_len]."""
+    _check_rows(batch, shape, q)
+    _check_weights(cache, weights)
+    ad = LraAdapters(_ptr(b_k), None, int(n_adapters))
+    _check(load_library().lra_key_weights(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(ad), ctypes.byref(batch), _ptr(q),
+                                          float(decay), _ptr(weights), _row_stride(weights), *_workspace_args(workspace), _tuning_ref,
+                                          _stream_ptr(stream)))

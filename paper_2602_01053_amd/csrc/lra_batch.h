@@ -1,6 +1,7 @@
 // Batches of queries with a window (lra_batch of the header): kernel parameters and what a query sees.
 #pragma once
 
+#include "lra_attn.h"
 #include "lra_common.h"
 
 namespace lra {
@@ -40,6 +41,14 @@ __device__ __forceinline__ BatchRow batch_row(const BatchParams& p, int tok) {
   b.n_keys = pos < 0 ? 0 : pos + 1 - b.gap;
   return b;
 }
+
+// Whether a query at position pos sees token j.
+__device__ __forceinline__ bool batch_sees(const BatchParams& p, int pos, int j) {
+  return j <= pos && (p.window == 0 || j > pos - p.window || j < p.sinks);
+}
+
+// Parameters of a call out of the ABI's structs (pointers of the workspace and of the outputs left NULL).
+BatchParams batch_params(const lra_shape* sh, const lra_cache* c, const lra_adapters* ad, const lra_batch* b, const void* q);
 
 hipError_t launch_batch_partials(const BatchParams& p, bool is_bf16, int rows, hipStream_t s);
 // States of n_splits key shares per row -> out; rows without any give zeros

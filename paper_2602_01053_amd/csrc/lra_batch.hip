@@ -82,8 +82,8 @@ hipError_t launch_batch_merge(const BatchParams& p, bool is_bf16, int rows, hipS
   return hipGetLastError();
 }
 
-static void fill_batch_params(BatchParams& p, const lra_shape* sh, const lra_cache* c, const lra_adapters* ad,
-                              const lra_batch* b, const void* q) {
+BatchParams batch_params(const lra_shape* sh, const lra_cache* c, const lra_adapters* ad, const lra_batch* b, const void* q) {
+  BatchParams p{};
   p.q = q;
   p.k_base = c->k_base;
   p.v_base = c->v_base;
@@ -118,6 +118,7 @@ static void fill_batch_params(BatchParams& p, const lra_shape* sh, const lra_cac
   p.causal = b->causal != 0;
   p.window = b->window;
   p.sinks = b->window > 0 ? b->sinks : 0;
+  return p;
 }
 
 }  // namespace lra
@@ -144,8 +145,7 @@ lra_status lra_attn_batch(const lra_shape* shape, const lra_cache* cache, const 
   const BatchPlan pl = plan_batch(shape, cache, batch, resolve_tuning(tuning));
   if (!pl.launchable) return LRA_ERR_UNSUPPORTED;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < pl.bytes) return LRA_ERR_WORKSPACE;
-  BatchParams p{};
-  fill_batch_params(p, shape, cache, adapters, batch, q);
+  BatchParams p = batch_params(shape, cache, adapters, batch, q);
   char* ws = static_cast<char*>(workspace);
   p.out = out;
   p.part_ml = reinterpret_cast<float*>(ws + pl.off_ml);

@@ -49,4 +49,15 @@ BatchPlan plan_batch(const lra_shape* sh, const lra_cache* c, const lra_batch* b
   return pl;
 }
 
+WeightsPlan plan_key_weights(const lra_shape* sh, const lra_cache* c, const lra_batch* b, const Tuning& tune) {
+  (void)c;
+  (void)tune;
+  WeightsPlan pl{};
+  pl.rows = b->n_queries * sh->n_q_heads;  // (checked: at most 2^30)
+  pl.off_qt = 0;
+  pl.off_lse = aligned(static_cast<size_t>(pl.rows) * sh->rank * sizeof(float));
+  pl.bytes = pl.off_lse + aligned(static_cast<size_t>(pl.rows) * sizeof(float));
+  return pl;
+}
+
 }  // namespace lra

@@ -16,4 +16,11 @@ struct BatchPlan {
 };
 BatchPlan plan_batch(const lra_shape* sh, const lra_cache* c, const lra_batch* b, const Tuning& tune);
 
+// lra_key_weights: the query rows' Q B_K^T and softmax statistics, then the sums over rows key by key.
+struct WeightsPlan {
+  int rows;
+  size_t off_qt, off_lse, bytes;
+};
+WeightsPlan plan_key_weights(const lra_shape* sh, const lra_cache* c, const lra_batch* b, const Tuning& tune);
+
 }  // namespace lra

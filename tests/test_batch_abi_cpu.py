@@ -87,3 +87,26 @@ def test_binding_refuses_what_the_library_cannot_see():
     for bad_q, bad_out in ((q[:1], q), (q, q.bfloat16()), (q.transpose(0, 1).contiguous().transpose(0, 1), q)):
         with pytest.raises(lra.LraError):
             lra.lra_attn_batch(sh, c, None, None, 1, batch, bad_q, bad_out, None)
+
+
+def weigh(lib, sh, c, ad, b, q=FAKE, decay=1.0, w=FAKE, stride=8192, ws=FAKE, ws_bytes=0):
+    ref = lambda x: None if x is None else ctypes.byref(x)  # noqa: E731
+    return lib.lra_key_weights(ref(sh), ref(c), ref(ad), ref(b), q, decay, w, stride, ws, ws_bytes, None, None)
+
+
+def test_key_weights_refuse_before_launch(lib):
+    sh, c, ad, b = good()
+    assert weigh(lib, None, c, ad, b) == NULL and weigh(lib, sh, c, None, b) == NULL and weigh(lib, sh, c, ad, None) == NULL
+    assert weigh(lib, sh, c, ad, b, q=None) == NULL and weigh(lib, sh, c, ad, b, w=None) == NULL
+    assert weigh(lib, sh, c, ad, b) == WS
+    assert weigh(lib, sh, c, ad, b, stride=8191) == SHAPE and weigh(lib, sh, c, ad, b, w=FAKE + 2) == SHAPE
+    for decay in (float("nan"), float("inf")):
+        assert weigh(lib, sh, c, ad, b, decay=decay) == SHAPE
+    sh.key_rope_theta = 10000.0
+    assert weigh(lib, sh, c, ad, b) == UNSUP
+    ad.b_k = None                                  # nothing is rotated then
+    assert weigh(lib, sh, c, ad, b) == WS
+    sh, c, ad, b = good()
+    b.n_queries = b.max_queries_per_seq = 1 << 25  # 2^30 rows of 16 ranks
+    assert weigh(lib, sh, c, ad, b, ws_bytes=1 << 50) == UNSUP
+    assert lib.lra_key_weights_workspace_bytes(ctypes.byref(sh), ctypes.byref(c), ctypes.byref(b), None) == ctypes.c_size_t(-1).value
