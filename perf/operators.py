@@ -215,13 +215,11 @@ def prepare(case, seed):
         s.cache = lra.make_cache(s.k, s.v, s.l, s.seq_lens, max(lengths), s.block_table, seq_lens_host=lengths)
         if case["op"] == "evict":
             s.dst_cache = lra.make_cache(*s.dst, s.new_lens, case["budget"], s.dst_table)
-            need = lra.lra_evict_workspace_bytes(s.cache, case["budget"])
         else:
             s.batch = lra.make_batch(s.start, s.query_adapter, s.most, causal=case["causal"], window=case["window"],
                                      sinks=case["sinks"])
             size = lra.lra_batch_workspace_bytes if case["op"] == "attend" else lra.lra_key_weights_workspace_bytes
-            need = size(s.shape, s.cache, s.batch)
-        s.workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+            s.workspace = torch.empty(max(size(s.shape, s.cache, s.batch), 256), dtype=torch.uint8, device=dev)
     return s
 
 
@@ -235,7 +233,7 @@ def run(s):
         if case["op"] == "weights":
             lra.lra_key_weights(s.shape, s.cache, s.b_k, s.n_adapters, s.batch, s.q, case["decay"], s.weights, s.workspace)
             return s.weights
-        lra.lra_evict_select(s.cache, s.weights, case["budget"], case["sinks"], case["recent"], s.kept, s.new_lens, s.workspace)
+        lra.lra_evict_select(s.cache, s.weights, case["budget"], case["sinks"], case["recent"], s.kept, s.new_lens)
         lra.lra_cache_gather(s.shape, s.cache, s.kept, s.dst_cache, weights=s.weights, dst_weights=s.dst_weights)
     elif case["op"] == "attend":
         return _plain_attend(s)
