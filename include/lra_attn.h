@@ -471,6 +471,40 @@ lra_status lra_key_weights(const lra_shape* shape, const lra_cache* cache, const
 size_t lra_key_weights_workspace_bytes(const lra_shape* shape, const lra_cache* cache, const lra_batch* batch,
                                        const lra_tuning* tuning);
 
+/*
+ * Which tokens of every sequence stay when its cache is cut to `budget` tokens.  A sequence of at most `budget` tokens
+ * keeps them all.  Of a longer one stay the first `sinks`, the last `recent`, and of those between the
+ * budget - sinks - recent with the largest weight, of equal ones the first (NaN counts as less than any number, -0 as 0).
+ *
+ *   cache      its seq_lens, n_seqs and max_seq_len are used, nothing else
+ *   weights    DEVICE float [n_seqs][weights_stride], weights_stride >= max_seq_len, for instance lra_key_weights's
+ *   budget     >= 1, sinks >= 0, recent >= 0, sinks + recent <= budget
+ *   kept       DEVICE int32 [n_seqs][kept_stride], kept_stride >= min(budget, max_seq_len): the tokens that stay, in
+ *              order; entries behind them are left as they are
+ *   new_lens   DEVICE int32 [n_seqs]: how many stay, min(seq_lens[t], budget); may be cache->seq_lens itself
+ */
+lra_status lra_evict_select(const lra_cache* cache, const float* weights, int64_t weights_stride, int32_t budget,
+                            int32_t sinks, int32_t recent, int32_t* kept, int64_t kept_stride, int32_t* new_lens,
+                            void* stream);
+
+/*
+ * The caches of the tokens that stay: row i of sequence t of dst becomes row kept[t][i] of src, for i < dst->seq_lens[t]
+ * (at most dst->max_seq_len), in K_base, V_base, L and, where both are given, the weights; rows behind are left as they
+ * are.  dst is a cache as for the attention calls, whose k_base / v_base / l are WRITTEN although declared const in the
+ * struct; its seq_lens are the new lengths that lra_evict_select has left.  src and dst may differ in layout (contiguous or
+ * paged, strides), and may lie in one pool of pages, but no row of dst may be a row of src: neither may have the other's
+ * block table, nor contiguous caches the same memory.
+ *
+ *   n_adapters   low-rank caches to move, >= 1; more than one only where both caches have an l_adapter_stride
+ *   kept         DEVICE int32 [n_seqs][kept_stride], kept_stride >= dst->max_seq_len; entries in [0, src length)
+ *   weights, dst_weights   DEVICE float [n_seqs][...] or both NULL; strides >= the max_seq_len of src and dst
+ * key_rope_theta > 0 is LRA_ERR_UNSUPPORTED: K_base may hold rotated keys (they keep the angles of their first
+ * positions), but an adapter's part that is rotated by the token's index would turn with the move.
+ */
+lra_status lra_cache_gather(const lra_shape* shape, const lra_cache* src, int32_t n_adapters, const int32_t* kept,
+                            int64_t kept_stride, const lra_cache* dst, const float* weights, int64_t weights_stride,
+                            float* dst_weights, int64_t dst_weights_stride, void* stream);
+
 /* Static, NUL-terminated description of a status code. */
 const char* lra_status_string(lra_status status);
 

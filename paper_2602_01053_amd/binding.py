@@ -22,7 +22,8 @@ STATIC_WORKSPACE_BYTES = 64 << 20   # LRA_STATIC_WORKSPACE_BYTES of the header
 
 EXPORTS = ("lra_workspace_bytes", "lra_attn_decode", "lra_attn_decode_static", "lra_attn_prefill", "lra_status_string",
            "lra_cache_append", "lra_append_workspace_bytes", "lra_probe_stream_read", "lra_probe_mfma_bf16",
-           "lra_attn_batch", "lra_batch_workspace_bytes", "lra_key_weights", "lra_key_weights_workspace_bytes")
+           "lra_attn_batch", "lra_batch_workspace_bytes", "lra_key_weights", "lra_key_weights_workspace_bytes",
+           "lra_evict_select", "lra_cache_gather")
 
 
 class LraShape(ctypes.Structure):
@@ -161,6 +162,11 @@ def load_library() -> ctypes.CDLL:
     lib.lra_key_weights.argtypes = [sp, cp, ap, bp, vp, ctypes.c_float, vp, ctypes.c_int64, vp, ctypes.c_size_t, tp, vp]
     lib.lra_key_weights_workspace_bytes.restype = ctypes.c_size_t
     lib.lra_key_weights_workspace_bytes.argtypes = [sp, cp, bp, tp]
+    i64 = ctypes.c_int64
+    lib.lra_evict_select.restype = ctypes.c_int
+    lib.lra_evict_select.argtypes = [cp, vp, i64, i32, i32, i32, vp, i64, vp, vp]
+    lib.lra_cache_gather.restype = ctypes.c_int
+    lib.lra_cache_gather.argtypes = [sp, cp, i32, vp, i64, cp, vp, i64, vp, i64, vp]
     lib.lra_probe_stream_read.restype = ctypes.c_int
     lib.lra_probe_stream_read.argtypes = [vp, ctypes.c_size_t, vp, vp]
     lib.lra_probe_mfma_bf16.restype = ctypes.c_int
@@ -468,3 +474,35 @@ def lra_key_weights(shape: LraShape, cache: LraCache, b_k: Optional[torch.Tensor
     _check(load_library().lra_key_weights(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(ad), ctypes.byref(batch), _ptr(q),
                                           float(decay), _ptr(weights), _row_stride(weights), *_workspace_args(workspace), _tuning_ref,
                                           _stream_ptr(stream)))
+
+
+def _check_kept(cache: LraCache, kept: torch.Tensor, tokens: int) -> None:
+    if kept.dtype != torch.int32 or kept.dim() != 2 or kept.size(0) != cache.n_seqs or kept.stride(1) != 1 or kept.size(1) < tokens:
+        raise LraError(2, f"kept must be int32 [{cache.n_seqs}][>= {tokens}], unit stride on the tokens")
+
+
+def lra_evict_select(cache: LraCache, weights: torch.Tensor, budget: int, sinks: int, recent: int, kept: torch.Tensor,
+                     new_lens: torch.Tensor, stream=None) -> None:
+    """The tokens of every sequence that stay in a cache of `budget` tokens: the first `sinks`, the last `recent` and the
+    heaviest between them.  kept: int32 [n_seqs][>= budget], new_lens: int32 [n_seqs]."""
+    _check_weights(cache, weights)
+    _check_kept(cache, kept, min(int(budget), cache.max_seq_len))
+    if new_lens.dtype != torch.int32 or not new_lens.is_contiguous() or new_lens.numel() != cache.n_seqs:
+        raise LraError(2, f"new_lens must be a dense int32 vector of {cache.n_seqs}")
+    _check(load_library().lra_evict_select(ctypes.byref(cache), _ptr(weights), _row_stride(weights), int(budget), int(sinks), int(recent),
+                                           _ptr(kept), _row_stride(kept), _ptr(new_lens), _stream_ptr(stream)))
+
+
+def lra_cache_gather(shape: LraShape, cache: LraCache, kept: torch.Tensor, dst: LraCache, n_adapters: int = 1,
+                     weights: Optional[torch.Tensor] = None, dst_weights: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Row i of sequence t of the cache dst becomes row kept[t][i] of `cache`, for i below dst's lengths (those that
+    lra_evict_select has left): K_base, V_base, the L rows of n_adapters adapters, and the weights where both are given."""
+    _check_kept(cache, kept, dst.max_seq_len)
+    if (weights is None) != (dst_weights is None):
+        raise LraError(1, "weights and dst_weights: both or neither")
+    if weights is not None:
+        _check_weights(cache, weights)
+        _check_weights(dst, dst_weights)
+    _check(load_library().lra_cache_gather(ctypes.byref(shape), ctypes.byref(cache), int(n_adapters), _ptr(kept), _row_stride(kept),
+                                           ctypes.byref(dst), _ptr(weights), 0 if weights is None else _row_stride(weights),
+                                           _ptr(dst_weights), 0 if weights is None else _row_stride(dst_weights), _stream_ptr(stream)))

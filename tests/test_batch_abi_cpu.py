@@ -110,3 +110,45 @@ def test_key_weights_refuse_before_launch(lib):
     b.n_queries = b.max_queries_per_seq = 1 << 25  # 2^30 rows of 16 ranks
     assert weigh(lib, sh, c, ad, b, ws_bytes=1 << 50) == UNSUP
     assert lib.lra_key_weights_workspace_bytes(ctypes.byref(sh), ctypes.byref(c), ctypes.byref(b), None) == ctypes.c_size_t(-1).value
+
+
+def test_eviction_refuses_before_launch(lib):
+    def select(c, w=FAKE, stride=8192, budget=100, sinks=4, recent=10, kept=FAKE, ks=100, new=FAKE):
+        return lib.lra_evict_select(None if c is None else ctypes.byref(c), w, stride, budget, sinks, recent, kept, ks, new, None)
+    _, c, _, _ = good()
+    assert select(None) == NULL and select(c, w=None) == NULL and select(c, kept=None) == NULL and select(c, new=None) == NULL
+    for bad in (dict(budget=0), dict(sinks=-1), dict(recent=-1), dict(sinks=95), dict(sinks=2 ** 31 - 1, recent=2 ** 31 - 1), dict(stride=8191),
+                dict(ks=99), dict(w=FAKE + 1), dict(kept=FAKE + 2), dict(new=FAKE + 3)):
+        assert select(c, **bad) == SHAPE, bad
+    c.max_seq_len = (1 << 30) + 1
+    assert select(c, stride=1 << 31) == UNSUP
+    c.max_seq_len = 0
+    assert select(c) == SHAPE
+
+
+def test_gather_refuses_before_launch(lib):
+    def gather(sh, src, dst, n=1, kept=FAKE, ks=4096, w=None, wst=0, w2=None, w2st=0):
+        ref = lambda x: None if x is None else ctypes.byref(x)  # noqa: E731
+        return lib.lra_cache_gather(ref(sh), ref(src), n, kept, ks, ref(dst), w, wst, w2, w2st, None)
+
+    def two():
+        sh, src, _, _ = good()
+        return sh, src, LraCache(2 * FAKE, 2 * FAKE, 2 * FAKE, 1024, 128, 0, 0, 0, 0, 1, 0, 0, None, FAKE, 4096)
+    sh, src, dst = two()
+    assert gather(None, src, dst) == NULL and gather(sh, None, dst) == NULL and gather(sh, src, None) == NULL
+    assert gather(sh, src, dst, kept=None) == NULL and gather(sh, src, dst, w=FAKE) == NULL and gather(sh, src, dst, w2=FAKE) == NULL
+    assert gather(sh, src, dst, ks=4095) == SHAPE and gather(sh, src, dst, n=0) == SHAPE and gather(sh, src, dst, n=2) == SHAPE
+    assert gather(sh, src, dst, w=FAKE, wst=8191, w2=FAKE, w2st=4096) == SHAPE
+    assert gather(sh, src, dst, w=FAKE, wst=8192, w2=FAKE, w2st=4095) == SHAPE
+    assert gather(sh, src, src, ks=8192) == SHAPE                       # in place
+    for field in ("k_base", "v_base", "l"):
+        sh, src, dst = two()
+        setattr(dst, field, FAKE)
+        assert gather(sh, src, dst) == SHAPE, field
+    sh, src, dst = two()
+    sh.key_rope_theta = 10000.0
+    assert gather(sh, src, dst) == UNSUP
+    page = lambda table: LraCache(FAKE, FAKE, FAKE, 128, 2048, 16384, 16, 512, 600, 3, 0, 0, table, FAKE, 8192)  # noqa: E731
+    sh, src, dst = two()
+    assert gather(sh, page(FAKE), dst) == SHAPE                         # three sequences and one
+    assert gather(sh, page(FAKE), page(FAKE), ks=8192) == SHAPE         # one table over one pool
