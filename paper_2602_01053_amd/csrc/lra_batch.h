@@ -9,6 +9,7 @@ namespace lra {
 // (fields of its own block: longer parameters would move those of the other kernels)
 struct BatchParams : Params {
   int32_t causal, window, sinks;
+  int32_t tile_places;  // batch_tiles_kernel: places of q tiles per kv head (batch_places, or the queries)
 };
 
 // Sequence of query `tok`: the last t with seq_query_start[t] <= tok.
@@ -42,6 +43,55 @@ __device__ __forceinline__ BatchRow batch_row(const BatchParams& p, int tok) {
   return b;
 }
 
+// The q tiles of a batch (lra_prefill_body.h): 128 rows of one sequence's chunk at most, a row being a new token of one of the
+// q heads of a kv head.  Without `causal` a tile is one query, since every query may have its own adapter.
+struct BatchTiles {
+  int t, adapter, n_t;
+  int first_query, n_queries;  // the queries of the chunk
+  int first_pos;               // position of the first of them
+  int tile;                    // of the chunk's tiles; past the last: nothing to do
+};
+
+// Sequence t takes ceil(c_t G / 128) tiles, and has the places from floor(start_t G / 128) + t on: at least as many, since
+// floor(a + b) >= floor(a) + floor(b), and found without a running sum over the sequences.  Place `at` is looked for by the
+// 64 lanes of a wave, sixty-four times fewer sequences a step.
+__device__ __forceinline__ int batch_places(int n_queries, int group, int n_seqs) {
+  return static_cast<int>((static_cast<int64_t>(n_queries) * group) >> 7) + n_seqs;
+}
+__device__ __forceinline__ BatchTiles batch_tiles(const BatchParams& p, int at, int lane) {
+  BatchTiles b;
+  if (!p.causal) {
+    b.t = p.n_seqs > 1 ? __builtin_amdgcn_readfirstlane(sequence_of_query(p, at)) : 0;
+    b.first_query = at;
+    b.n_queries = 1;
+    b.tile = 0;
+    b.n_t = __builtin_amdgcn_readfirstlane(min(p.seq_lens[b.t], p.max_seq_len));
+    b.first_pos = b.n_t - 1;
+    b.adapter = __builtin_amdgcn_readfirstlane(min(max(p.query_adapter[at], 0), p.n_adapters - 1));
+    return b;
+  }
+  auto first_of = [&](int t) __attribute__((always_inline)) -> int {
+    return t >= p.n_seqs ? p.n_queries : (t == 0 ? 0 : min(max(p.seq_query_start[t], 0), p.n_queries));
+  };
+  int lo = 0, cnt = p.n_seqs;
+  while (cnt > 1) {
+    const int step = (cnt + 63) >> 6;
+    const int t = lo + lane * step;
+    const bool before = t < lo + cnt && (t == lo || batch_places(first_of(t), p.group, t) <= at);
+    const int k = 63 - __builtin_clzll(__builtin_amdgcn_ballot_w64(before));
+    cnt = min(step, lo + cnt - (lo + k * step));
+    lo += k * step;
+  }
+  b.t = lo;
+  b.first_query = __builtin_amdgcn_readfirstlane(first_of(lo));
+  const int end = __builtin_amdgcn_readfirstlane(first_of(lo + 1));
+  b.n_queries = max(0, end - b.first_query);
+  b.tile = at - batch_places(b.first_query, p.group, lo);
+  b.n_t = __builtin_amdgcn_readfirstlane(min(p.seq_lens[lo], p.max_seq_len));
+  b.first_pos = b.n_t - b.n_queries;
+  b.adapter = b.n_queries > 0 ? __builtin_amdgcn_readfirstlane(min(max(p.query_adapter[b.first_query], 0), p.n_adapters - 1)) : 0;
+  return b;
+}
 // Whether a query at position pos sees token j.
 __device__ __forceinline__ bool batch_sees(const BatchParams& p, int pos, int j) {
   return j <= pos && (p.window == 0 || j > pos - p.window || j < p.sinks);
@@ -50,6 +100,9 @@ __device__ __forceinline__ bool batch_sees(const BatchParams& p, int pos, int j)
 // Parameters of a call out of the ABI's structs (pointers of the workspace and of the outputs left NULL).
 BatchParams batch_params(const lra_shape* sh, const lra_cache* c, const lra_adapters* ad, const lra_batch* b, const void* q);
 
+// part_ml NULL: no states, the outputs themselves (n_splits 1)
+hipError_t launch_batch_tiles_d64(const BatchParams& p, hipStream_t s);
+hipError_t launch_batch_tiles_d128(const BatchParams& p, hipStream_t s);
 hipError_t launch_batch_partials(const BatchParams& p, bool is_bf16, int rows, hipStream_t s);
 // States of n_splits key shares per row -> out; rows without any give zeros
 hipError_t launch_batch_merge(const BatchParams& p, bool is_bf16, int rows, hipStream_t s);

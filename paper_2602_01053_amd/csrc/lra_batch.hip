@@ -116,8 +116,9 @@ BatchParams batch_params(const lra_shape* sh, const lra_cache* c, const lra_adap
   p.scale = sh->scale > 0.f ? sh->scale : 1.0f / std::sqrt(static_cast<float>(sh->head_dim));
   p.key_rope_theta = sh->key_rope_theta;
   p.causal = b->causal != 0;
-  p.window = b->window;
-  p.sinks = b->window > 0 ? b->sinks : 0;
+  // (longer ones change nothing, and sums with positions stay in 32 bits)
+  p.window = b->window < c->max_seq_len ? b->window : c->max_seq_len;
+  p.sinks = b->window <= 0 ? 0 : (b->sinks < c->max_seq_len ? b->sinks : c->max_seq_len);
   return p;
 }
 
@@ -144,20 +145,28 @@ lra_status lra_attn_batch(const lra_shape* shape, const lra_cache* cache, const 
     return LRA_ERR_SHAPE;
   const BatchPlan pl = plan_batch(shape, cache, batch, resolve_tuning(tuning));
   if (!pl.launchable) return LRA_ERR_UNSUPPORTED;
-  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < pl.bytes) return LRA_ERR_WORKSPACE;
+  if (pl.bytes > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < pl.bytes)) return LRA_ERR_WORKSPACE;
   BatchParams p = batch_params(shape, cache, adapters, batch, q);
-  char* ws = static_cast<char*>(workspace);
   p.out = out;
-  p.part_ml = reinterpret_cast<float*>(ws + pl.off_ml);
-  p.part_o = reinterpret_cast<float*>(ws + pl.off_o);
-  p.part_lr = reinterpret_cast<float*>(ws + pl.off_lr);
-  p.part_adapter = reinterpret_cast<int32_t*>(ws + pl.off_adapter);
   p.split_keys = pl.split_keys;
   p.n_splits = pl.n_splits;
+  if (pl.states) {
+    char* ws = static_cast<char*>(workspace);
+    p.part_ml = reinterpret_cast<float*>(ws + pl.off_ml);
+    p.part_o = reinterpret_cast<float*>(ws + pl.off_o);
+    p.part_lr = reinterpret_cast<float*>(ws + pl.off_lr);
+    p.part_adapter = reinterpret_cast<int32_t*>(ws + pl.off_adapter);
+  }
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bool bf16 = shape->dtype == LRA_BF16;
-  if (launch_batch_partials(p, bf16, pl.rows, s) != hipSuccess) return LRA_ERR_HIP;
-  if (launch_batch_merge(p, bf16, pl.rows, s) != hipSuccess) return LRA_ERR_HIP;
+  if (pl.tiles) {
+    p.row_mul = (65535 + p.group) / p.group;
+    p.tile_places = pl.tile_places;
+    if ((p.head_dim == 128 ? launch_batch_tiles_d128(p, s) : launch_batch_tiles_d64(p, s)) != hipSuccess) return LRA_ERR_HIP;
+  } else if (launch_batch_partials(p, bf16, pl.rows, s) != hipSuccess) {
+    return LRA_ERR_HIP;
+  }
+  if (pl.states && launch_batch_merge(p, bf16, pl.rows, s) != hipSuccess) return LRA_ERR_HIP;
   return LRA_OK;
 }
 

@@ -21,10 +21,57 @@ static int64_t keys_per_row(const lra_cache* c, const lra_batch* b) {
   return b->window > 0 ? std::min<int64_t>(c->max_seq_len, static_cast<int64_t>(b->window) + b->sinks) : c->max_seq_len;
 }
 
+// Whether the MFMA kernels can address the caches: a contiguous kv head's rows, and the low-rank rows of one adapter, by
+// 32-bit byte offsets inside one buffer resource, below the offset that stands for "outside" (2^31).
+static bool mfma_fits(const lra_shape* sh, const lra_cache* c) {
+  const int64_t lim = (int64_t{1} << 31) - 4096;
+  const int64_t pitch = c->l_row_stride ? c->l_row_stride : sh->rank;
+  const int64_t l_rows = c->block_size == 0 ? c->max_seq_len : static_cast<int64_t>(c->num_blocks) * 16;
+  if (pitch > lim / 2 / l_rows) return false;
+  return c->block_size != 0 || static_cast<int64_t>(c->max_seq_len) * c->kv_token_stride * 2 <= lim;
+}
+
+static bool pool_fits(const lra_shape* sh, const lra_cache* c) {  // (prefill_pool_fits on the ABI's structs)
+  const int64_t blocks = std::max(c->num_blocks, c->max_blocks_per_seq), lim = 0x7ffff000 / 2;
+  return c->kv_block_stride <= lim / blocks && blocks * c->kv_block_stride + sh->n_kv_heads * c->kv_head_stride + 16 * c->kv_token_stride <= lim;
+}
+
+static void place_states(BatchPlan& pl, const lra_shape* sh) {
+  const size_t states = static_cast<size_t>(pl.rows) * static_cast<size_t>(pl.n_splits);
+  pl.states = true;
+  pl.off_ml = 0;
+  pl.off_o = aligned(states * 2 * sizeof(float));
+  pl.off_lr = pl.off_o + aligned(states * sh->head_dim * sizeof(float));
+  pl.off_adapter = pl.off_lr + aligned(states * sh->rank * sizeof(float));
+  pl.bytes = pl.off_adapter + aligned(static_cast<size_t>(pl.rows) * sizeof(int32_t));
+}
+
+// Chunks of many sequences, each workgroup 128 rows of one: the key tiles of a q tile are shared where there are fewer q
+// tiles than the chip has places, two per compute unit, and then so that they fill the places once; a share walks two tiles
+// at least.
+static bool plan_tiles(BatchPlan& pl, const lra_shape* sh, const lra_cache* c, const lra_batch* b) {
+  const int64_t G = sh->n_q_heads / sh->n_kv_heads;
+  const int64_t places = b->causal ? b->n_queries * G / 128 + c->n_seqs : b->n_queries;
+  if (places * sh->n_kv_heads >= (int64_t{1} << 24)) return false;  // (a grid dimension holds fewer than 2^32 threads)
+  const int64_t q_tiles = b->causal ? std::max<int64_t>((b->n_queries * G + 127) / 128, std::min(c->n_seqs, b->n_queries)) : b->n_queries;
+  const int64_t chunk = b->causal ? std::min<int64_t>(b->max_queries_per_seq, 128 / G + 1) : 1;
+  const int64_t key_tiles = (std::min<int64_t>(c->max_seq_len, keys_per_row(c, b) + chunk) + 63) / 64 + (b->window > 0 ? 2 : 0);
+  const int64_t shares = std::max<int64_t>(1, std::min<int64_t>({2 * kCUs / (q_tiles * sh->n_kv_heads), (key_tiles + 1) / 2, 64}));
+  pl.tiles = true;
+  pl.tile_places = static_cast<int>(places);
+  pl.n_splits = static_cast<int>(shares);
+  const bool far = c->block_size != 0 && !pool_fits(sh, c);
+  if (shares > 1 || far || sh->key_rope_theta > 0.f) place_states(pl, sh);
+  return true;
+}
+
 BatchPlan plan_batch(const lra_shape* sh, const lra_cache* c, const lra_batch* b, const Tuning& tune) {
   BatchPlan pl{};
   const int64_t rows = static_cast<int64_t>(b->n_queries) * sh->n_q_heads;
   const int64_t keys = keys_per_row(c, b);
+  pl.rows = static_cast<int>(rows);
+  pl.launchable = true;
+  if (sh->dtype == LRA_BF16 && sh->rank % 8 == 0 && tune.variant != 1 && mfma_fits(sh, c) && plan_tiles(pl, sh, c, b)) return pl;
   // vector-ALU kernels: one workgroup per row and share, three to a compute unit; a share of 256 keys at least, so
   // that its loop is longer than what stands around it
   int64_t share = tune.split_keys;
@@ -33,19 +80,13 @@ BatchPlan plan_batch(const lra_shape* sh, const lra_cache* c, const lra_batch* b
     share = std::max<int64_t>((keys + shares - 1) / shares, 256);
   }
   share = std::min<int64_t>((share + 63) / 64 * 64, int64_t{1} << 30);
-  pl.rows = static_cast<int>(rows);
   pl.split_keys = static_cast<int>(share);
   const int64_t splits = (keys + share - 1) / share;
   const bool rotary = sh->key_rope_theta > 0.f;
   pl.launchable = splits <= 65535 && (!rotary || rows < (int64_t{1} << 26));  // (a grid dimension holds fewer than 2^32 threads)
   if (!pl.launchable) return pl;
   pl.n_splits = static_cast<int>(splits);
-  const size_t states = static_cast<size_t>(rows) * static_cast<size_t>(splits);
-  pl.off_ml = 0;
-  pl.off_o = aligned(states * 2 * sizeof(float));
-  pl.off_lr = pl.off_o + aligned(states * sh->head_dim * sizeof(float));
-  pl.off_adapter = pl.off_lr + aligned(states * sh->rank * sizeof(float));
-  pl.bytes = pl.off_adapter + aligned(static_cast<size_t>(rows) * sizeof(int32_t));
+  place_states(pl, sh);
   return pl;
 }
 

@@ -8,8 +8,11 @@ namespace lra {
 lra_status check_batch(const lra_shape* sh, const lra_cache* c, const lra_batch* b);
 
 struct BatchPlan {
+  bool tiles;      // batch_tiles_kernel, else the vector-ALU kernels
+  int tile_places; // ... and its q tiles per kv head
+  bool states;     // the shares of a row leave states for the merge kernel
   int rows;        // n_queries x Hq
-  int split_keys;  // keys per share, of those that a row sees
+  int split_keys;  // vector-ALU kernels: keys per share, of those that a row sees
   int n_splits;
   size_t off_ml, off_o, off_lr, off_adapter, bytes;
   bool launchable;  // false: LRA_ERR_UNSUPPORTED
