@@ -91,13 +91,27 @@ BatchPlan plan_batch(const lra_shape* sh, const lra_cache* c, const lra_batch* b
 }
 
 WeightsPlan plan_key_weights(const lra_shape* sh, const lra_cache* c, const lra_batch* b, const Tuning& tune) {
-  (void)c;
-  (void)tune;
   WeightsPlan pl{};
   pl.rows = b->n_queries * sh->n_q_heads;  // (checked: at most 2^30)
+  const size_t rows = static_cast<size_t>(pl.rows);
   pl.off_qt = 0;
-  pl.off_lse = aligned(static_cast<size_t>(pl.rows) * sh->rank * sizeof(float));
-  pl.bytes = pl.off_lse + aligned(static_cast<size_t>(pl.rows) * sizeof(float));
+  const int64_t row_groups = (static_cast<int64_t>(b->max_queries_per_seq) * (sh->n_q_heads / sh->n_kv_heads) + 511) / 512;
+  if (sh->dtype == LRA_BF16 && sh->rank % 8 == 0 && c->l_adapter_stride == 0 && tune.variant != 1 && row_groups <= 65535 &&
+      b->n_queries < (1 << 23) && sh->n_kv_heads <= 4096) {
+    pl.mfma = true;
+    // statistics: workgroups of (kv head, share, sequence, 512 rows), two to a compute unit, each with a 64-key tile for
+    // every wave; at most 32 shares, which the pass over them reads
+    const int64_t units = static_cast<int64_t>(sh->n_kv_heads) * c->n_seqs * row_groups;
+    const int64_t tiles = (std::min<int64_t>(c->max_seq_len, keys_per_row(c, b) + (b->causal ? b->max_queries_per_seq : 1)) + 63) / 64 + 1;
+    pl.n_splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({2 * kCUs / units, (tiles + 3) / 4, 32})));
+    const size_t rp = sh->rank <= 16 ? 16 : (sh->rank <= 32 ? 32 : 64);
+    pl.off_lse = aligned(rows * 2 * rp * 2);
+    pl.off_stats = pl.off_lse + aligned(rows * sizeof(float));
+    pl.bytes = pl.off_stats + aligned(rows * static_cast<size_t>(pl.n_splits) * 2 * sizeof(float));
+    return pl;
+  }
+  pl.off_lse = aligned(rows * sh->rank * sizeof(float));
+  pl.bytes = pl.off_lse + aligned(rows * sizeof(float));
   return pl;
 }
 

@@ -21,8 +21,10 @@ BatchPlan plan_batch(const lra_shape* sh, const lra_cache* c, const lra_batch* b
 
 // lra_key_weights: the query rows' Q B_K^T and softmax statistics, then the sums over rows key by key.
 struct WeightsPlan {
+  bool mfma;     // else the vector-ALU kernels
+  int n_splits;  // MFMA: key shares of the statistics
   int rows;
-  size_t off_qt, off_lse, bytes;
+  size_t off_qt, off_lse, off_stats, bytes;
 };
 WeightsPlan plan_key_weights(const lra_shape* sh, const lra_cache* c, const lra_batch* b, const Tuning& tune);
 

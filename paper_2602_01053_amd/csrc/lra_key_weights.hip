@@ -1,4 +1,5 @@
-// Attention weight per cached token: lra_key_weights of the header.
+// Attention weight per cached token: entry points and vector-ALU kernels of lra_key_weights (fp32, ranks that are no multiple of
+// 8, one low-rank cache per adapter); bf16 runs on lra_key_weights_mfma.hip.
 //
 // Two passes over the keys, since a weight needs its row's maximum and sum first:
 //   Qt    = Q B_K^T of every query row                                        (once, to the workspace)
@@ -8,18 +9,11 @@
 #include "lra_batch.h"
 #include "lra_batch_plan.h"
 #include "lra_decode_util.h"
+#include "lra_key_weights.h"
 
 #include <cmath>
 
 namespace lra {
-
-struct WeightsParams : BatchParams {
-  float* qt;       // [rows][rank]
-  float* lse;      // [rows], base 2; minus infinity: the row sees nothing
-  float* weights;  // [n_seqs][weights_stride]
-  int64_t weights_stride;
-  float decay;
-};
 
 constexpr float kLog2e = 1.44269504088896340736f;
 
@@ -183,11 +177,16 @@ lra_status lra_key_weights(const lra_shape* shape, const lra_cache* cache, const
   char* ws = static_cast<char*>(workspace);
   p.qt = reinterpret_cast<float*>(ws + pl.off_qt);
   p.lse = reinterpret_cast<float*>(ws + pl.off_lse);
+  p.stats = reinterpret_cast<float*>(ws + pl.off_stats);
+  p.n_splits = pl.n_splits;
+  p.rows_per_head = batch->n_queries * p.group;
   p.weights = weights;
   p.weights_stride = weights_stride;
   p.decay = decay;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const hipError_t err = shape->dtype == LRA_BF16 ? launch_weights<bf16_t>(p, pl.rows, s) : launch_weights<float>(p, pl.rows, s);
+  const hipError_t err = pl.mfma ? launch_key_weights_mfma(p, s)
+                         : shape->dtype == LRA_BF16 ? launch_weights<bf16_t>(p, pl.rows, s)
+                                                    : launch_weights<float>(p, pl.rows, s);
   return err == hipSuccess ? LRA_OK : LRA_ERR_HIP;
 }
 
