@@ -9,7 +9,8 @@ namespace lra {
 // (fields of its own block: longer parameters would move those of the other kernels)
 struct BatchParams : Params {
   int32_t causal, window, sinks;
-  int32_t tile_places;  // batch_tiles_kernel: places of q tiles per kv head (batch_places, or the queries)
+  int32_t tile_places;     // batch_tiles_kernel: places of q tiles per kv head (batch_places, or the queries)
+  int32_t tile_per_query;  // ... whose tiles hold one query each
 };
 
 // Sequence of query `tok`: the last t with seq_query_start[t] <= tok.
@@ -43,10 +44,11 @@ __device__ __forceinline__ BatchRow batch_row(const BatchParams& p, int tok) {
   return b;
 }
 
-// The q tiles of a batch (lra_prefill_body.h): 128 rows of one sequence's chunk at most, a row being a new token of one of the
-// q heads of a kv head.  Without `causal` a tile is one query, since every query may have its own adapter.
+// The q tiles of a batch (lra_batch_tiles.h): 128 rows of one sequence's queries at most, a row being a query's token at one of
+// the q heads of a kv head; or one query, where its adapter decides what the keys or their low-rank rows are.
 struct BatchTiles {
-  int t, adapter, n_t;
+  int t, n_t;
+  int adapter;                 // of the first query: of all, where the call is causal or a tile holds one
   int first_query, n_queries;  // the queries of the chunk
   int first_pos;               // position of the first of them
   int tile;                    // of the chunk's tiles; past the last: nothing to do
@@ -60,14 +62,16 @@ __device__ __forceinline__ int batch_places(int n_queries, int group, int n_seqs
 }
 __device__ __forceinline__ BatchTiles batch_tiles(const BatchParams& p, int at, int lane) {
   BatchTiles b;
-  if (!p.causal) {
+  if (p.tile_per_query) {
     b.t = p.n_seqs > 1 ? __builtin_amdgcn_readfirstlane(sequence_of_query(p, at)) : 0;
     b.first_query = at;
     b.n_queries = 1;
     b.tile = 0;
     b.n_t = __builtin_amdgcn_readfirstlane(min(p.seq_lens[b.t], p.max_seq_len));
-    b.first_pos = b.n_t - 1;
-    b.adapter = __builtin_amdgcn_readfirstlane(min(max(p.query_adapter[at], 0), p.n_adapters - 1));
+    // (of a causal chunk it is one too, with its place in it)
+    const int first = b.t > 0 ? p.seq_query_start[b.t] : 0, end = b.t + 1 < p.n_seqs ? p.seq_query_start[b.t + 1] : p.n_queries;
+    b.first_pos = p.causal ? b.n_t - __builtin_amdgcn_readfirstlane(end - at) : b.n_t - 1;
+    b.adapter = __builtin_amdgcn_readfirstlane(min(max(p.query_adapter[p.causal ? first : at], 0), p.n_adapters - 1));
     return b;
   }
   auto first_of = [&](int t) __attribute__((always_inline)) -> int {
@@ -88,7 +92,7 @@ __device__ __forceinline__ BatchTiles batch_tiles(const BatchParams& p, int at, 
   b.n_queries = max(0, end - b.first_query);
   b.tile = at - batch_places(b.first_query, p.group, lo);
   b.n_t = __builtin_amdgcn_readfirstlane(min(p.seq_lens[lo], p.max_seq_len));
-  b.first_pos = b.n_t - b.n_queries;
+  b.first_pos = p.causal ? b.n_t - b.n_queries : b.n_t - 1;
   b.adapter = b.n_queries > 0 ? __builtin_amdgcn_readfirstlane(min(max(p.query_adapter[b.first_query], 0), p.n_adapters - 1)) : 0;
   return b;
 }
@@ -103,8 +107,8 @@ BatchParams batch_params(const lra_shape* sh, const lra_cache* c, const lra_adap
 // part_ml NULL: no states, the outputs themselves (n_splits 1)
 hipError_t launch_batch_tiles_d64(const BatchParams& p, hipStream_t s);
 hipError_t launch_batch_tiles_d128(const BatchParams& p, hipStream_t s);
+// The partial kernels' states go to the merge kernels of every other call (launch_merge), which divide by the row sum: a row that
+// sees nothing has the state m = 0, l = 1, O = 0, O_lr = 0 in its first share.
 hipError_t launch_batch_partials(const BatchParams& p, bool is_bf16, int rows, hipStream_t s);
-// States of n_splits key shares per row -> out; rows without any give zeros
-hipError_t launch_batch_merge(const BatchParams& p, bool is_bf16, int rows, hipStream_t s);
 
 }  // namespace lra

@@ -1,4 +1,4 @@
-// Attention of a batch with a window and sinks: entry points and the merge of key shares.
+// Attention of a batch with a window and sinks: entry points.
 // Declarations and argument contracts are in lra_attn.h.
 #include "lra_batch.h"
 
@@ -6,81 +6,8 @@
 
 #include "lra_attn.h"
 #include "lra_batch_plan.h"
-#include "lra_decode_util.h"
 
 namespace lra {
-
-// Merge of the key shares of a row and the epilogue of Alg. 1:
-//   M = max_s m_s, w_s = exp(m_s - M), l = sum w_s l_s, O = sum w_s O_s, O_lr = sum w_s O_lr,s ;  out = (O + O_lr B_V) / l,
-// zeros for a row that no share has a key for.  A wave per row: a lane holds the weight of one share at a time and D / 64
-// columns; rank rho of O_lr is summed by lane rho and handed round by readlane, once per row of B_V.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void batch_merge_kernel(BatchParams p, int rows) {
-  constexpr int CPL = D / 64;
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int S = p.n_splits, r = p.rank;
-  for (int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + wave; row < rows; row += static_cast<int64_t>(gridDim.x) * 4) {
-    const int h = static_cast<int>(row % p.n_q_heads) / p.group;
-    const float* ml = p.part_ml + row * S * 2;
-    float top = -INFINITY;
-    bool nan = false;
-    for (int s0 = lane; s0 < S; s0 += 64) {
-      top = fmaxf(top, ml[2 * s0]);
-      nan |= !(ml[2 * s0 + 1] == ml[2 * s0 + 1]);
-    }
-    top = wave_max(top);
-    float ell = 0.f, olr = 0.f, o[CPL];
-#pragma unroll
-    for (int k = 0; k < CPL; ++k) o[k] = 0.f;
-    for (int s0 = 0; s0 < S; s0 += 64) {
-      float w = 0.f;
-      if (s0 + lane < S) {
-        const float m = ml[2 * (s0 + lane)], l = ml[2 * (s0 + lane) + 1];
-        w = m == -INFINITY ? 0.f : expf(m - top);
-        if (w != 0.f) ell = fmaf(w, l, ell);
-      }
-      const int cnt = min(64, S - s0);
-#pragma unroll 4
-      for (int i = 0; i < cnt; ++i) {
-        const float wi = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), i));
-        const float* po = p.part_o + (row * S + s0 + i) * D + lane * CPL;
-        const float* pr = p.part_lr + (row * S + s0 + i) * r;
-        // (a share without keys leaves its O rows unwritten)
-#pragma unroll
-        for (int k = 0; k < CPL; ++k) o[k] = fmaf(wi, wi != 0.f ? po[k] : 0.f, o[k]);
-        if (lane < r) olr = fmaf(wi, wi != 0.f ? pr[lane] : 0.f, olr);
-      }
-    }
-    ell = wave_sum(ell);
-    if (__builtin_amdgcn_ballot_w64(nan) != 0) ell = NAN;
-    if (p.b_v != nullptr) {
-      const T* bv = static_cast<const T*>(p.b_v) + static_cast<int64_t>(p.part_adapter[row]) * r * p.n_kv_heads * D + h * D + lane * CPL;
-#pragma unroll 8
-      for (int rho = 0; rho < r; ++rho) {
-        const float x = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, olr), rho));
-#pragma unroll
-        for (int k = 0; k < CPL; ++k) o[k] = fmaf(x, to_f32<T>(bv[static_cast<int64_t>(rho) * p.n_kv_heads * D + k]), o[k]);
-      }
-    }
-    T* out = static_cast<T*>(p.out) + row * D + lane * CPL;
-    const bool some = top != -INFINITY || ell != 0.f;
-#pragma unroll
-    for (int k = 0; k < CPL; ++k) out[k] = from_f32<T>(some ? o[k] / ell : 0.f);
-  }
-}
-
-hipError_t launch_batch_merge(const BatchParams& p, bool is_bf16, int rows, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(rows < (1 << 22) ? (rows + 3) / 4 : 1 << 20));
-  if (p.head_dim == 128) {
-    if (is_bf16) hipLaunchKernelGGL((batch_merge_kernel<bf16_t, 128>), grid, dim3(256), 0, s, p, rows);
-    else hipLaunchKernelGGL((batch_merge_kernel<float, 128>), grid, dim3(256), 0, s, p, rows);
-  } else {
-    if (is_bf16) hipLaunchKernelGGL((batch_merge_kernel<bf16_t, 64>), grid, dim3(256), 0, s, p, rows);
-    else hipLaunchKernelGGL((batch_merge_kernel<float, 64>), grid, dim3(256), 0, s, p, rows);
-  }
-  return hipGetLastError();
-}
 
 BatchParams batch_params(const lra_shape* sh, const lra_cache* c, const lra_adapters* ad, const lra_batch* b, const void* q) {
   BatchParams p{};
@@ -162,11 +89,12 @@ lra_status lra_attn_batch(const lra_shape* shape, const lra_cache* cache, const 
   if (pl.tiles) {
     p.row_mul = (65535 + p.group) / p.group;
     p.tile_places = pl.tile_places;
+    p.tile_per_query = pl.tile_per_query;
     if ((p.head_dim == 128 ? launch_batch_tiles_d128(p, s) : launch_batch_tiles_d64(p, s)) != hipSuccess) return LRA_ERR_HIP;
   } else if (launch_batch_partials(p, bf16, pl.rows, s) != hipSuccess) {
     return LRA_ERR_HIP;
   }
-  if (pl.states && launch_batch_merge(p, bf16, pl.rows, s) != hipSuccess) return LRA_ERR_HIP;
+  if (pl.states && launch_merge(p, bf16, pl.rows, s) != hipSuccess) return LRA_ERR_HIP;
   return LRA_OK;
 }
 

@@ -37,6 +37,11 @@ static bool pool_fits(const lra_shape* sh, const lra_cache* c) {  // (prefill_po
 }
 
 static void place_states(BatchPlan& pl, const lra_shape* sh) {
+  // (the merge kernels: 128 to 1024 threads per row where there are more than 65535 queries)
+  if (pl.rows / sh->n_q_heads > 65535 && static_cast<int64_t>(pl.rows) * (pl.n_splits <= 8 ? 128 : 1024) >= (int64_t{1} << 32)) {
+    pl.launchable = false;
+    return;
+  }
   const size_t states = static_cast<size_t>(pl.rows) * static_cast<size_t>(pl.n_splits);
   pl.states = true;
   pl.off_ml = 0;
@@ -46,22 +51,26 @@ static void place_states(BatchPlan& pl, const lra_shape* sh) {
   pl.bytes = pl.off_adapter + aligned(static_cast<size_t>(pl.rows) * sizeof(int32_t));
 }
 
-// Chunks of many sequences, each workgroup 128 rows of one: the key tiles of a q tile are shared where there are fewer q
-// tiles than the chip has places, two per compute unit, and then so that they fill the places once; a share walks two tiles
-// at least.
+// A workgroup of batch_tiles_kernel takes 128 rows of one sequence; where a query's adapter decides what the keys or their
+// low-rank rows are (a rotated key side, a low-rank cache per adapter), and the queries of a sequence may have different ones,
+// one query.  The key tiles of a q tile are shared where there are fewer q tiles than the chip has places, two per compute
+// unit, and then so that they fill the places once; a share walks two tiles at least.
 static bool plan_tiles(BatchPlan& pl, const lra_shape* sh, const lra_cache* c, const lra_batch* b) {
   const int64_t G = sh->n_q_heads / sh->n_kv_heads;
-  const int64_t places = b->causal ? b->n_queries * G / 128 + c->n_seqs : b->n_queries;
+  pl.tile_per_query = !b->causal && (sh->key_rope_theta > 0.f || c->l_adapter_stride > 0);
+  const int64_t places = pl.tile_per_query ? b->n_queries : b->n_queries * G / 128 + c->n_seqs;
   if (places * sh->n_kv_heads >= (int64_t{1} << 24)) return false;  // (a grid dimension holds fewer than 2^32 threads)
-  const int64_t q_tiles = b->causal ? std::max<int64_t>((b->n_queries * G + 127) / 128, std::min(c->n_seqs, b->n_queries)) : b->n_queries;
+  const int64_t q_tiles = pl.tile_per_query ? b->n_queries : std::max<int64_t>((b->n_queries * G + 127) / 128, std::min(c->n_seqs, b->n_queries));
   const int64_t chunk = b->causal ? std::min<int64_t>(b->max_queries_per_seq, 128 / G + 1) : 1;
   const int64_t key_tiles = (std::min<int64_t>(c->max_seq_len, keys_per_row(c, b) + chunk) + 63) / 64 + (b->window > 0 ? 2 : 0);
   const int64_t shares = std::max<int64_t>(1, std::min<int64_t>({2 * kCUs / (q_tiles * sh->n_kv_heads), (key_tiles + 1) / 2, 64}));
   pl.tiles = true;
   pl.tile_places = static_cast<int>(places);
   pl.n_splits = static_cast<int>(shares);
+  // states also where the rows of a tile have adapters of their own (the merge kernel applies B_V row by row), and in the forms
+  // that are built with them only
   const bool far = c->block_size != 0 && !pool_fits(sh, c);
-  if (shares > 1 || far || sh->key_rope_theta > 0.f) place_states(pl, sh);
+  if (shares > 1 || far || sh->key_rope_theta > 0.f || (!b->causal && !pl.tile_per_query)) place_states(pl, sh);
   return true;
 }
 

@@ -9,7 +9,8 @@ lra_status check_batch(const lra_shape* sh, const lra_cache* c, const lra_batch*
 
 struct BatchPlan {
   bool tiles;      // batch_tiles_kernel, else the vector-ALU kernels
-  int tile_places; // ... and its q tiles per kv head
+  int tile_places; // ... and its q tiles per kv head,
+  bool tile_per_query;  // ... of one query each
   bool states;     // the shares of a row leave states for the merge kernel
   int rows;        // n_queries x Hq
   int split_keys;  // vector-ALU kernels: keys per share, of those that a row sees

@@ -222,7 +222,8 @@ __device__ __forceinline__ void batch_tiles_body(const BatchParams p) {
   const int t = item.t, a_idx = item.adapter, n_t = item.n_t;
   if (static_cast<int64_t>(item.tile) * BM >= n_rows) return;
   const int q0 = item.tile * BM;
-  const int base_vis = item.first_pos;  // new token i sees keys up to base_vis + i
+  const int base_vis = item.first_pos;     // query i sees keys up to base_vis + i vis_step
+  const int vis_step = p.causal ? 1 : 0;
   // First new token of the tile, how many of its q heads lie in the tile before, and the live rows of the tile.  A
   // lane's row is in_tile = 32 wave + l32 rows further: token tok0 + (head0 + in_tile) / G, the quotient (of at most
   // 143 by at most 16) taken exactly by a multiplication, so that it is cheap to form again wherever it is needed:
@@ -252,14 +253,20 @@ __device__ __forceinline__ void batch_tiles_body(const BatchParams p) {
     map_row(in_tile, tok, gq);
     return tok0 + tok;
   };
-  const int wave_first = __builtin_amdgcn_readfirstlane(base_vis + token_of(wave * 32));  // the smallest limit of this wave
-  const int wave_last = __builtin_amdgcn_readfirstlane(base_vis + token_of(wave * 32 + 31));  // and the largest
-  const int wg_last = __builtin_amdgcn_readfirstlane(base_vis + token_of(BM - 1));       // last key any row of the workgroup sees
+  auto limit_of = [&](int in_tile) __attribute__((always_inline)) -> int { return base_vis + vis_step * token_of(in_tile); };
+  const int wave_first = __builtin_amdgcn_readfirstlane(limit_of(wave * 32));  // the smallest limit of this wave
+  const int wave_last = __builtin_amdgcn_readfirstlane(limit_of(wave * 32 + 31));  // and the largest
+  const int wg_last = __builtin_amdgcn_readfirstlane(limit_of(BM - 1));       // last key any row of the workgroup sees
+  const bool live_wave = q0 + wave * 32 < n_rows;  // (a wave without rows helps with the tiles' traffic only)
+  // (for the merge kernel, which keeps it inside the table)
+  auto adapter_of = [&](int row) __attribute__((always_inline)) -> int {
+    return vis_step != 0 || p.tile_per_query ? a_idx : p.query_adapter[row / Hq];
+  };
   // Window: the first key that any row of the tile sees of its window, the sinks before it, and the key tiles between the
   // two that are passed over (tile number v of the workgroup is the sequence's tile v, or v + gap_tiles from sink_tiles on)
   int win_lo = 0, n_sinks = 0, sink_tiles = 0, gap_tiles = 0;
   if (p.window > 0) {
-    win_lo = max(0, base_vis + tok0 - p.window + 1);
+    win_lo = max(0, base_vis + vis_step * tok0 - p.window + 1);
     n_sinks = min(p.sinks, win_lo);
     sink_tiles = (n_sinks + BN - 1) / BN;
     gap_tiles = max(0, win_lo / BN - sink_tiles);
@@ -282,13 +289,20 @@ __device__ __forceinline__ void batch_tiles_body(const BatchParams p) {
   }
   if (SPLIT && tile_begin >= tile_end) {
     // more workgroups than key tiles: leave an empty state (zero row sum), all the merge
-    // kernel looks at
+    // kernel looks at; for a row that sees nothing at all the first share leaves one that gives zeros
     const int out_row = global_row(false);
-    if (out_row >= 0 && g2 == 0) {
+    if (out_row >= 0) {
       const int64_t slot = static_cast<int64_t>(out_row) * p.n_splits + split;
-      p.part_ml[slot * 2 + 0] = -INFINITY;
-      p.part_ml[slot * 2 + 1] = 0.f;
-      if (split == 0) p.part_adapter[out_row] = a_idx;
+      const bool nothing = split == 0 && limit_of(wave * 32 + l32) < 0;
+      if (g2 == 0) {
+        p.part_ml[slot * 2 + 0] = nothing ? 0.f : -INFINITY;
+        p.part_ml[slot * 2 + 1] = nothing ? 1.f : 0.f;
+        if (split == 0) p.part_adapter[out_row] = adapter_of(out_row);
+      }
+      if (nothing) {
+        for (int c = g2; c < D; c += 2) p.part_o[slot * D + c] = 0.f;
+        for (int c = g2; c < r; c += 2) p.part_lr[slot * r + c] = 0.f;
+      }
     }
     return;
   }
@@ -362,35 +376,52 @@ __device__ __forceinline__ void batch_tiles_body(const BatchParams p) {
   // As B operand of the rank k-steps of S^T, k-step ks' takes registers 8ks'..8ks'+7 of
   // block b = ks'/2, i.e. element e <-> rho = 16ks' + 8(e/4) + 4g2 + e%4; the L operand
   // below is read in the same order.
+  // Rows of several agents: one product per query of the wave's rows, kept in that query's lanes; the rows of B_K of the next
+  // are requested before those of one are used.
   pf_bf16x8 qtb[RKS];
   if (HAS_BK) {
+#pragma unroll
+    for (int ks = 0; ks < RKS; ++ks) qtb[ks] = pf_as_bf16x8(make_uint4(0u, 0u, 0u, 0u));
     const int64_t ldb = static_cast<int64_t>(Hkv) * D;
-    const bf16_t* bkg = static_cast<const bf16_t*>(p.b_k);
-    // rows of this adapter's B_K for kv head hk; rows past the rank (and everything when
-    // there is no B_K) lie outside the resource and read as zero
-    const __amdgpu_buffer_rsrc_t rs_b = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<bf16_t*>(bkg) + (bkg != nullptr ? static_cast<int64_t>(a_idx) * r * ldb + hk * D : 0), 0,
-        bkg != nullptr ? static_cast<int>((static_cast<int64_t>(r - 1) * ldb + D) * 2) : 0, 0x00020000);
+    const bf16_t* bkg = static_cast<const bf16_t*>(p.b_k) + hk * D;
+    const bool one = !SPLIT || vis_step != 0 || p.tile_per_query;  // adapter (rows of several leave states)
+    const int tok_a = __builtin_amdgcn_readfirstlane(token_of(wave * 32)), tok_b = __builtin_amdgcn_readfirstlane(token_of(wave * 32 + 31));
+    const int mine = token_of(wave * 32 + (static_cast<int>(threadIdx.x) & 31)) - tok_a;
+    const int n_it = !SPLIT ? 1 : (!live_wave ? 0 : (one ? 1 : tok_b - tok_a + 1));
+    pf_u32x4 bk[RB][KS];
+    auto request = [&](int it) __attribute__((always_inline)) {
+      const int a = one ? a_idx : min(max(__builtin_amdgcn_readfirstlane(p.query_adapter[item.first_query + tok_a + it]), 0), p.n_adapters - 1);
+      // rows of this adapter's B_K for kv head hk; rows past the rank lie outside the resource and read as zero
+      const __amdgpu_buffer_rsrc_t rs_b = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(bkg) + static_cast<int64_t>(a) * r * ldb, 0,
+                                                                            static_cast<int>((static_cast<int64_t>(r - 1) * ldb + D) * 2), 0x00020000);
 #pragma unroll
-    for (int b = 0; b < RB; ++b) {
-      pf_f32x16 acc;
+      for (int b = 0; b < RB; ++b) {
+        const int rho = b * 32 + l32;
+        const uint32_t boff = rho < r ? static_cast<uint32_t>(rho * ldb * 2 + g2 * 16) : kPfOob;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) acc[i] = 0.f;
-      const int rho = b * 32 + l32;
-      const uint32_t boff = rho < r ? static_cast<uint32_t>(rho * ldb * 2 + g2 * 16) : kPfOob;
-      pf_u32x4 bk[KS];
+        for (int ks = 0; ks < KS; ++ks) bk[b][ks] = __builtin_amdgcn_raw_buffer_load_b128(rs_b, boff, ks * 32, 0);
+      }
+    };
+    if (n_it > 0) request(0);
+#pragma unroll 1
+    for (int it = 0; it < n_it; ++it) {
+      pf_f32x16 acc[RB];
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) bk[ks] = __builtin_amdgcn_raw_buffer_load_b128(rs_b, boff, ks * 32, 0);
+      for (int b = 0; b < RB; ++b) {
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(pf_bf16x8, bk[ks]), qb[ks], acc, 0, 0, 0);
+        for (int i = 0; i < 16; ++i) acc[b][i] = 0.f;
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int ks2 = b * 2 + half;
-        if (ks2 < RKS) {
-          const int o = half * 8;
-          qtb[ks2] = pf_as_bf16x8(make_uint4(pf_pack2(acc[o + 0], acc[o + 1]), pf_pack2(acc[o + 2], acc[o + 3]),
-                                             pf_pack2(acc[o + 4], acc[o + 5]), pf_pack2(acc[o + 6], acc[o + 7])));
+        for (int ks = 0; ks < KS; ++ks)
+          acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(pf_bf16x8, bk[b][ks]), qb[ks], acc[b], 0, 0, 0);
+      }
+      if (it + 1 < n_it) request(it + 1);
+      if (one || mine == it) {
+#pragma unroll
+        for (int ks2 = 0; ks2 < RKS; ++ks2) {
+          const pf_f32x16& c = acc[ks2 >> 1];
+          const int o = (ks2 & 1) * 8;
+          qtb[ks2] = pf_as_bf16x8(make_uint4(pf_pack2(c[o + 0], c[o + 1]), pf_pack2(c[o + 2], c[o + 3]), pf_pack2(c[o + 4], c[o + 5]),
+                                             pf_pack2(c[o + 6], c[o + 7])));
         }
       }
     }
@@ -521,6 +552,12 @@ __device__ __forceinline__ void batch_tiles_body(const BatchParams p) {
       }
     }
 
+    if (SPLIT && !live_wave) {
+      pf_wait_vm0();
+      __syncthreads();
+      return;
+    }
+
     // S^T for the two 32-key halves of the tile.  The halves alternate, so consecutive
     // matrix instructions never wait for each other's result, and the LDS reads run
     // kReadAheadS operands ahead of the products that consume them.
@@ -567,7 +604,7 @@ __device__ __forceinline__ void batch_tiles_body(const BatchParams p) {
     // causal mask + online softmax.  Element (kt, i) of this lane is key
     // j + 32kt + 8(i/4) + 4g2 + i%4 of row l32.
     if (j + BN - 1 > wave_first) {  // some row of this wave does not see the whole tile
-      const int limit = base_vis + token_of(wave * 32 + (static_cast<int>(threadIdx.x) & 31));  // last visible key of this lane's row
+      const int limit = limit_of(wave * 32 + (static_cast<int>(threadIdx.x) & 31));  // last visible key of this lane's row
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -577,7 +614,7 @@ __device__ __forceinline__ void batch_tiles_body(const BatchParams p) {
         }
     }
     if (p.window > 0 && j + p.window <= wave_last && j + BN > p.sinks) {  // some row of this wave's window starts behind the first key
-      const int first = base_vis + token_of(wave * 32 + (static_cast<int>(threadIdx.x) & 31)) - p.window + 1;
+      const int first = limit_of(wave * 32 + (static_cast<int>(threadIdx.x) & 31)) - p.window + 1;
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -687,9 +724,10 @@ __device__ __forceinline__ void batch_tiles_body(const BatchParams p) {
     if (out_row >= 0) {
       const int64_t slot = static_cast<int64_t>(out_row) * p.n_splits + split;
       if (g2 == 0) {
-        p.part_ml[slot * 2 + 0] = m_run * 0.69314718055994530942f;
-        p.part_ml[slot * 2 + 1] = l_run;
-        if (split == 0) p.part_adapter[out_row] = a_idx;
+        const bool nothing = split == 0 && limit_of(wave * 32 + l32) < 0;  // (such a row's O and O_lr are zeros)
+        p.part_ml[slot * 2 + 0] = nothing ? 0.f : m_run * 0.69314718055994530942f;
+        p.part_ml[slot * 2 + 1] = nothing ? 1.f : l_run;
+        if (split == 0) p.part_adapter[out_row] = adapter_of(out_row);
       }
 #pragma unroll
       for (int b = 0; b < DB; ++b)
@@ -753,7 +791,7 @@ __device__ __forceinline__ void batch_tiles_body(const BatchParams p) {
     }
   }
   if (out_row >= 0) {
-    const float inv = l_run == 0.f ? 0.f : 1.0f / l_run;  // (a row that sees nothing: zeros)
+    const float inv = limit_of(wave * 32 + l32) < 0 ? 0.f : 1.0f / l_run;  // (a row that sees nothing: zeros)
     bf16_t* orow = static_cast<bf16_t*>(p.out) + static_cast<int64_t>(out_row) * D;
 #pragma unroll
     for (int b = 0; b < DB; ++b)

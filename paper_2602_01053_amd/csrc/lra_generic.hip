@@ -186,6 +186,18 @@ __global__ __launch_bounds__(256, 3) void generic_partial_kernel(P p) {
   const int64_t slot = static_cast<int64_t>(row) * p.n_splits + split;
   const int j0 = split * p.split_keys;
   const int j1 = min(j0 + p.split_keys, n_vis);
+  if constexpr (BATCH) {
+    if (n_vis == 0 && split == 0) {  // the row sees nothing at all: a state that the merge turns into zeros
+      if (tid < D) p.part_o[slot * D + tid] = 0.f;
+      if (tid < r) p.part_lr[slot * r + tid] = 0.f;
+      if (tid == 0) {
+        p.part_ml[slot * 2 + 0] = 0.f;
+        p.part_ml[slot * 2 + 1] = 1.f;
+        p.part_adapter[row] = a;
+      }
+      return;
+    }
+  }
   if (j0 >= j1) {  // nothing visible: (-inf, 0), rows that the merge does not read
     if (tid == 0) {
       p.part_ml[slot * 2 + 0] = -INFINITY;
@@ -539,6 +551,10 @@ __global__ __launch_bounds__(kWave) void generic_partial_rope_kernel(P p) {
   }
 
   const int64_t slot = static_cast<int64_t>(row) * p.n_splits + split;
+  if (BATCH && n_vis == 0 && split == 0) {  // (as in generic_partial_kernel)
+    m = 0.f;
+    ell = 1.f;
+  }
   if (lane == 0) {
     p.part_ml[slot * 2 + 0] = m;  // a split past the row's last visible key leaves (-inf, 0)
     p.part_ml[slot * 2 + 1] = ell;
