@@ -17,52 +17,65 @@ struct SelectParams {
 
 // Bits that order as the weights do, NaN below everything, -0 as 0; zero stands for no weight at all.
 __device__ __forceinline__ uint32_t order_bits(float w) {
-  if (w != w) return 1u;
   const uint32_t u = __float_as_uint(w + 0.f);
-  return (u >> 31) ? ~u : (u | 0x80000000u);
+  const uint32_t o = u ^ (static_cast<uint32_t>(static_cast<int32_t>(u) >> 31) | 0x80000000u);
+  return w != w ? 1u : o;
 }
 
 // One workgroup of sixteen waves per sequence.  The weights between sinks and recent tokens are cut into sixteen runs, one
 // per wave, lane l of a wave taking every 64th of its run: loads are whole lines, and the order of tokens is that of (wave,
 // step, lane).  The k-th largest is found digit by digit, eight bits at a time, from a histogram of those that agree with it
-// in all digits before; digits are counted from the highest bit in which the weights differ, since those above would put
-// every weight into one counter.  Then every wave counts what it keeps, sixteen counts are added up, and every wave writes.
-// K > 0: the lane's K weights stay in registers (K * 1024 weights at most); K == 0: read again for every digit.
+// in all digits before; of weights less the smallest, from the highest bit that the largest has, since bits that all have
+// would put every weight into one counter (weights of a long tail have few exponents, and half of them the smallest one), and
+// with four counters per digit, side by side, for the lanes that count the same one.  Once 64 weights or fewer are left, a
+// wave ranks them against each other (after two digits of 64 k weights, usually).  Then every wave counts what it keeps,
+// sixteen counts are added up, and every wave writes its own.
+// A pass over the weights is bound by the one compute unit: at 64 k weights loading takes 3 us, their range 3.5, the first
+// digit 7, the second 3, the list of the last few 3, counting 2.4 and writing 7 of 34; at 16 k all 11.7.  (First digits of raw
+// bits in sixteen counters each, one set per wave, 20 and 63 us; weights in fours, kept tokens and candidates through lists in
+// LDS: level.)
+// K > 0: the lane's K weights stay in registers (K * 1024 weights at most); K == 0: read again for every pass.
 template <int K>
 __global__ __launch_bounds__(1024) void evict_select_kernel(SelectParams p) {
-  __shared__ __align__(16) uint32_t hist[16][256];
+  __shared__ __align__(16) uint32_t hist[256][4];
   __shared__ uint32_t range_s[2][16];
-  __shared__ uint32_t pick_s[2];
+  __shared__ uint32_t pick_s[3];
+  __shared__ uint32_t few_s[64], few_n;
   __shared__ int count_s[2][16];
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int t = blockIdx.x;
   const int n = max(0, min(p.seq_lens[t], p.max_seq_len));
   int32_t* kept = p.kept + t * p.kept_stride;
   __syncthreads();  // (new_lens may be seq_lens)
   const int m = min(n, p.budget);
-  if (threadIdx.x == 0) p.new_lens[t] = m;
+  if (tid == 0) p.new_lens[t] = m;
   if (n <= p.budget) {
-    for (int i = threadIdx.x; i < n; i += 1024) kept[i] = i;
+    for (int i = tid; i < n; i += 1024) kept[i] = i;
     return;
   }
-  for (int i = threadIdx.x; i < p.sinks; i += 1024) kept[i] = i;
-  for (int i = threadIdx.x; i < p.recent; i += 1024) kept[m - p.recent + i] = n - p.recent + i;
-  int want = m - p.sinks - p.recent;  // of the weights between, fewer than there are
-  if (want == 0) return;
   const int cnt = n - p.sinks - p.recent;
+  int want = m - p.sinks - p.recent;  // of the cnt weights between, fewer than there are
   const float* w = p.weights + t * p.weights_stride + p.sinks;
   const int steps = K > 0 ? K : (cnt + 1023) / 1024;
   const int first = wave * steps * 64 + lane;
   uint32_t held[K > 0 ? K : 1];
+  uint32_t base = 0u;  // (K == 0: taken off what is read again)
   auto load = [&](int i) __attribute__((always_inline)) {
-    const uint32_t u = order_bits(w[min(first + 64 * i, cnt - 1)]);
+    const uint32_t u = order_bits(w[min(first + 64 * i, cnt - 1)]) - base;
     return first + 64 * i < cnt ? u : 0u;
   };
-  if constexpr (K > 0) {
+  if (want > 0) {
+    if constexpr (K > 0) {
 #pragma unroll
-    for (int i = 0; i < K; ++i) held[i] = load(i);
+      for (int i = 0; i < K; ++i) held[i] = load(i);
+    }
   }
+  for (int i = tid; i < p.sinks; i += 1024) kept[i] = i;
+  for (int i = tid; i < p.recent; i += 1024) kept[m - p.recent + i] = n - p.recent + i;
+  if (want == 0) return;
+  (&hist[0][0])[tid] = 0u;
+  if (tid == 0) few_n = 0u;
   // f(bits) for the lane's weights (zero past the end)
   auto each = [&](auto f) __attribute__((always_inline)) {
     if constexpr (K > 0) {
@@ -96,32 +109,35 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(SelectParams p) {
     lo = min(lo, range_s[0][i]);
     hi = max(hi, range_s[1][i]);
   }
-  lo += 1u;
-  // threshold: (u >> shift) compares with cut; `want` of those equal to it are kept
-  int shift = lo == hi ? 0 : 32 - __builtin_clz(lo ^ hi);  // bits above agree
-  uint32_t cut = shift < 32 ? hi >> shift : 0u;
-  while (shift > 0) {
+  // From here on weights are counted from below the smallest: 1 for that one, still 0 for what stands past the end.
+  const uint32_t range = hi - lo;  // (lo is one less than the smallest)
+  if constexpr (K > 0) {
+#pragma unroll
+    for (int i = 0; i < K; ++i) held[i] = held[i] == 0u ? 0u : held[i] - lo;
+  }
+  base = lo;
+  // The threshold: weights with (u >> shift) > cut stay, and `want` of the `left` weights with (u >> shift) == cut.
+  // (Zeros agree with a cut of zero only, and are then counted among the smallest: never wanted.)
+  int shift = range == 1u ? 0 : 32 - __builtin_clz(range), left = cnt;
+  uint32_t cut = range == 1u ? 1u : 0u;
+  auto agrees = [&](uint32_t u) __attribute__((always_inline)) -> bool { return ((u >> (shift - 1)) >> 1) == cut; };  // (shift: 1 to 32)
+  while (shift > 0 && left > 64) {
     const int width = min(8, shift);
     const int below = shift - width;
-    for (int i = threadIdx.x; i < 16 * 256; i += 1024) (&hist[0][0])[i] = 0u;
-    __syncthreads();
+    const uint32_t mask = (1u << width) - 1u;
     each([&](uint32_t u) __attribute__((always_inline)) {
-      if (u != 0u && (shift == 32 || (u >> shift) == cut)) atomicAdd(&hist[wave][(u >> below) & ((1u << width) - 1u)], 1u);
+      if (agrees(u)) atomicAdd(&hist[(u >> below) & mask][lane & 3], 1u);
     });
     __syncthreads();
     if (wave == 0) {
-      // lane l: the four counters 255 - 4 l .. 252 - 4 l, so that a prefix over the lanes runs from the largest digit
-      uint32_t c[4] = {0u, 0u, 0u, 0u};
-#pragma unroll 1
-      for (int v = 0; v < 16; v += 4) {  // (all sixteen at once want more registers than the weights leave)
+      // lane l: digits 255 - 4 l .. 252 - 4 l, so that a sum over the lanes before runs from the largest digit
+      uint32_t c[4];
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const uint4 four = *reinterpret_cast<const uint4*>(&hist[v + x][252 - 4 * lane]);
-          c[0] += four.w;
-          c[1] += four.z;
-          c[2] += four.y;
-          c[3] += four.x;
-        }
+      for (int k = 0; k < 4; ++k) {
+        uint4* at = reinterpret_cast<uint4*>(&hist[255 - 4 * lane - k][0]);
+        const uint4 four = *at;
+        c[k] = (four.x + four.y) + (four.z + four.w);
+        *at = make_uint4(0u, 0u, 0u, 0u);  // (for the next digit)
       }
       const uint32_t sum = (c[0] + c[1]) + (c[2] + c[3]);
       uint32_t before = sum;
@@ -136,17 +152,41 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(SelectParams p) {
         if (before < static_cast<uint32_t>(want) && static_cast<uint32_t>(want) <= before + c[k]) {
           pick_s[0] = static_cast<uint32_t>(255 - 4 * lane - k);
           pick_s[1] = static_cast<uint32_t>(want) - before;
+          pick_s[2] = c[k];
         }
         before += c[k];
       }
     }
-    __syncthreads();
+    __syncthreads();  // (pick_s is written next behind the barrier of the next digit)
     cut = (shift == 32 ? 0u : cut << width) | pick_s[0];
     want = static_cast<int>(pick_s[1]);
+    left = static_cast<int>(pick_s[2]);
     shift = below;
-    __syncthreads();  // (pick_s and the counters are written again)
   }
-  // u > cut stays, and the first `want` with u == cut
+  if (shift > 0) {
+    // 64 weights or fewer: in any order to LDS, where every lane of every wave counts those above its own
+    each([&](uint32_t u) __attribute__((always_inline)) {
+      if (u != 0u && agrees(u)) few_s[atomicAdd(&few_n, 1u)] = u;
+    });
+    __syncthreads();
+    left = static_cast<int>(few_n);
+    const uint32_t mine = lane < left ? few_s[lane] : 0u;
+    int above = 0, equal = 0;
+    for (int i = 0; i < left; ++i) {
+      const uint32_t o = few_s[i];
+      above += o > mine;
+      equal += o == mine;
+    }
+    const uint64_t is = __builtin_amdgcn_ballot_w64(lane < left && above < want && want <= above + equal);
+    const int who = __builtin_ctzll(is);
+    cut = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(mine), who));
+    want -= __builtin_amdgcn_readlane(above, who);
+    left = __builtin_amdgcn_readlane(equal, who);
+  }
+  // u > cut stays, and the first `want` of the `left` with u == cut
+  cut = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(cut)));
+  want = __builtin_amdgcn_readfirstlane(want);
+  left = __builtin_amdgcn_readfirstlane(left);
   int above = 0, equal = 0;
   each([&](uint32_t u) __attribute__((always_inline)) {
     above += u > cut;
@@ -164,18 +204,30 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(SelectParams p) {
   __syncthreads();
   int eq_before = 0, at = p.sinks;
   for (int v = 0; v < wave; ++v) {
-    at += count_s[0][v];
-    eq_before += count_s[1][v];
+    at += __builtin_amdgcn_readfirstlane(count_s[0][v]);
+    eq_before += __builtin_amdgcn_readfirstlane(count_s[1][v]);
   }
   at += min(eq_before, want);
-  const uint64_t below_me = (uint64_t{1} << lane) - 1;
+  asm volatile("" : "+s"(cut));  // (or the 2 K comparisons of the counts are kept, in scalar registers that there are not)
+  const bool all_equal_stay = want >= left;
+  // (K > 0, at most 64 k weights: lanes that keep nothing store outside the resource, without a branch a step)
+  const __amdgpu_buffer_rsrc_t rs = make_rsrc(kept + p.sinks, K > 0 ? static_cast<uint32_t>(m - p.sinks - p.recent) * 4u : 0u);
+  auto below_me = [&](uint64_t mask) __attribute__((always_inline)) -> int {
+    return __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(mask >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(mask), 0u));
+  };
   auto emit = [&](int i, uint32_t u) __attribute__((always_inline)) {  // (cut is a weight's, not zero)
-    const uint64_t eq = __builtin_amdgcn_ballot_w64(u == cut);
-    const bool stay = u > cut || (u == cut && eq_before + __builtin_popcountll(eq & below_me) < want);
+    bool stay = u >= cut;
+    if (!all_equal_stay) {
+      const uint64_t eq = __builtin_amdgcn_ballot_w64(u == cut);
+      stay = u > cut || (u == cut && eq_before + below_me(eq) < want);
+      eq_before += __builtin_popcountll(eq);
+    }
     const uint64_t all = __builtin_amdgcn_ballot_w64(stay);
-    if (stay) kept[at + __builtin_popcountll(all & below_me)] = p.sinks + first + 64 * i;
+    if constexpr (K > 0)
+      __builtin_amdgcn_raw_buffer_store_b32(p.sinks + first + 64 * i, rs, stay ? (at - p.sinks + below_me(all)) * 4 : static_cast<int>(kOob), 0, 0);
+    else if (stay)
+      kept[at + below_me(all)] = p.sinks + first + 64 * i;
     at += __builtin_popcountll(all);
-    eq_before += __builtin_popcountll(eq);
   };
   if constexpr (K > 0) {
 #pragma unroll
