@@ -21,14 +21,14 @@ static int64_t keys_per_row(const lra_cache* c, const lra_batch* b) {
   return b->window > 0 ? std::min<int64_t>(c->max_seq_len, static_cast<int64_t>(b->window) + b->sinks) : c->max_seq_len;
 }
 
-// Whether the MFMA kernels can address the caches: a contiguous kv head's rows, and the low-rank rows of one adapter, by
+// Whether the MFMA kernels can address the caches: a contiguous kv head's rows (or a block's), and the low-rank rows of one adapter, by
 // 32-bit byte offsets inside one buffer resource, below the offset that stands for "outside" (2^31).
 static bool mfma_fits(const lra_shape* sh, const lra_cache* c) {
   const int64_t lim = (int64_t{1} << 31) - 4096;
   const int64_t pitch = c->l_row_stride ? c->l_row_stride : sh->rank;
   const int64_t l_rows = c->block_size == 0 ? c->max_seq_len : static_cast<int64_t>(c->num_blocks) * 16;
   if (pitch > lim / 2 / l_rows) return false;
-  return c->block_size != 0 || static_cast<int64_t>(c->max_seq_len) * c->kv_token_stride * 2 <= lim;
+  return (c->block_size != 0 ? 16 : static_cast<int64_t>(c->max_seq_len)) * c->kv_token_stride * 2 <= lim;
 }
 
 static bool pool_fits(const lra_shape* sh, const lra_cache* c) {  // (prefill_pool_fits on the ABI's structs)
@@ -104,15 +104,18 @@ WeightsPlan plan_key_weights(const lra_shape* sh, const lra_cache* c, const lra_
   pl.rows = b->n_queries * sh->n_q_heads;  // (checked: at most 2^30)
   const size_t rows = static_cast<size_t>(pl.rows);
   pl.off_qt = 0;
-  const int64_t row_groups = (static_cast<int64_t>(b->max_queries_per_seq) * (sh->n_q_heads / sh->n_kv_heads) + 511) / 512;
-  if (sh->dtype == LRA_BF16 && sh->rank % 8 == 0 && c->l_adapter_stride == 0 && tune.variant != 1 && row_groups <= 65535 &&
-      b->n_queries < (1 << 23) && sh->n_kv_heads <= 4096) {
+  const int64_t G = sh->n_q_heads / sh->n_kv_heads;
+  const int64_t places = b->n_queries * G / 128 + c->n_seqs;
+  // statistics: workgroups of (kv head, 128 rows, share), three to a compute unit, each with two 64-key tiles at least; at most
+  // 32 shares, which the pass over them reads
+  const int64_t q_tiles = std::max<int64_t>((b->n_queries * G + 127) / 128, std::min(c->n_seqs, b->n_queries));
+  const int64_t tiles = (std::min<int64_t>(c->max_seq_len, keys_per_row(c, b) + (b->causal ? std::min<int64_t>(b->max_queries_per_seq, 128 / G + 1) : 1)) + 63) / 64 + 1;
+  const int64_t shares = std::max<int64_t>(1, std::min<int64_t>({3 * kCUs / (q_tiles * sh->n_kv_heads), (tiles + 1) / 2, 32}));
+  if (sh->dtype == LRA_BF16 && sh->rank % 8 == 0 && c->l_adapter_stride == 0 && tune.variant != 1 && mfma_fits(sh, c) &&
+      places * shares * sh->n_kv_heads < (int64_t{1} << 24)) {
     pl.mfma = true;
-    // statistics: workgroups of (kv head, share, sequence, 512 rows), two to a compute unit, each with a 64-key tile for
-    // every wave; at most 32 shares, which the pass over them reads
-    const int64_t units = static_cast<int64_t>(sh->n_kv_heads) * c->n_seqs * row_groups;
-    const int64_t tiles = (std::min<int64_t>(c->max_seq_len, keys_per_row(c, b) + (b->causal ? b->max_queries_per_seq : 1)) + 63) / 64 + 1;
-    pl.n_splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({2 * kCUs / units, (tiles + 3) / 4, 32})));
+    pl.n_splits = static_cast<int>(shares);
+    pl.tile_places = static_cast<int>(places);
     const size_t rp = sh->rank <= 16 ? 16 : (sh->rank <= 32 ? 32 : 64);
     pl.off_lse = aligned(rows * 2 * rp * 2);
     pl.off_stats = pl.off_lse + aligned(rows * sizeof(float));

@@ -24,6 +24,7 @@ BatchPlan plan_batch(const lra_shape* sh, const lra_cache* c, const lra_batch* b
 struct WeightsPlan {
   bool mfma;     // else the vector-ALU kernels
   int n_splits;  // MFMA: key shares of the statistics
+  int tile_places;  // ... and places of 128 rows per kv head
   int rows;
   size_t off_qt, off_lse, off_stats, bytes;
 };

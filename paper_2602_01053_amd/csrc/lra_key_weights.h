@@ -16,10 +16,9 @@ struct WeightsParams : BatchParams {
   int64_t weights_stride;
   float decay;
   int32_t rows_per_head;  // n_queries x group
+  int32_t sum_tiles;      // weights_sum_rows_kernel: tiles of 32 keys per workgroup
 };
 
 hipError_t launch_key_weights_mfma(const WeightsParams& p, hipStream_t s);
-
-constexpr int kWeightRows = 512;  // rows of a (sequence, kv head) that a workgroup of the statistics kernel takes
 
 }  // namespace lra

@@ -180,6 +180,8 @@ lra_status lra_key_weights(const lra_shape* shape, const lra_cache* cache, const
   p.stats = reinterpret_cast<float*>(ws + pl.off_stats);
   p.n_splits = pl.n_splits;
   p.rows_per_head = batch->n_queries * p.group;
+  p.row_mul = (65535 + p.group) / p.group;
+  p.tile_places = pl.tile_places;
   p.weights = weights;
   p.weights_stride = weights_stride;
   p.decay = decay;
