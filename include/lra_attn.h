@@ -437,7 +437,8 @@ typedef struct {
  *   q    DEVICE [n_queries][Hq][d]        out  DEVICE [n_queries][Hq][d]
  *   workspace  DEVICE, 256-byte aligned, >= lra_batch_workspace_bytes(...) bytes; contents undefined afterwards;
  *              calls that overlap in time, captured graphs among them, need separate ones
- *   tuning     kernel_variant (1: vector-ALU kernels), decode_split_keys (keys per workgroup)
+ *   tuning     kernel_variant (1: vector-ALU kernels, 2: no kernel of its own for few query rows), decode_split_keys
+ *              (vector-ALU kernels: keys per workgroup)
  */
 lra_status lra_attn_batch(const lra_shape* shape, const lra_cache* cache, const lra_adapters* adapters,
                           const lra_batch* batch, const void* q, void* out, void* workspace, size_t workspace_bytes,
@@ -462,7 +463,7 @@ size_t lra_batch_workspace_bytes(const lra_shape* shape, const lra_cache* cache,
  *              caches are formed from q B_K^T in 16 bits of mantissa, so that small sums keep their order.
  *   workspace  DEVICE, 256-byte aligned, >= lra_key_weights_workspace_bytes(...), as for lra_attn_batch
  * A rotated key-side adapter (key_rope_theta > 0 with a b_k) is LRA_ERR_UNSUPPORTED: its keys depend on the token's
- * index, which an eviction changes.
+ * index, which an eviction changes.  So are more than 65535 sequences.
  */
 lra_status lra_key_weights(const lra_shape* shape, const lra_cache* cache, const lra_adapters* adapters,
                            const lra_batch* batch, const void* q, float decay, float* weights, int64_t weights_stride,
@@ -498,7 +499,7 @@ lra_status lra_evict_select(const lra_cache* cache, const float* weights, int64_
  *   n_adapters   low-rank caches to move, >= 1; more than one only where both caches have an l_adapter_stride
  *   kept         DEVICE int32 [n_seqs][kept_stride], kept_stride >= dst->max_seq_len; entries in [0, src length)
  *   weights, dst_weights   DEVICE float [n_seqs][...] or both NULL; strides >= the max_seq_len of src and dst
- * key_rope_theta > 0 is LRA_ERR_UNSUPPORTED: K_base may hold rotated keys (they keep the angles of their first
+ * More than 65535 sequences are LRA_ERR_UNSUPPORTED, and so is key_rope_theta > 0: K_base may hold rotated keys (they keep the angles of their first
  * positions), but an adapter's part that is rotated by the token's index would turn with the move.
  */
 lra_status lra_cache_gather(const lra_shape* shape, const lra_cache* src, int32_t n_adapters, const int32_t* kept,

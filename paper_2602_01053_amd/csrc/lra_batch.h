@@ -107,6 +107,7 @@ BatchParams batch_params(const lra_shape* sh, const lra_cache* c, const lra_adap
 // part_ml NULL: no states, the outputs themselves (n_splits 1)
 hipError_t launch_batch_tiles_d64(const BatchParams& p, hipStream_t s);
 hipError_t launch_batch_tiles_d128(const BatchParams& p, hipStream_t s);
+hipError_t launch_batch_rows(const BatchParams& p, hipStream_t s);
 // The partial kernels' states go to the merge kernels of every other call (launch_merge), which divide by the row sum: a row that
 // sees nothing has the state m = 0, l = 1, O = 0, O_lr = 0 in its first share.
 hipError_t launch_batch_partials(const BatchParams& p, bool is_bf16, int rows, hipStream_t s);

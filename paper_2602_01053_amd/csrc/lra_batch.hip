@@ -86,7 +86,9 @@ lra_status lra_attn_batch(const lra_shape* shape, const lra_cache* cache, const 
   }
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bool bf16 = shape->dtype == LRA_BF16;
-  if (pl.tiles) {
+  if (pl.few_rows) {
+    if (launch_batch_rows(p, s) != hipSuccess) return LRA_ERR_HIP;
+  } else if (pl.tiles) {
     p.row_mul = (65535 + p.group) / p.group;
     p.tile_places = pl.tile_places;
     p.tile_per_query = pl.tile_per_query;

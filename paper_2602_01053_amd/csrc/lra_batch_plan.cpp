@@ -74,13 +74,31 @@ static bool plan_tiles(BatchPlan& pl, const lra_shape* sh, const lra_cache* c, c
   return true;
 }
 
+// 32 rows at most per sequence and kv head, with one low-rank cache: workgroups of (kv head, key share, sequence), two to a compute
+// unit, whose waves have a tile of 32 keys each at least.
+static bool plan_few_rows(BatchPlan& pl, const lra_shape* sh, const lra_cache* c, const lra_batch* b) {
+  const int64_t G = sh->n_q_heads / sh->n_kv_heads;
+  if (b->max_queries_per_seq * G > 32 || sh->key_rope_theta > 0.f || c->n_seqs > 65535) return false;
+  if (c->l_adapter_stride > 0 && !b->causal) return false;  // (the rows of a sequence share their low-rank rows)
+  const int64_t units = static_cast<int64_t>(sh->n_kv_heads) * std::min(c->n_seqs, b->n_queries);
+  const int64_t chunk = b->causal ? b->max_queries_per_seq : 1;
+  const int64_t key_tiles = (std::min<int64_t>(c->max_seq_len, keys_per_row(c, b) + chunk) + 31) / 32 + (b->window > 0 ? 2 : 0);
+  pl.few_rows = true;
+  pl.n_splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({2 * kCUs / units, (key_tiles + 3) / 4, 64})));
+  place_states(pl, sh);
+  return true;
+}
+
 BatchPlan plan_batch(const lra_shape* sh, const lra_cache* c, const lra_batch* b, const Tuning& tune) {
   BatchPlan pl{};
   const int64_t rows = static_cast<int64_t>(b->n_queries) * sh->n_q_heads;
   const int64_t keys = keys_per_row(c, b);
   pl.rows = static_cast<int>(rows);
   pl.launchable = true;
-  if (sh->dtype == LRA_BF16 && sh->rank % 8 == 0 && tune.variant != 1 && mfma_fits(sh, c) && plan_tiles(pl, sh, c, b)) return pl;
+  if (sh->dtype == LRA_BF16 && sh->rank % 8 == 0 && tune.variant != 1 && mfma_fits(sh, c)) {
+    if (tune.variant == 0 && plan_few_rows(pl, sh, c, b)) return pl;
+    if (plan_tiles(pl, sh, c, b)) return pl;
+  }
   // vector-ALU kernels: one workgroup per row and share, three to a compute unit; a share of 256 keys at least, so
   // that its loop is longer than what stands around it
   int64_t share = tune.split_keys;
@@ -122,8 +140,10 @@ WeightsPlan plan_key_weights(const lra_shape* sh, const lra_cache* c, const lra_
     pl.bytes = pl.off_stats + aligned(rows * static_cast<size_t>(pl.n_splits) * 2 * sizeof(float));
     return pl;
   }
-  pl.off_lse = aligned(rows * sh->rank * sizeof(float));
-  pl.bytes = pl.off_lse + aligned(rows * sizeof(float));
+  // vector-ALU kernels: three workgroups to a compute unit, a share of 128 keys at least
+  pl.n_splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({3 * kCUs / static_cast<int64_t>(rows), (keys_per_row(c, b) + 127) / 128, 32})));
+  pl.off_lse = pl.off_stats = aligned(rows * sh->rank * sizeof(float));
+  pl.bytes = pl.off_stats + aligned(rows * static_cast<size_t>(pl.n_splits) * 2 * sizeof(float));
   return pl;
 }
 

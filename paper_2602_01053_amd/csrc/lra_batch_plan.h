@@ -8,7 +8,8 @@ namespace lra {
 lra_status check_batch(const lra_shape* sh, const lra_cache* c, const lra_batch* b);
 
 struct BatchPlan {
-  bool tiles;      // batch_tiles_kernel, else the vector-ALU kernels
+  bool few_rows;   // batch_rows_kernel
+  bool tiles;      // batch_tiles_kernel; neither: the vector-ALU kernels
   int tile_places; // ... and its q tiles per kv head,
   bool tile_per_query;  // ... of one query each
   bool states;     // the shares of a row leave states for the merge kernel
@@ -23,8 +24,8 @@ BatchPlan plan_batch(const lra_shape* sh, const lra_cache* c, const lra_batch* b
 // lra_key_weights: the query rows' Q B_K^T and softmax statistics, then the sums over rows key by key.
 struct WeightsPlan {
   bool mfma;     // else the vector-ALU kernels
-  int n_splits;  // MFMA: key shares of the statistics
-  int tile_places;  // ... and places of 128 rows per kv head
+  int n_splits;  // key shares of the statistics
+  int tile_places;  // MFMA: places of 128 rows per kv head
   int rows;
   size_t off_qt, off_lse, off_stats, bytes;
 };

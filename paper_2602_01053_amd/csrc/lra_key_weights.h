@@ -6,12 +6,12 @@
 namespace lra {
 
 struct WeightsParams : BatchParams {
-  // vector-ALU kernels: Qt [rows][rank], lse [rows], row = query Hq + q head.  MFMA kernels: Qt as bf16 (below), lse
-  // [Hkv][row], row = query group + q head of the group.  lse: base-2 logarithm of the row's sum, +inf (MFMA) or -inf where it
-  // sees nothing.
+  // vector-ALU kernels: Qt [rows][rank], statistics [rows][shares][2], row = query Hq + q head.  MFMA kernels: Qt as bf16
+  // (weights_stats_mfma_kernel), statistics [Hkv][shares][row][2] and lse [Hkv][row], row = query group + q head of the group; lse
+  // the base-2 logarithm of the row's sum, +inf where it sees nothing.  Statistics: maximum and sum of a share's scores, base 2.
   float* qt;
   float* lse;
-  float* stats;    // MFMA: [Hkv][shares][row][2], maximum and sum of a key share's scores, base 2
+  float* stats;
   float* weights;  // [n_seqs][weights_stride]
   int64_t weights_stride;
   float decay;

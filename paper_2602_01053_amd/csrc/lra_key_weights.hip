@@ -18,65 +18,81 @@ namespace lra {
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // Row idx of the batch: query idx / Hq, q head idx % Hq.
-template <typename T>
-__global__ __launch_bounds__(256) void weights_qt_kernel(WeightsParams p, int64_t n) {
-  const int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;  // (row, rank)
-  if (at >= n) return;
-  const int64_t row = at / p.rank;
-  const int rho = static_cast<int>(at - row * p.rank), d = p.head_dim;
-  const int tok = static_cast<int>(row / p.n_q_heads), h = static_cast<int>(row % p.n_q_heads) / p.group;
-  const int a = batch_row(p, tok).adapter;
-  const T* q = static_cast<const T*>(p.q) + row * d;
-  const T* b = static_cast<const T*>(p.b_k) + ((static_cast<int64_t>(a) * p.rank + rho) * p.n_kv_heads + h) * d;
+
+// A row's Q . K of token j, the K row in 16-byte pieces, sixteen requested before the first is used
+template <typename T, int D>
+__device__ __forceinline__ float dot_key(const WeightsParams& p, int t, int j, int h, const float* q) {
+  constexpr int E = 16 / static_cast<int>(sizeof(T)), N = D / E, U = N < 16 ? N : 16;
+  const u32x4* k = reinterpret_cast<const u32x4*>(static_cast<const T*>(p.k_base) + kv_offset(p, t, j, h));
   float acc = 0.f;
-  for (int c = 0; c < d; ++c) acc = fmaf(to_f32<T>(q[c]), to_f32<T>(b[c]), acc);
-  p.qt[at] = acc;
+#pragma unroll
+  for (int c0 = 0; c0 < N; c0 += U) {
+    u32x4 v[U];
+#pragma unroll
+    for (int c = 0; c < U; ++c) v[c] = k[c0 + c];
+#pragma unroll
+    for (int c = 0; c < U; ++c)
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        float x;
+        if constexpr (sizeof(T) == 4) x = __uint_as_float(v[c][e]);
+        else x = __uint_as_float((e & 1) ? (v[c][e >> 1] & 0xffff0000u) : (v[c][e >> 1] << 16));
+        acc = fmaf(x, q[(c0 + c) * E + e], acc);
+      }
+  }
+  return acc;
 }
 
-// scale log2(e) times the score of a row (q in LDS, Qt) and a key
-template <typename T>
+// scale log2(e) times the score of a row (q and Qt in LDS) and a key; the low-rank row eight elements at a time, past its end the
+// last one again against zeros of Qt
+template <typename T, int D>
 __device__ __forceinline__ float score(const WeightsParams& p, int t, int j, int h, int a, const float* q, const float* qt) {
-  const T* k = static_cast<const T*>(p.k_base) + kv_offset(p, t, j, h);
-  constexpr int PER = 16 / static_cast<int>(sizeof(T));
-  float acc = 0.f;
-  for (int c = 0; c < p.head_dim; c += PER) {
-    const uint4 piece = *reinterpret_cast<const uint4*>(k + c);
-    const uint32_t w[4] = {piece.x, piece.y, piece.z, piece.w};
-#pragma unroll
-    for (int e = 0; e < PER; ++e) {
-      float x;
-      if constexpr (sizeof(T) == 4) x = __uint_as_float(w[e]);
-      else x = __uint_as_float((e & 1) ? (w[e >> 1] & 0xffff0000u) : (w[e >> 1] << 16));
-      acc = fmaf(x, q[c + e], acc);
-    }
-  }
+  float low = 0.f;
   if (p.b_k != nullptr) {
     const T* l = static_cast<const T*>(p.l) + l_offset(p, t, j, a);
-    for (int rho = 0; rho < p.rank; ++rho) acc = fmaf(to_f32<T>(l[rho]), qt[rho], acc);
+    for (int r0 = 0; r0 < p.rank; r0 += 8) {
+      T v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = l[min(r0 + e, p.rank - 1)];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) low = fmaf(to_f32<T>(v[e]), qt[r0 + e], low);
+    }
   }
-  return acc * (p.scale * kLog2e);
+  return (dot_key<T, D>(p, t, j, h, q) + low) * (p.scale * kLog2e);
 }
 
-template <typename T>
-__device__ __forceinline__ void stage_row(const WeightsParams& p, int64_t row, float* q, float* qt, int first, int step) {
-  for (int c = first; c < p.head_dim; c += step) q[c] = to_f32<T>(static_cast<const T*>(p.q)[row * p.head_dim + c]);
-  if (p.b_k != nullptr)
-    for (int c = first; c < p.rank; c += step) qt[c] = p.qt[row * p.rank + c];
-}
-
-// One workgroup per row; a lane takes every 256th key.
-template <typename T>
+// One workgroup per row and key share; a lane takes every 256th key.  Qt of the row is formed here, four lanes to a rank, and left
+// for the sums.
+template <typename T, int D>
 __global__ __launch_bounds__(256) void weights_stats_kernel(WeightsParams p, int64_t rows) {
-  __shared__ float q[128], qt[64], m_s[4], l_s[4];
+  __shared__ float q[D], qt[64], m_s[4], l_s[4];
+  const int tid = threadIdx.x, split = blockIdx.y;
   for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
     const int tok = static_cast<int>(row / p.n_q_heads), h = static_cast<int>(row % p.n_q_heads) / p.group;
     const BatchRow b = batch_row(p, tok);
     __syncthreads();
-    stage_row<T>(p, row, q, qt, threadIdx.x, 256);
+    if (tid < D) q[tid] = to_f32<T>(static_cast<const T*>(p.q)[row * D + tid]);
+    __syncthreads();
+    {
+      const int rho = tid >> 2, part = tid & 3;
+      float acc = 0.f;
+      if (p.b_k != nullptr && rho < p.rank) {
+        const T* bk = static_cast<const T*>(p.b_k) + ((static_cast<int64_t>(b.adapter) * p.rank + rho) * p.n_kv_heads + h) * D;
+#pragma unroll 16
+        for (int c = 0; c < D / 4; ++c) acc = fmaf(q[4 * c + part], to_f32<T>(bk[4 * c + part]), acc);
+      }
+      acc += __shfl_xor(acc, 1, kWave);
+      acc += __shfl_xor(acc, 2, kWave);
+      if (part == 0) {
+        qt[rho] = acc;
+        if (p.b_k != nullptr && rho < p.rank && split == 0) p.qt[row * p.rank + rho] = acc;
+      }
+    }
     __syncthreads();
     float m = -INFINITY, l = 0.f;
-    for (int k = threadIdx.x; k < b.n_keys; k += 256) {
-      const float s = score<T>(p, b.t, k < b.n_sinks ? k : k + b.gap, h, b.adapter, q, qt);
+    const int k1 = static_cast<int>(static_cast<int64_t>(b.n_keys) * (split + 1) / p.n_splits);
+    for (int k = static_cast<int>(static_cast<int64_t>(b.n_keys) * split / p.n_splits) + tid; k < k1; k += 256) {
+      const float s = score<T, D>(p, b.t, k < b.n_sinks ? k : k + b.gap, h, b.adapter, q, qt);
       if (s == -INFINITY) continue;
       const float m_new = fmaxf(m, s);
       l = l * exp2f(m - m_new) + exp2f(s - m_new);
@@ -84,25 +100,25 @@ __global__ __launch_bounds__(256) void weights_stats_kernel(WeightsParams p, int
     }
     const float top_w = wave_max(m);
     const float sum_w = wave_sum(m == -INFINITY ? l : l * exp2f(m - top_w));
-    const int wave = threadIdx.x >> 6;
-    if ((threadIdx.x & 63) == 0) {
+    const int wave = tid >> 6;
+    if ((tid & 63) == 0) {
       m_s[wave] = top_w;
       l_s[wave] = sum_w;
     }
     __syncthreads();
-    if (threadIdx.x == 0) {
+    if (tid == 0) {
       const float top = fmaxf(fmaxf(m_s[0], m_s[1]), fmaxf(m_s[2], m_s[3]));
       float sum = 0.f;
       for (int w = 0; w < 4; ++w) sum += m_s[w] == -INFINITY ? l_s[w] : l_s[w] * exp2f(m_s[w] - top);
-      p.lse[row] = sum == 0.f ? -INFINITY : top + log2f(sum);
+      reinterpret_cast<float2*>(p.stats)[row * p.n_splits + split] = make_float2(top, sum);
     }
   }
 }
 
-// One workgroup per (64 keys, sequence); a wave takes every fourth row of the sequence, a lane one key.
-template <typename T>
-__global__ __launch_bounds__(256) void weights_sum_kernel(WeightsParams p) {
-  __shared__ float q[4][128], qt[4][64], sum_s[4][64];
+// One workgroup per (64 keys, sequence); a wave takes every sixteenth row of the sequence, a lane one key.
+template <typename T, int D>
+__global__ __launch_bounds__(1024) void weights_sum_kernel(WeightsParams p) {
+  __shared__ float q[16][D], qt[16][64], sum_s[16][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int t = blockIdx.y;
   const int j = blockIdx.x * 64 + lane;
@@ -110,35 +126,43 @@ __global__ __launch_bounds__(256) void weights_sum_kernel(WeightsParams p) {
   if (static_cast<int>(blockIdx.x) * 64 >= n_t) return;
   const int c0 = t > 0 ? p.seq_query_start[t] : 0, c1 = t + 1 < p.n_seqs ? p.seq_query_start[t + 1] : p.n_queries;
   float sum = 0.f;
-  for (int64_t row = static_cast<int64_t>(c0) * p.n_q_heads + wave; row < static_cast<int64_t>(c1) * p.n_q_heads; row += 4) {
+  for (int64_t row = static_cast<int64_t>(c0) * p.n_q_heads + wave; row < static_cast<int64_t>(c1) * p.n_q_heads; row += 16) {
     const int tok = static_cast<int>(row / p.n_q_heads), h = static_cast<int>(row % p.n_q_heads) / p.group;
-    const float lse = p.lse[row];
-    if (lse == -INFINITY) continue;
-    stage_row<T>(p, row, q[wave], qt[wave], lane, 64);
+    // the shares' statistics joined, a lane each (32 at most)
+    const float2 ml = lane < p.n_splits ? reinterpret_cast<const float2*>(p.stats)[row * p.n_splits + lane] : make_float2(-INFINITY, 0.f);
+    const float top = wave_max(ml.x);
+    const float all = wave_sum(ml.x == -INFINITY ? ml.y : ml.y * exp2f(ml.x - top));  // (a share's NaN is the row's)
+    if (all == 0.f) continue;  // the row sees nothing
+    const float lse = top + log2f(all);
+    for (int c = lane; c < D; c += 64) q[wave][c] = to_f32<T>(static_cast<const T*>(p.q)[row * D + c]);
+    qt[wave][lane] = p.b_k != nullptr && lane < p.rank ? p.qt[row * p.rank + lane] : 0.f;
     lds_fence();
     const int pos = p.causal ? n_t - (c1 - tok) : n_t - 1;
     const int a = min(max(p.query_adapter[p.causal ? c0 : tok], 0), p.n_adapters - 1);
-    if (j < n_t && batch_sees(p, pos, j)) sum += exp2f(score<T>(p, t, j, h, a, q[wave], qt[wave]) - lse);
+    if (j < n_t && batch_sees(p, pos, j)) sum += exp2f(score<T, D>(p, t, j, h, a, q[wave], qt[wave]) - lse);
     lds_fence();
   }
   sum_s[wave][lane] = sum;
   __syncthreads();
   if (wave == 0 && j < n_t) {
     float* w = p.weights + t * p.weights_stride + j;
-    const float all = (sum_s[0][lane] + sum_s[1][lane]) + (sum_s[2][lane] + sum_s[3][lane]);
+    float all = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) all += sum_s[i][lane];
     *w = p.decay == 0.f ? all : fmaf(p.decay, *w, all);
   }
 }
 
-template <typename T>
+template <typename T, int D>
 static hipError_t launch_weights(const WeightsParams& p, int rows, hipStream_t s) {
-  if (p.b_k != nullptr) {
-    const int64_t n = static_cast<int64_t>(rows) * p.rank;
-    hipLaunchKernelGGL((weights_qt_kernel<T>), dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, s, p, n);
-  }
-  hipLaunchKernelGGL((weights_stats_kernel<T>), dim3(static_cast<unsigned>(rows < 65536 ? rows : 65536)), dim3(256), 0, s, p, static_cast<int64_t>(rows));
-  hipLaunchKernelGGL((weights_sum_kernel<T>), dim3((p.max_seq_len + 63) / 64, p.n_seqs), dim3(256), 0, s, p);
+  hipLaunchKernelGGL((weights_stats_kernel<T, D>), dim3(static_cast<unsigned>(rows < 65536 ? rows : 65536), p.n_splits), dim3(256), 0, s, p, static_cast<int64_t>(rows));
+  hipLaunchKernelGGL((weights_sum_kernel<T, D>), dim3((p.max_seq_len + 63) / 64, p.n_seqs), dim3(1024), 0, s, p);
   return hipGetLastError();
+}
+
+template <typename T>
+static hipError_t launch_weights_t(const WeightsParams& p, int rows, hipStream_t s) {
+  return p.head_dim == 128 ? launch_weights<T, 128>(p, rows, s) : launch_weights<T, 64>(p, rows, s);
 }
 
 }  // namespace lra
@@ -150,8 +174,7 @@ extern "C" {
 static lra_status check_key_weights(const lra_shape* shape, const lra_cache* cache, const lra_batch* batch) {
   const lra_status st = check_batch(shape, cache, batch);
   if (st != LRA_OK) return st;
-  // (a grid dimension holds fewer than 2^32 threads)
-  if (cache->n_seqs > 65535 || static_cast<int64_t>(batch->n_queries) * shape->n_q_heads * shape->rank >= (int64_t{1} << 32)) return LRA_ERR_UNSUPPORTED;
+  if (cache->n_seqs > 65535) return LRA_ERR_UNSUPPORTED;  // (sequences in a grid's y)
   return LRA_OK;
 }
 
@@ -187,8 +210,8 @@ lra_status lra_key_weights(const lra_shape* shape, const lra_cache* cache, const
   p.decay = decay;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const hipError_t err = pl.mfma ? launch_key_weights_mfma(p, s)
-                         : shape->dtype == LRA_BF16 ? launch_weights<bf16_t>(p, pl.rows, s)
-                                                    : launch_weights<float>(p, pl.rows, s);
+                         : shape->dtype == LRA_BF16 ? launch_weights_t<bf16_t>(p, pl.rows, s)
+                                                    : launch_weights_t<float>(p, pl.rows, s);
   return err == hipSuccess ? LRA_OK : LRA_ERR_HIP;
 }
 

@@ -107,7 +107,7 @@ def test_key_weights_refuse_before_launch(lib):
     ad.b_k = None                                  # nothing is rotated then
     assert weigh(lib, sh, c, ad, b) == WS
     sh, c, ad, b = good()
-    b.n_queries = b.max_queries_per_seq = 1 << 25  # 2^30 rows of 16 ranks
+    b.n_queries = b.max_queries_per_seq = (1 << 25) + 1  # more than 2^30 rows
     assert weigh(lib, sh, c, ad, b, ws_bytes=1 << 50) == UNSUP
     assert lib.lra_key_weights_workspace_bytes(ctypes.byref(sh), ctypes.byref(c), ctypes.byref(b), None) == ctypes.c_size_t(-1).value
 

@@ -56,6 +56,29 @@ def test_masks(mask, dtype, rank, heads):
     check(BatchCase(lens, counts, causal, window, sinks, heads, rank, dtype, paged=True, seed=mask))
 
 
+@pytest.mark.parametrize("variant", [1, 2])
+@pytest.mark.parametrize("rank,heads", [(16, (8, 2, 128)), (64, (6, 3, 128)), (32, (14, 2, 64))])
+@pytest.mark.parametrize("mask", range(len(MASKS)))
+def test_masks_on_the_kernels_that_other_sizes_take(mask, rank, heads, variant):
+    """1: the vector-ALU kernels, 2: the tile-walking kernel also where a sequence has few rows."""
+    lens, counts, causal, window, sinks = MASKS[mask]
+    old = lra.lra_set_kernel_variant(variant)
+    try:
+        check(BatchCase(lens, counts, causal, window, sinks, heads, rank, BF16, paged=mask % 2 == 0 or len(lens) > 1, seed=mask))
+    finally:
+        lra.lra_set_kernel_variant(old)
+
+
+@pytest.mark.parametrize("heads,rank", [((8, 2, 128), 16), ((8, 2, 64), 32), ((4, 4, 128), 64), ((28, 4, 128), 8)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_few_rows_on_long_contexts(causal, heads, rank):
+    """Every wave of a share with several tiles, shares without keys, sequences without queries, a window that starts inside a block."""
+    most = 32 // (heads[0] // heads[1])
+    counts = [min(4, most), 1, 0, min(3, most)]
+    check(BatchCase([5000, 37, 900, 2311], counts, causal, 0, 0, heads, rank, BF16, seed=6))
+    check(BatchCase([5000, 37, 900, 2311], counts, causal, 1999, 70, heads, rank, BF16, seed=7))
+
+
 @pytest.mark.parametrize("dtype,rank", [(F32, 8), (BF16, 16), (BF16, 12), (BF16, 64)])
 @pytest.mark.parametrize("mask", [0, 2, 4, 5, 8, 10, 11])
 @pytest.mark.parametrize("head_major", [False, True])
