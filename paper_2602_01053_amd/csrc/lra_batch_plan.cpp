@@ -137,7 +137,16 @@ WeightsPlan plan_key_weights(const lra_shape* sh, const lra_cache* c, const lra_
     const size_t rp = sh->rank <= 16 ? 16 : (sh->rank <= 32 ? 32 : 64);
     pl.off_lse = aligned(rows * 2 * rp * 2);
     pl.off_stats = pl.off_lse + aligned(rows * sizeof(float));
-    pl.bytes = pl.off_stats + aligned(rows * static_cast<size_t>(pl.n_splits) * 2 * sizeof(float));
+    pl.off_sums = pl.bytes = pl.off_stats + aligned(rows * static_cast<size_t>(pl.n_splits) * 2 * sizeof(float));
+    // sums over many rows: workgroups of 128 keys, the heads divided as long as all workgroups are on the chip at once, two to a
+    // compute unit (64 queries, 18 k tokens, 8 heads: 29 us in 3 groups; 31 in 8, which come in three turns)
+    const int64_t spans = (c->max_seq_len + 127) / 128 * c->n_seqs;
+    pl.sum_groups = 1;
+    if (b->max_queries_per_seq * G > 32) {
+      pl.sum_groups = static_cast<int>(std::min<int64_t>(sh->n_kv_heads, std::max<int64_t>(1, 2 * kCUs / spans)));
+      if (pl.sum_groups > 1)
+        pl.bytes += aligned(static_cast<size_t>(pl.sum_groups) * static_cast<size_t>(c->n_seqs) * static_cast<size_t>(c->max_seq_len) * sizeof(float));
+    }
     return pl;
   }
   // vector-ALU kernels: three workgroups to a compute unit, a share of 128 keys at least

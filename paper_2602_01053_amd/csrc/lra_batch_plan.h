@@ -27,7 +27,8 @@ struct WeightsPlan {
   int n_splits;  // key shares of the statistics
   int tile_places;  // MFMA: places of 128 rows per kv head
   int rows;
-  size_t off_qt, off_lse, off_stats, bytes;
+  int sum_groups;   // MFMA, many rows: groups of kv heads that sum on their own
+  size_t off_qt, off_lse, off_stats, off_sums, bytes;
 };
 WeightsPlan plan_key_weights(const lra_shape* sh, const lra_cache* c, const lra_batch* b, const Tuning& tune);
 

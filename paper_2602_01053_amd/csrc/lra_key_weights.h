@@ -17,6 +17,8 @@ struct WeightsParams : BatchParams {
   float decay;
   int32_t rows_per_head;  // n_queries x group
   int32_t sum_tiles;      // weights_sum_rows_kernel: tiles of 32 keys per workgroup
+  int32_t sum_groups;     // weights_sum_mfma_kernel: groups that the kv heads are divided into
+  float* group_sums;      // [sum_groups][n_seqs][max_seq_len], more than one group only
 };
 
 hipError_t launch_key_weights_mfma(const WeightsParams& p, hipStream_t s);

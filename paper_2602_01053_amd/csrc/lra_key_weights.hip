@@ -202,6 +202,8 @@ lra_status lra_key_weights(const lra_shape* shape, const lra_cache* cache, const
   p.lse = reinterpret_cast<float*>(ws + pl.off_lse);
   p.stats = reinterpret_cast<float*>(ws + pl.off_stats);
   p.n_splits = pl.n_splits;
+  p.sum_groups = pl.sum_groups;
+  p.group_sums = reinterpret_cast<float*>(ws + pl.off_sums);
   p.rows_per_head = batch->n_queries * p.group;
   p.row_mul = (65535 + p.group) / p.group;
   p.tile_places = pl.tile_places;

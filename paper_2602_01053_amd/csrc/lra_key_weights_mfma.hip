@@ -8,9 +8,9 @@
 // Scores are products of bf16 in fp32, so the weights come out as exactly as fp32 sums of them allow; Qt rounded to one
 // bf16 term alone would put 1e-3 into each.  K is read twice, since a weight needs its row's maximum and sum first.
 //
-// Both passes take 64-key tiles of a kv head through LDS (buffer_load ... lds, swizzled as in the prefill kernels) past
-// query rows held 32 to a wave.  In the statistics a workgroup owns 128 rows of a sequence and a share of its keys; in the
-// sums it owns 64 keys and walks the kv heads and 128 rows at a time, so that the sum over heads and rows stays in the
+// K comes through LDS (buffer_load ... lds, swizzled as in the prefill kernels) past query rows held 32 to a wave.  In the
+// statistics a workgroup owns 128 rows of a sequence and a share of its keys, 64 at a time; in the sums it owns keys and walks
+// the kv heads and the rows, so that the sum over them stays in the
 // workgroup, is added up in one fixed order, and needs no atomics.  (K rows straight to registers as matrix operands: 64
 // lanes of a load then touch 64 places, which held the batch of 16 sequences to 3.0 and 2.3 TB/s.)
 #include "lra_decode_util.h"
@@ -318,140 +318,224 @@ __global__ __launch_bounds__(256) void weights_lse_kernel(WeightsParams p) {
   p.lse[static_cast<int64_t>(h) * p.rows_per_head + row] = sum == 0.f ? INFINITY : top + log2f(sum);
 }
 
-// Many rows: a workgroup's four waves divide them, 128 at a time, and K of the next head travels meanwhile.
+// Many rows: a workgroup owns 128 keys, 32 to a wave, which holds a head's K rows of them as matrix operands while Q walks through
+// LDS 64 rows at a time, read by all four waves.  Short or few sequences have too few workgroups for the chip: then the heads
+// are divided too, and weights_join_kernel adds the groups' sums in their order.  64 queries of 18 k tokens, 8 kv heads, d = 128:
+// 29 us and the join's 4.7 (with 64 keys to a workgroup, 128 rows at a time past K in LDS: 45); instruction issue and the turn
+// of a step, 64 rows, bound it.
+constexpr int kSumKeys = 128;
 template <int D, int RP, bool HAS_BK, bool PAGED>
 __global__ __launch_bounds__(256, 2) void weights_sum_mfma_kernel(WeightsParams p) {
   typedef KeyTiles<D, RP, PAGED> Tiles;
-  constexpr int KS = D / 16, RKS = RP / 16, KCH = D / 8, KROWS = 64 / KCH, Q_BYTES = 32 * D * 2;
-  constexpr int L_AT = 2 * Tiles::K_BYTES, Q_AT = L_AT + (HAS_BK ? Tiles::L_BYTES : 0);
-  __shared__ __align__(16) unsigned char smem[Q_AT + 4 * Q_BYTES];
-  __shared__ float sum_s[4][64];
+  constexpr int KS = D / 16, RKS = RP / 16, KCH = D / 8, KROWS = 64 / KCH, LCH = RP / 8, Q_BYTES = 64 * D * 2;
+  constexpr bool QT_EARLY = RP < 64;  // (64 registers of it would send d = 128 to scratch memory)
+  constexpr int L_AT = 2 * Tiles::K_BYTES, Q_AT = L_AT + (HAS_BK ? 2 * Tiles::L_BYTES : 0);
+  __shared__ __align__(16) unsigned char smem[Q_AT + 2 * Q_BYTES];
   const int lane = threadIdx.x & 63, l32 = lane & 31, g2 = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int j = blockIdx.x * 64, t = blockIdx.y, G = p.group;
+  const int j0 = blockIdx.x * kSumKeys, t = blockIdx.y, G = p.group;
   const int n_t = min(PF_CONST_I32(p.seq_lens)[t], p.max_seq_len);
-  if (j >= n_t) return;
+  if (j0 >= n_t) return;
   const int c0 = t > 0 ? min(max(PF_CONST_I32(p.seq_query_start)[t], 0), p.n_queries) : 0;
   const int c1 = t + 1 < p.n_seqs ? min(max(PF_CONST_I32(p.seq_query_start)[t + 1], c0), p.n_queries) : p.n_queries;
   const int n_rows = (c1 - c0) * G, step = p.causal ? 1 : 0;
   const int first_pos = p.causal ? n_t - (c1 - c0) : n_t - 1;
   const int lo = p.window > 0 ? max(0, first_pos - p.window + 1) : 0, sinks = min(p.sinks, lo);
   const float sc = p.scale * 1.44269504088896340736f;
-  pf_f32x16 acc[2];
+  pf_f32x16 acc;
 #pragma unroll
-  for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) acc[kt][i] = 0.f;
-  if (n_rows > 0 && (j < sinks || j + 63 >= lo)) {
-    Tiles tiles(p, smem, t, n_t, sinks, lo, wave, lane);
-    tiles.look_up(j);
-    if (HAS_BK) tiles.issue_l(j, L_AT);
-    tiles.issue_k(j, 0, 0);
-    const int rgs = (n_rows + 127) / 128;
-    // A wave's 32 rows of group rg of head h: Q to its part of LDS, Qt and lse to registers, one item ahead
-    const uint32_t q_lds = Q_AT + wave * Q_BYTES;
-    pf_u32x4 hi_next[RKS], lo_next[RKS];
-    float lse_next = 0.f;
-    auto request = [&](int h, int rg) __attribute__((always_inline)) {
-      const int r0 = rg * 128 + wave * 32;
-      if (r0 >= n_rows) return;
+  for (int i = 0; i < 16; ++i) acc[i] = 0.f;
+  if (n_rows > 0 && (j0 < sinks || j0 + kSumKeys > lo)) {
+    Tiles tile_a(p, smem, t, n_t, sinks, lo, wave, lane), tile_b = tile_a;
+    tile_a.look_up(j0);
+    tile_b.look_up(j0 + 64);
+    int h = p.n_kv_heads * static_cast<int>(blockIdx.z) / static_cast<int>(gridDim.z);
+    const int h_end = p.n_kv_heads * (static_cast<int>(blockIdx.z) + 1) / static_cast<int>(gridDim.z);
+    auto request_k = [&](int head) __attribute__((always_inline)) {
+      tile_a.issue_k(j0, head, 0);
+      tile_b.issue_k(j0 + 64, head, Tiles::K_BYTES);
+    };
+    auto request_q = [&](int head, int rg, uint32_t at) __attribute__((always_inline)) {
+      const int r0 = rg * 64;
       int tok0, head0;
       split_row(r0, G, tok0, head0);
-      const pf_u32x4 rs = pf_rsrc(static_cast<const bf16_t*>(p.q) + (static_cast<int64_t>(c0 + tok0) * p.n_q_heads + h * G) * D, 0x7ffff000u);
+      const pf_u32x4 rs = pf_rsrc(static_cast<const bf16_t*>(p.q) + (static_cast<int64_t>(c0 + tok0) * p.n_q_heads + head * G) * D, 0x7ffff000u);
 #pragma unroll
-      for (int i = 0; i < 32 / KROWS; ++i) {
+      for (int i = 0; i < 64 / KROWS / 4; ++i) {
         // (past the end the last row again: zeros would turn infinite keys into NaN)
-        const int r = i * KROWS + lane / KCH, at = head0 + min(r, n_rows - 1 - r0), dt = (at * p.row_mul) >> 16;
-        const uint32_t off = static_cast<uint32_t>((dt * p.n_q_heads + at - dt * G) * D * 2) + ((lane % KCH ^ pf_swz_k<D>(r)) << 4);
-        pf_load16_to_lds(rs, tiles.lds0 + q_lds + i * 1024, off, 0);
+        const int r = (wave + 4 * i) * KROWS + lane / KCH, in = head0 + min(r, n_rows - 1 - r0), dt = (in * p.row_mul) >> 16;
+        const uint32_t off = static_cast<uint32_t>((dt * p.n_q_heads + in - dt * G) * D * 2) + ((lane % KCH ^ pf_swz_k<D>(r)) << 4);
+        pf_load16_to_lds(rs, tile_a.lds0 + at + (wave + 4 * i) * 1024, off, 0);
       }
-      const int64_t row = static_cast<int64_t>(h) * p.rows_per_head + static_cast<int64_t>(c0) * G + min(r0 + l32, n_rows - 1);
-      if constexpr (HAS_BK) {
-        const bf16_t* qt = reinterpret_cast<const bf16_t*>(p.qt) + row * 2 * RP + g2 * 8;
-#pragma unroll
-        for (int ks = 0; ks < RKS; ++ks) {
-          hi_next[ks] = *reinterpret_cast<const pf_u32x4*>(qt + ks * 16);
-          lo_next[ks] = *reinterpret_cast<const pf_u32x4*>(qt + RP + ks * 16);
-        }
-      }
-      lse_next = p.lse[row];
     };
-    request(0, 0);
-    int h = 0, rg = 0;
-    uint32_t k_at = 0;
-    for (;;) {
-      pf_wait_vm0();
-      lds_fence();
-      if (rg == 0) {
-        __syncthreads();  // K of this head is here for everyone, and everyone is done with the one before
-        if (h + 1 < p.n_kv_heads) tiles.issue_k(j, h + 1, k_at ^ Tiles::K_BYTES);
-      }
-      const int r0 = rg * 128 + wave * 32;
-      const bool live = r0 < n_rows;
-      pf_bf16x8 q[KS], hi[RKS], low[RKS];
-      float nl = -INFINITY;
-      int pos = 0, pos_first = 0, pos_last = -1;
-      if (live) {
-        const int q_pre = l32 * (D * 2) + (pf_swz_k<D>(l32) << 4);
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) q[ks] = pf_as_bf16x8(*reinterpret_cast<const uint4*>(smem + q_lds + (q_pre ^ ((2 * ks + g2) << 4))));
-#pragma unroll
-        for (int ks = 0; ks < RKS; ++ks) {
-          hi[ks] = __builtin_bit_cast(pf_bf16x8, hi_next[ks]);
-          low[ks] = __builtin_bit_cast(pf_bf16x8, lo_next[ks]);
-        }
-        nl = -lse_next;
-        if (r0 + l32 >= n_rows) nl = -INFINITY;
-        int tok, g;
-        split_row(min(r0 + l32, n_rows - 1), G, tok, g);
-        pos = first_pos + step * tok;
-        pos_first = __builtin_amdgcn_readfirstlane(pos);
-        pos_last = __builtin_amdgcn_readlane(pos, 31);
-        __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): the rows have been read before the next ones are asked for
+    const int rgs = (n_rows + 63) / 64;
+    if (HAS_BK) {
+      tile_a.issue_l(j0, L_AT);
+      tile_b.issue_l(j0 + 64, L_AT + Tiles::L_BYTES);
+    }
+    request_k(h);
+    request_q(h, 0, Q_AT);
+    const int jw = j0 + 32 * wave;  // the wave's first key
+    pf_bf16x8 ka[KS], la[RKS];
+    uint32_t q_at = Q_AT;
+    const int pre = l32 * (D * 2) + (pf_swz_k<D>(l32) << 4);
+    bool first = true;
+    for (; h < h_end; ++h) {
+      const bf16_t* qt_h = reinterpret_cast<const bf16_t*>(p.qt) + (static_cast<int64_t>(h) * p.rows_per_head + static_cast<int64_t>(c0) * G) * 2 * RP + g2 * 8;
+      const float* lse_h = p.lse + static_cast<int64_t>(h) * p.rows_per_head + static_cast<int64_t>(c0) * G;
+      for (int rg = 0; rg < rgs; ++rg) {
+        pf_wait_vm0();
         lds_fence();
-      }
-      const uint32_t k_now = k_at;
-      const bool more = rg + 1 < rgs || h + 1 < p.n_kv_heads;
-      if (rg + 1 < rgs) {
-        ++rg;
-      } else {
-        rg = 0;
-        ++h;
-        k_at ^= Tiles::K_BYTES;
-      }
-      if (more) request(h, rg);
-      if (live && j <= pos_last && !(p.window > 0 && j + 63 + p.window <= pos_first && j >= p.sinks)) {
+        __syncthreads();  // these rows (and K of the head) are here for everyone, and everyone is done with the rows before
+        if (rg == 0) {
+          const unsigned char* k = smem + wave * 32 * D * 2;
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) ka[ks] = pf_as_bf16x8(*reinterpret_cast<const uint4*>(k + (pre ^ ((2 * ks + g2) << 4))));
+          if (HAS_BK && first) {
+            const unsigned char* row = smem + L_AT + (32 * wave + l32) * (RP * 2) + g2 * 8;
+#pragma unroll
+            for (int ks = 0; ks < RKS; ++ks) {
+              const uint2 x = *reinterpret_cast<const uint2*>(row + (((2 * ks) ^ pf_swz_l<LCH>(l32)) << 4));
+              const uint2 y = *reinterpret_cast<const uint2*>(row + (((2 * ks + 1) ^ pf_swz_l<LCH>(l32)) << 4));
+              la[ks] = pf_as_bf16x8(make_uint4(x.x, x.y, y.x, y.y));
+            }
+          }
+          first = false;
+          if (h + 1 < h_end) {
+            __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): a wave reads only K rows that
+            __syncthreads();                     // others requested: all have read theirs before the next head's come
+            request_k(h + 1);
+          }
+        }
+        const int r0 = rg * 64;
+        // lse and Qt of this lane's two rows: on the way while K Q^T is formed
+        float nl[2];
+        pf_u32x4 hi[2][RKS], low[2][RKS];
+        auto load_qt = [&](int rt, int r) __attribute__((always_inline)) {
+          const bf16_t* row = qt_h + static_cast<int64_t>(r) * 2 * RP;
+#pragma unroll
+          for (int ks = 0; ks < RKS; ++ks) {
+            hi[rt][ks] = *reinterpret_cast<const pf_u32x4*>(row + ks * 16);
+            low[rt][ks] = *reinterpret_cast<const pf_u32x4*>(row + RP + ks * 16);
+          }
+        };
+#pragma unroll
+        for (int rt = 0; rt < 2; ++rt) {
+          const int r = min(r0 + 32 * rt + l32, n_rows - 1);
+          nl[rt] = lse_h[r];
+          if constexpr (HAS_BK && QT_EARLY) load_qt(rt, r);
+        }
+        const int pos_first = first_pos + step * __builtin_amdgcn_readfirstlane(r0 / G);
+        const int pos_last = first_pos + step * __builtin_amdgcn_readfirstlane(min(r0 + 63, n_rows - 1) / G);
+        const bool live = jw <= pos_last && !(p.window > 0 && jw + 31 + p.window <= pos_first && jw >= p.sinks);
         pf_f32x16 s[2];
-        tile_scores<D, RP, HAS_BK>(p, smem + k_now, smem + L_AT, l32, g2, q, hi, low, j, pos, pos_first, pos_last, s);
+        if (live) {
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
+          for (int rt = 0; rt < 2; ++rt)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) acc[kt][i] += __builtin_amdgcn_exp2f(fmaf(s[kt][i], sc, nl));
+            for (int i = 0; i < 16; ++i) s[rt][i] = 0.f;
+          // (two k-steps of Q read ahead of the products: left to itself the compiler waits for each read)
+          uint4 q[2][2][2];
+          auto read_q = [&](int part) __attribute__((always_inline)) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+              for (int rt = 0; rt < 2; ++rt)
+                q[part & 1][k][rt] = *reinterpret_cast<const uint4*>(smem + q_at + (pre ^ ((2 * (2 * part + k) + g2) << 4)) + rt * 32 * D * 2);
+          };
+          read_q(0);
+#pragma unroll
+          for (int part = 0; part < KS / 2; ++part) {
+            if (part + 1 < KS / 2) read_q(part + 1);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+              for (int rt = 0; rt < 2; ++rt)
+                s[rt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[2 * part + k], pf_as_bf16x8(q[part & 1][k][rt]), s[rt], 0, 0, 0);
+          }
+          if constexpr (HAS_BK && !QT_EARLY) {
+#pragma unroll
+            for (int rt = 0; rt < 2; ++rt) load_qt(rt, min(r0 + 32 * rt + l32, n_rows - 1));
+          }
+          if constexpr (HAS_BK) {
+#pragma unroll
+            for (int ks = 0; ks < RKS; ++ks)
+#pragma unroll
+              for (int rt = 0; rt < 2; ++rt) {
+                s[rt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(la[ks], __builtin_bit_cast(pf_bf16x8, low[rt][ks]), s[rt], 0, 0, 0);
+                s[rt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(la[ks], __builtin_bit_cast(pf_bf16x8, hi[rt][ks]), s[rt], 0, 0, 0);
+              }
+          }
+        }
+        // the next rows (here, since the wait for Qt would be one for them too; behind the last they come once more)
+        q_at = q_at == Q_AT ? Q_AT + Q_BYTES : Q_AT;
+        const bool same = rg + 1 < rgs, last_head = h + 1 >= h_end;
+        request_q(same || last_head ? h : h + 1, same ? rg + 1 : (last_head ? rg : 0), q_at);
+        if (live) {
+#pragma unroll
+          for (int rt = 0; rt < 2; ++rt) {
+            const int pos = first_pos + step * (min(r0 + 32 * rt + l32, n_rows - 1) / G);  // (used at the edges only)
+            if (jw + 31 > pos_first) {  // some row does not see the last key
+              const int last = pos - jw - 4 * g2;
+#pragma unroll
+              for (int i = 0; i < 16; ++i)
+                if (8 * (i >> 2) + (i & 3) > last) s[rt][i] = -INFINITY;
+            }
+            if (p.window > 0 && jw + p.window <= pos_last && jw + 32 > p.sinks) {  // some row's window starts behind the first key
+              const int from = p.sinks - jw - 4 * g2;  // hidden: `hidden` keys from here on
+              const uint32_t hidden = static_cast<uint32_t>(max(0, pos - p.window + 1 - p.sinks));
+#pragma unroll
+              for (int i = 0; i < 16; ++i)
+                if (static_cast<uint32_t>(8 * (i >> 2) + (i & 3) - from) < hidden) s[rt][i] = -INFINITY;
+            }
+            const float minus = r0 + 32 * rt + l32 < n_rows ? -nl[rt] : -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[i] += __builtin_amdgcn_exp2f(fmaf(s[rt][i], sc, minus));
+          }
+        }
       }
-      if (!more) break;
     }
   }
-  // over the 32 lanes of a half (its rows), then the waves
-#pragma unroll
-  for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float v = acc[kt][i];
-      v += lane_ror<8>(v);
-      v += lane_ror<4>(v);
-      v += lane_ror<2>(v);
-      v += lane_ror<1>(v);
-      float o = v;
-      permlane16_swap(v, o);
-      v += o;
-      if (l32 == 0) sum_s[wave][32 * kt + 8 * (i >> 2) + 4 * g2 + (i & 3)] = v;
-    }
+  // over the 32 lanes of a half (its rows); the Q buffers serve the way to one key per lane (once the last
+  // request has arrived there)
+  pf_wait_vm0();
+  lds_fence();
   __syncthreads();
-  if (wave == 0 && j + lane < n_t) {
-    float* w = p.weights + t * p.weights_stride + j + lane;
-    const float all = (sum_s[0][lane] + sum_s[1][lane]) + (sum_s[2][lane] + sum_s[3][lane]);
-    *w = p.decay == 0.f ? all : fmaf(p.decay, *w, all);
+  float* sum_s = reinterpret_cast<float*>(smem + Q_AT) + wave * 32;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    float v = acc[i];
+    v += lane_ror<8>(v);
+    v += lane_ror<4>(v);
+    v += lane_ror<2>(v);
+    v += lane_ror<1>(v);
+    float o = v;
+    permlane16_swap(v, o);
+    v += o;
+    if (l32 == 0) sum_s[8 * (i >> 2) + 4 * g2 + (i & 3)] = v;
   }
+  __builtin_amdgcn_s_waitcnt(0xc07f);
+  lds_fence();
+  const int j = j0 + 32 * wave + l32;
+  if (g2 == 0 && j < n_t) {
+    if (gridDim.z > 1) {
+      p.group_sums[(static_cast<int64_t>(blockIdx.z) * p.n_seqs + t) * p.max_seq_len + j] = sum_s[l32];
+    } else {
+      float* w = p.weights + t * p.weights_stride + j;
+      *w = p.decay == 0.f ? sum_s[l32] : fmaf(p.decay, *w, sum_s[l32]);
+    }
+  }
+}
+
+// the sums of groups of heads, in the groups' order
+__global__ __launch_bounds__(256) void weights_join_kernel(WeightsParams p) {
+  const int t = blockIdx.y, j = blockIdx.x * 256 + threadIdx.x;
+  if (j >= min(PF_CONST_I32(p.seq_lens)[t], p.max_seq_len)) return;
+  float* w = p.weights + t * p.weights_stride + j;
+  float all = 0.f;
+  for (int g = 0; g < p.sum_groups; ++g) all += p.group_sums[(static_cast<int64_t>(g) * p.n_seqs + t) * p.max_seq_len + j];
+  *w = p.decay == 0.f ? all : fmaf(p.decay, *w, all);
 }
 
 // Few rows (32 at most per sequence and kv head: a decode step of some agents).  Waves divide the heads: a wave holds the rows
@@ -651,7 +735,8 @@ static void launch_passes(const WeightsParams& p, hipStream_t s) {
     hipLaunchKernelGGL((weights_sum_rows_kernel<D, RP, HAS_BK, PAGED>), grid, dim3(256), 0, s, q);
   } else {
     hipLaunchKernelGGL(weights_lse_kernel, dim3((p.rows_per_head + 63) / 64, p.n_kv_heads), dim3(256), 0, s, p);
-    hipLaunchKernelGGL((weights_sum_mfma_kernel<D, RP, HAS_BK, PAGED>), dim3((p.max_seq_len + 63) / 64, p.n_seqs), dim3(256), 0, s, p);
+    hipLaunchKernelGGL((weights_sum_mfma_kernel<D, RP, HAS_BK, PAGED>), dim3((p.max_seq_len + kSumKeys - 1) / kSumKeys, p.n_seqs, p.sum_groups), dim3(256), 0, s, p);
+    if (p.sum_groups > 1) hipLaunchKernelGGL(weights_join_kernel, dim3((p.max_seq_len + 255) / 256, p.n_seqs), dim3(256), 0, s, p);
   }
 }
 

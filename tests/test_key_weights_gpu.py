@@ -87,6 +87,13 @@ def test_long_contexts():
     check(BatchCase([9000, 20000], [40, 1], True, 5000, 4, (4, 1, 64), 32, seed=2))
 
 
+@pytest.mark.parametrize("heads,rank", [((8, 4, 64), 16), ((6, 3, 128), 64), ((10, 5, 128), 32)])
+@pytest.mark.parametrize("longest", [3000, 12000, 40000])  # (one, some and all of the heads to a workgroup)
+def test_several_heads_of_a_workgroup(longest, heads, rank):
+    check(BatchCase([1333, 2900], [70, 33], True, 0, 0, heads, rank, seed=7), max_seq_len=longest, decay=0.5)
+    check(BatchCase([1333, 2900], [33, 170], True, 700, 3, heads, rank, seed=8), max_seq_len=longest)
+
+
 @pytest.mark.parametrize("dtype,rank", [(F32, 8), (BF16, 16)])
 def test_scores_of_minus_infinity(dtype, rank):
     c = BatchCase([600], [3], False, 0, 0, (4, 2, 64), rank, dtype, key_side=False, seed=5)
