@@ -140,7 +140,7 @@ WeightsPlan plan_key_weights(const lra_shape* sh, const lra_cache* c, const lra_
     pl.off_sums = pl.bytes = pl.off_stats + aligned(rows * static_cast<size_t>(pl.n_splits) * 2 * sizeof(float));
     // sums over many rows: workgroups of 128 keys, the heads divided as long as all workgroups are on the chip at once, two to a
     // compute unit (64 queries, 18 k tokens, 8 heads: 29 us in 3 groups; 31 in 8, which come in three turns)
-    const int64_t spans = (c->max_seq_len + 127) / 128 * c->n_seqs;
+    const int64_t spans = static_cast<int64_t>(c->max_seq_len + 127) / 128 * c->n_seqs;
     pl.sum_groups = 1;
     if (b->max_queries_per_seq * G > 32) {
       pl.sum_groups = static_cast<int>(std::min<int64_t>(sh->n_kv_heads, std::max<int64_t>(1, 2 * kCUs / spans)));
