@@ -452,7 +452,7 @@ size_t lra_batch_workspace_bytes(const lra_shape* shape, const lra_cache* cache,
  * cache that may not grow goes by when it lets tokens go.  For j < seq_lens[t]
  *     weights[t][j] = decay * weights[t][j] + sum over the queries of sequence t and the Hq heads of P[j],
  * P the softmax of the query's scores (as lra_attn_batch has them: same mask, scale and key-side adapters; zero where
- * the query does not see j).  One sum per token and not per head: the L row of a token serves every head and every
+ * the query does not see j; a query whose every visible score is minus infinity adds nothing).  One sum per token and not per head: the L row of a token serves every head and every
  * agent, so a token leaves the cache for all of them or for none.  For a prompt, the queries may be its last few
  * tokens only (causal): the batch need not hold every new token.
  *
@@ -498,7 +498,8 @@ lra_status lra_evict_select(const lra_cache* cache, const float* weights, int64_
  *
  *   n_adapters   low-rank caches to move, >= 1; more than one only where both caches have an l_adapter_stride
  *   kept         DEVICE int32 [n_seqs][kept_stride], kept_stride >= dst->max_seq_len; entries in [0, src length)
- *   weights, dst_weights   DEVICE float [n_seqs][...] or both NULL; strides >= the max_seq_len of src and dst
+ *   weights, dst_weights   DEVICE float [n_seqs][...] or both NULL, not the same memory; strides >= the max_seq_len of
+ *                          src and dst
  * More than 65535 sequences are LRA_ERR_UNSUPPORTED, and so is key_rope_theta > 0: K_base may hold rotated keys (they keep the angles of their first
  * positions), but an adapter's part that is rotated by the token's index would turn with the move.
  */

@@ -396,6 +396,7 @@ lra_status lra_cache_gather(const lra_shape* shape, const lra_cache* src, int32_
   if (src->n_seqs != dst->n_seqs || n_adapters < 1 || kept_stride < dst->max_seq_len) return LRA_ERR_SHAPE;
   if (n_adapters > 1 && (src->l_adapter_stride == 0 || dst->l_adapter_stride == 0)) return LRA_ERR_SHAPE;
   if (weights && (weights_stride < src->max_seq_len || dst_weights_stride < dst->max_seq_len)) return LRA_ERR_SHAPE;
+  if (weights && weights == dst_weights) return LRA_ERR_SHAPE;  // (workgroups would overwrite what others have yet to read)
   if (src->block_size == 0 ? src->k_base == dst->k_base || src->v_base == dst->v_base || src->l == dst->l
                            : dst->block_size != 0 && src->block_table == dst->block_table && src->k_base == dst->k_base)
     return LRA_ERR_SHAPE;

@@ -152,3 +152,9 @@ def test_gather_refuses_before_launch(lib):
     sh, src, dst = two()
     assert gather(sh, page(FAKE), dst) == SHAPE                         # three sequences and one
     assert gather(sh, page(FAKE), page(FAKE), ks=8192) == SHAPE         # one table over one pool
+
+
+def test_gather_refuses_weights_in_place(lib):
+    sh, src, _, _ = good()
+    dst = LraCache(2 * FAKE, 2 * FAKE, 2 * FAKE, 1024, 128, 0, 0, 0, 0, 1, 0, 0, None, FAKE, 4096)
+    assert lib.lra_cache_gather(ctypes.byref(sh), ctypes.byref(src), 1, FAKE, 4096, ctypes.byref(dst), FAKE, 8192, FAKE, 8192, None) == SHAPE
