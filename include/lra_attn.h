@@ -463,7 +463,7 @@ size_t lra_batch_workspace_bytes(const lra_shape* shape, const lra_cache* cache,
  *              caches are formed from q B_K^T in 16 bits of mantissa, so that small sums keep their order.
  *   workspace  DEVICE, 256-byte aligned, >= lra_key_weights_workspace_bytes(...), as for lra_attn_batch
  * A rotated key-side adapter (key_rope_theta > 0 with a b_k) is LRA_ERR_UNSUPPORTED: its keys depend on the token's
- * index, which an eviction changes.  So are more than 65535 sequences.
+ * index, which an eviction changes.  So are more than 65535 sequences and a max_seq_len beyond 2^27.
  */
 lra_status lra_key_weights(const lra_shape* shape, const lra_cache* cache, const lra_adapters* adapters,
                            const lra_batch* batch, const void* q, float decay, float* weights, int64_t weights_stride,
@@ -500,8 +500,9 @@ lra_status lra_evict_select(const lra_cache* cache, const float* weights, int64_
  *   kept         DEVICE int32 [n_seqs][kept_stride], kept_stride >= dst->max_seq_len; entries in [0, src length)
  *   weights, dst_weights   DEVICE float [n_seqs][...] or both NULL, not the same memory; strides >= the max_seq_len of
  *                          src and dst
- * More than 65535 sequences are LRA_ERR_UNSUPPORTED, and so is key_rope_theta > 0: K_base may hold rotated keys (they keep the angles of their first
- * positions), but an adapter's part that is rotated by the token's index would turn with the move.
+ * More than 65535 sequences or a max_seq_len of dst beyond 2^27 are LRA_ERR_UNSUPPORTED, and so is key_rope_theta > 0:
+ * K_base may hold rotated keys (they keep the angles of their first positions), but an adapter's part that is rotated by
+ * the token's index would turn with the move.
  */
 lra_status lra_cache_gather(const lra_shape* shape, const lra_cache* src, int32_t n_adapters, const int32_t* kept,
                             int64_t kept_stride, const lra_cache* dst, const float* weights, int64_t weights_stride,

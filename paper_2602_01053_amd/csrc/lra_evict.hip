@@ -400,7 +400,7 @@ lra_status lra_cache_gather(const lra_shape* shape, const lra_cache* src, int32_
   if (src->block_size == 0 ? src->k_base == dst->k_base || src->v_base == dst->v_base || src->l == dst->l
                            : dst->block_size != 0 && src->block_table == dst->block_table && src->k_base == dst->k_base)
     return LRA_ERR_SHAPE;
-  if (shape->key_rope_theta > 0.f || src->n_seqs > 65535) return LRA_ERR_UNSUPPORTED;
+  if (shape->key_rope_theta > 0.f || src->n_seqs > 65535 || dst->max_seq_len > (1 << 27)) return LRA_ERR_UNSUPPORTED;
   GatherParams p{};
   p.src = gather_side(shape, src);
   p.dst = gather_side(shape, dst);

@@ -207,7 +207,8 @@ extern "C" {
 static lra_status check_key_weights(const lra_shape* shape, const lra_cache* cache, const lra_batch* batch) {
   const lra_status st = check_batch(shape, cache, batch);
   if (st != LRA_OK) return st;
-  if (cache->n_seqs > 65535) return LRA_ERR_UNSUPPORTED;  // (sequences in a grid's y)
+  // (sequences in a grid's y; sixteen threads per token in a dimension of fewer than 2^32)
+  if (cache->n_seqs > 65535 || cache->max_seq_len > (1 << 27)) return LRA_ERR_UNSUPPORTED;
   return LRA_OK;
 }
 

@@ -158,3 +158,14 @@ def test_gather_refuses_weights_in_place(lib):
     sh, src, _, _ = good()
     dst = LraCache(2 * FAKE, 2 * FAKE, 2 * FAKE, 1024, 128, 0, 0, 0, 0, 1, 0, 0, None, FAKE, 4096)
     assert lib.lra_cache_gather(ctypes.byref(sh), ctypes.byref(src), 1, FAKE, 4096, ctypes.byref(dst), FAKE, 8192, FAKE, 8192, None) == SHAPE
+
+
+def test_longest_sequences(lib):
+    """Beyond 2^27 tokens a grid would hold 2^32 threads."""
+    ref = ctypes.byref
+    sh, c, ad, b = good()
+    for n, status in ((1 << 27, WS), ((1 << 27) + 1, UNSUP)):
+        c.max_seq_len = n
+        assert weigh(lib, sh, c, ad, b, stride=n) == status
+    dst = LraCache(2 * FAKE, 2 * FAKE, 2 * FAKE, 1024, 128, 0, 0, 0, 0, 1, 0, 0, None, FAKE, (1 << 27) + 1)
+    assert lib.lra_cache_gather(ref(sh), ref(c), 1, FAKE, 1 << 30, ref(dst), None, 0, None, 0, None) == UNSUP
