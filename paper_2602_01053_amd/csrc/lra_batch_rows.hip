@@ -236,8 +236,8 @@ __global__ __launch_bounds__(256, 2) void batch_rows_kernel(BatchParams p) {
       for (int i = 0; i < 16; ++i)
         if (static_cast<uint32_t>(8 * (i >> 2) + (i & 3) - from) < hidden) s[i] = -INFINITY;
     }
-    // Every tile's probabilities against the larger of its own maximum and 2^-16 of the largest so far would be finer by a per cent of
-    // the error; against the running maximum the accumulators are rescaled in few tiles only.
+    // (the accumulators are rescaled only where some row's maximum grows; the probabilities, at most 1, round to bf16 for the
+    // matrix cores, their sum is taken in fp32 before)
     float mx = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[i]);
