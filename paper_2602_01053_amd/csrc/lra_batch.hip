@@ -57,8 +57,7 @@ extern "C" {
 
 size_t lra_batch_workspace_bytes(const lra_shape* shape, const lra_cache* cache, const lra_batch* batch, const lra_tuning* tuning) {
   if (check_batch(shape, cache, batch) != LRA_OK) return static_cast<size_t>(-1);
-  const BatchPlan pl = plan_batch(shape, cache, batch, resolve_tuning(tuning));
-  return pl.launchable ? pl.bytes : static_cast<size_t>(-1);
+  return batch_workspace_bytes(shape, cache, batch, resolve_tuning(tuning));
 }
 
 lra_status lra_attn_batch(const lra_shape* shape, const lra_cache* cache, const lra_adapters* adapters, const lra_batch* batch,
@@ -70,7 +69,7 @@ lra_status lra_attn_batch(const lra_shape* shape, const lra_cache* cache, const 
   if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out) | reinterpret_cast<uintptr_t>(adapters->b_k) |
        reinterpret_cast<uintptr_t>(adapters->b_v)) & 15)
     return LRA_ERR_SHAPE;
-  const BatchPlan pl = plan_batch(shape, cache, batch, resolve_tuning(tuning));
+  const BatchPlan pl = plan_batch(shape, cache, batch, resolve_tuning(tuning), adapters->b_k != nullptr);
   if (!pl.launchable) return LRA_ERR_UNSUPPORTED;
   if (pl.bytes > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < pl.bytes)) return LRA_ERR_WORKSPACE;
   BatchParams p = batch_params(shape, cache, adapters, batch, q);

@@ -55,9 +55,9 @@ static void place_states(BatchPlan& pl, const lra_shape* sh) {
 // low-rank rows are (a rotated key side, a low-rank cache per adapter), and the queries of a sequence may have different ones,
 // one query.  The key tiles of a q tile are shared where there are fewer q tiles than the chip has places, two per compute
 // unit, and then so that they fill the places once; a share walks two tiles at least.
-static bool plan_tiles(BatchPlan& pl, const lra_shape* sh, const lra_cache* c, const lra_batch* b) {
+static bool plan_tiles(BatchPlan& pl, const lra_shape* sh, const lra_cache* c, const lra_batch* b, bool rotary) {
   const int64_t G = sh->n_q_heads / sh->n_kv_heads;
-  pl.tile_per_query = !b->causal && (sh->key_rope_theta > 0.f || c->l_adapter_stride > 0);
+  pl.tile_per_query = !b->causal && (rotary || c->l_adapter_stride > 0);
   const int64_t places = pl.tile_per_query ? b->n_queries : b->n_queries * G / 128 + c->n_seqs;
   if (places * sh->n_kv_heads >= (int64_t{1} << 24)) return false;  // (a grid dimension holds fewer than 2^32 threads)
   const int64_t q_tiles = pl.tile_per_query ? b->n_queries : std::max<int64_t>((b->n_queries * G + 127) / 128, std::min(c->n_seqs, b->n_queries));
@@ -70,15 +70,15 @@ static bool plan_tiles(BatchPlan& pl, const lra_shape* sh, const lra_cache* c, c
   // states also where the rows of a tile have adapters of their own (the merge kernel applies B_V row by row), and in the forms
   // that are built with them only
   const bool far = c->block_size != 0 && !pool_fits(sh, c);
-  if (shares > 1 || far || sh->key_rope_theta > 0.f || (!b->causal && !pl.tile_per_query)) place_states(pl, sh);
+  if (shares > 1 || far || rotary || (!b->causal && !pl.tile_per_query)) place_states(pl, sh);
   return true;
 }
 
 // 32 rows at most per sequence and kv head, with one low-rank cache: workgroups of (kv head, key share, sequence), two to a compute
 // unit, whose waves have a tile of 32 keys each at least.
-static bool plan_few_rows(BatchPlan& pl, const lra_shape* sh, const lra_cache* c, const lra_batch* b) {
+static bool plan_few_rows(BatchPlan& pl, const lra_shape* sh, const lra_cache* c, const lra_batch* b, bool rotary) {
   const int64_t G = sh->n_q_heads / sh->n_kv_heads;
-  if (b->max_queries_per_seq * G > 32 || sh->key_rope_theta > 0.f || c->n_seqs > 65535) return false;
+  if (b->max_queries_per_seq * G > 32 || rotary || c->n_seqs > 65535) return false;
   if (c->l_adapter_stride > 0 && !b->causal) return false;  // (the rows of a sequence share their low-rank rows)
   const int64_t units = static_cast<int64_t>(sh->n_kv_heads) * std::min(c->n_seqs, b->n_queries);
   const int64_t chunk = b->causal ? b->max_queries_per_seq : 1;
@@ -89,15 +89,16 @@ static bool plan_few_rows(BatchPlan& pl, const lra_shape* sh, const lra_cache* c
   return true;
 }
 
-BatchPlan plan_batch(const lra_shape* sh, const lra_cache* c, const lra_batch* b, const Tuning& tune) {
+BatchPlan plan_batch(const lra_shape* sh, const lra_cache* c, const lra_batch* b, const Tuning& tune, bool key_adapter) {
   BatchPlan pl{};
+  const bool rotary = sh->key_rope_theta > 0.f && key_adapter;
   const int64_t rows = static_cast<int64_t>(b->n_queries) * sh->n_q_heads;
   const int64_t keys = keys_per_row(c, b);
   pl.rows = static_cast<int>(rows);
   pl.launchable = true;
   if (sh->dtype == LRA_BF16 && sh->rank % 8 == 0 && tune.variant != 1 && mfma_fits(sh, c)) {
-    if (tune.variant == 0 && plan_few_rows(pl, sh, c, b)) return pl;
-    if (plan_tiles(pl, sh, c, b)) return pl;
+    if (tune.variant == 0 && plan_few_rows(pl, sh, c, b, rotary)) return pl;
+    if (plan_tiles(pl, sh, c, b, rotary)) return pl;
   }
   // vector-ALU kernels: one workgroup per row and share, three to a compute unit; a share of 256 keys at least, so
   // that its loop is longer than what stands around it
@@ -109,12 +110,17 @@ BatchPlan plan_batch(const lra_shape* sh, const lra_cache* c, const lra_batch* b
   share = std::min<int64_t>((share + 63) / 64 * 64, int64_t{1} << 30);
   pl.split_keys = static_cast<int>(share);
   const int64_t splits = (keys + share - 1) / share;
-  const bool rotary = sh->key_rope_theta > 0.f;
   pl.launchable = splits <= 65535 && (!rotary || rows < (int64_t{1} << 26));  // (a grid dimension holds fewer than 2^32 threads)
   if (!pl.launchable) return pl;
   pl.n_splits = static_cast<int>(splits);
   place_states(pl, sh);
   return pl;
+}
+
+size_t batch_workspace_bytes(const lra_shape* sh, const lra_cache* c, const lra_batch* b, const Tuning& tune) {
+  const BatchPlan with = plan_batch(sh, c, b, tune, true), without = plan_batch(sh, c, b, tune, false);
+  if (!with.launchable && !without.launchable) return static_cast<size_t>(-1);
+  return std::max(with.launchable ? with.bytes : 0, without.launchable ? without.bytes : 0);
 }
 
 WeightsPlan plan_key_weights(const lra_shape* sh, const lra_cache* c, const lra_batch* b, const Tuning& tune) {

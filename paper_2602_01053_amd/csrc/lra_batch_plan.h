@@ -19,7 +19,11 @@ struct BatchPlan {
   size_t off_ml, off_o, off_lr, off_adapter, bytes;
   bool launchable;  // false: LRA_ERR_UNSUPPORTED
 };
-BatchPlan plan_batch(const lra_shape* sh, const lra_cache* c, const lra_batch* b, const Tuning& tune);
+// key_adapter: whether the call has a B_K (without one a rotary key side has nothing to rotate).  lra_batch_workspace_bytes cannot
+// know and tells the larger need of the two.
+BatchPlan plan_batch(const lra_shape* sh, const lra_cache* c, const lra_batch* b, const Tuning& tune, bool key_adapter = true);
+// 0 bytes is a valid need, (size_t)-1: neither call can be launched.
+size_t batch_workspace_bytes(const lra_shape* sh, const lra_cache* c, const lra_batch* b, const Tuning& tune);
 
 // lra_key_weights: the query rows' Q B_K^T and softmax statistics, then the sums over rows key by key.
 struct WeightsPlan {

@@ -1,0 +1,22 @@
+"""Forms of the batch calls that sizes, layouts and missing operands choose."""
+import pytest
+import torch
+
+import paper_2602_01053_amd as lra
+from tests.batch_reference import BatchCase, Device, make
+from tests.test_batch_gpu import check
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("counts,causal,window", [([4, 1, 4], False, 0), ([4, 1, 4], False, 200), ([70, 1, 5], True, 0)])
+def test_a_rotary_key_side_without_adapters_is_none(counts, causal, window, dtype):
+    """Value-only adapters under key_rope_theta > 0: nothing is rotated, and the call is the one without, bit for bit."""
+    same = dict(lens=[900, 33, 500], counts=counts, causal=causal, window=window, sinks=4 if window else 0, heads=(8, 2, 128), rank=16,
+                dtype=dtype, key_side=False, seed=21)
+    out = [Device(make(BatchCase(rope=theta, **same)), lra).attend() for theta in (0.0, 10000.0)]
+    assert torch.equal(*out)
+    check(BatchCase(rope=10000.0, **same))

@@ -1,0 +1,69 @@
+"""Which kernel the batch calls take and what they need, asked of the planner compiled for the CPU (tests/batch_plan_query.cpp)."""
+from __future__ import annotations
+
+import ctypes
+import os
+import shutil
+import subprocess
+
+import pytest
+
+from paper_2602_01053_amd.binding import LraBatch, LraCache, LraShape, LraTuning
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+FIELDS = ("few_rows", "tiles", "tile_places", "tile_per_query", "states", "n_splits", "split_keys", "launchable", "pages")
+FAKE = 0x1000  # never dereferenced
+
+
+@pytest.fixture(scope="module")
+def planner(tmp_path_factory):
+    gxx = shutil.which("g++")
+    if gxx is None:
+        pytest.skip("no host C++ compiler")
+    lib = str(tmp_path_factory.mktemp("plan") / "batch_plan_query.so")
+    csrc = os.path.join(ROOT, "paper_2602_01053_amd", "csrc")
+    subprocess.run([gxx, "-std=c++17", "-O1", "-shared", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", csrc,
+                    os.path.join(csrc, "lra_plan.cpp"), os.path.join(csrc, "lra_batch_plan.cpp"),
+                    os.path.join(ROOT, "tests", "batch_plan_query.cpp"), "-o", lib], check=True)
+    return ctypes.CDLL(lib)
+
+
+def structs(hq, hkv, d, r, n, queries, *, seqs=1, causal=False, window=0, sinks=0, theta=0.0, fp32=False, variant=0, own=False):
+    """The planner's arguments for a call: contiguous for one sequence, else pages; `queries` of each sequence."""
+    cache = LraCache(FAKE, FAKE, FAKE, hkv * d, d, 0, 0, 0, 0, 1, 0, 0, None, FAKE, n)
+    if seqs > 1:
+        per = -(-n // 16)
+        cache = LraCache(FAKE, FAKE, FAKE, d, 16 * d, 16 * d * hkv, 16, per, per * seqs, seqs, 0, 0, FAKE, FAKE, n)
+    if own:
+        cache.l_adapter_stride = n * seqs * 64
+    return (LraShape(hq, hkv, d, r, int(fp32), 0.0, theta), cache,
+            LraBatch(FAKE, FAKE, seqs * queries, queries, int(causal), window, sinks), LraTuning(kernel_variant=variant))
+
+
+def plan(planner, *call, key_adapter=True, **kw):
+    out = (ctypes.c_int32 * len(FIELDS))()
+    planner.batch_plan_query(*(ctypes.byref(x) for x in structs(*call, **kw)), int(key_adapter), out)
+    return dict(zip(FIELDS, out))
+
+
+def need(planner, *call, **kw):
+    return planner.batch_workspace_query(*(ctypes.byref(x) for x in structs(*call, **kw)))
+
+
+CALLS = [dict(queries=4), dict(queries=4, window=4096, sinks=4), dict(queries=3, seqs=16, window=500), dict(queries=200, causal=True),
+         dict(queries=7, seqs=5, causal=True), dict(queries=40, seqs=3), dict(queries=2, fp32=True), dict(queries=4, own=True)]
+
+
+@pytest.mark.parametrize("call", CALLS, ids=lambda c: "-".join(f"{k}{v}" for k, v in c.items()))
+@pytest.mark.parametrize("layer", [(32, 8, 128), (28, 4, 128), (4, 4, 64)])
+def test_a_rotary_key_side_without_adapters_is_planned_as_none(planner, layer, call):
+    """Nothing is rotated where there is no B_K: the call takes the kernel and the shares of one without a rotary key side."""
+    call = dict(call)
+    queries = call.pop("queries")
+    for n in (700, 33000):
+        rotary = plan(planner, *layer, 16, n, queries, theta=500000.0, key_adapter=False, **call)
+        plain = plan(planner, *layer, 16, n, queries, key_adapter=False, **call)
+        assert rotary == plain
+        # the workspace is told before it is known whether the call has a B_K
+        size = need(planner, *layer, 16, n, queries, theta=500000.0, **call)
+        assert size == max(rotary["pages"], plan(planner, *layer, 16, n, queries, theta=500000.0, **call)["pages"])
