@@ -14,6 +14,8 @@
 
 namespace lra {
 
+constexpr int kRowsLds = 80 * 1024;  // half of a compute unit's LDS
+
 template <int D, int RP, bool HAS_BK, bool PAGED>
 __global__ __launch_bounds__(256, 2) void batch_rows_kernel(BatchParams p) {
   constexpr int KS = D / 16, RKS = RP / 16, DB = D / 32, RB = (RP + 31) / 32;
@@ -22,9 +24,19 @@ __global__ __launch_bounds__(256, 2) void batch_rows_kernel(BatchParams p) {
   constexpr int NK = 32 / KROWS, NV = NK, NL = LCH / 2;  // requests of a tile
   constexpr int SLOT = ((DB + RB) * 16 + 1) * 64 * 4;    // a wave's state, lane by lane
   constexpr int SMEM = 4 * WAVE > 2 * SLOT ? 4 * WAVE : 2 * SLOT;
+  // Two workgroups to a compute unit, as the plan counts them: where the tiles alone take half of its LDS (d = 128, ranks above 32), Qt
+  // passes through the last wave's V tile before that is requested, and the maxima through the K tiles behind the loop.  (One workgroup to
+  // a unit, rank 64: 4 agents on 32 k tokens 48 us against 38, behind a window of 4 k 25 against 18, 16 sequences behind 8 k 78 against 70.)
+  constexpr bool TIGHT = SMEM + 4 * 32 * 4 + (HAS_BK ? RKS * 1024 : 0) > kRowsLds;
+  constexpr int QT_AT = 3 * WAVE + K_BYTES;
+  static_assert(!TIGHT || (SMEM <= kRowsLds && RKS * 1024 <= K_BYTES && 4 * WAVE == SMEM));
   __shared__ __align__(16) unsigned char smem[SMEM];
-  __shared__ float m_s[4][32];
-  __shared__ __align__(16) pf_u32x4 qt_s[HAS_BK ? RKS : 1][64];
+  __shared__ float m_own[TIGHT ? 1 : 4][32];
+  __shared__ __align__(16) pf_u32x4 qt_own[HAS_BK && !TIGHT ? RKS : 1][64];
+  auto m_s = [&](int w) __attribute__((always_inline)) -> float* { return TIGHT ? reinterpret_cast<float*>(smem + w * WAVE) : m_own[w]; };
+  auto qt_s = [&](int ks) __attribute__((always_inline)) -> pf_u32x4* {
+    return TIGHT ? reinterpret_cast<pf_u32x4*>(smem + QT_AT) + ks * 64 : qt_own[ks];
+  };
   const int lane = threadIdx.x & 63, l32 = lane & 31, g2 = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int Hq = p.n_q_heads, Hkv = p.n_kv_heads, G = p.group, r = p.rank;
@@ -101,7 +113,8 @@ __global__ __launch_bounds__(256, 2) void batch_rows_kernel(BatchParams p) {
     }
   };
   auto issue_k = [&](int j) __attribute__((always_inline)) { issue_rows(p.k_base, j, 0, [](int row) { return pf_swz_k<D>(row); }); };
-  auto issue_lv = [&](int j) __attribute__((always_inline)) {
+  auto issue_v = [&](int j) __attribute__((always_inline)) { issue_rows(p.v_base, j, K_BYTES, [](int row) { return pf_swz_v<D>(row); }); };
+  auto issue_l = [&](int j) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       const int row = i * LROWS + lane / LCH, key = j + row;
@@ -109,13 +122,14 @@ __global__ __launch_bounds__(256, 2) void batch_rows_kernel(BatchParams p) {
       const int ch = lane % LCH ^ pf_swz_l<LCH>(row);
       pf_load16_to_lds(rs_l, lds0 + 2 * K_BYTES + i * 1024, kept(key) && ch * 8 < r ? index * lp2 + (ch << 4) : kPfOob, 0);
     }
-    issue_rows(p.v_base, j, K_BYTES, [](int row) { return pf_swz_v<D>(row); });
   };
   const int first = t0 + wave;
+  const bool v_late = TIGHT && HAS_BK && wave == 3;
   if (first < t1) {
     look_up(key_of(first));
     issue_k(key_of(first));
-    issue_lv(key_of(first));
+    issue_l(key_of(first));
+    if (!v_late) issue_v(key_of(first));
   }
 
   // ---------------- prologue: Q operands, Qt = Q B_K^T (as in batch_tiles_body) ----------------
@@ -158,13 +172,18 @@ __global__ __launch_bounds__(256, 2) void batch_rows_kernel(BatchParams p) {
         for (int ks = 0; ks < RKS; ++ks) {
           const pf_f32x16& c = acc[ks >> 1];
           const int o = (ks & 1) * 8;
-          qt_s[ks][lane] = pf_u32x4{pf_pack2(c[o + 0], c[o + 1]), pf_pack2(c[o + 2], c[o + 3]), pf_pack2(c[o + 4], c[o + 5]), pf_pack2(c[o + 6], c[o + 7])};
+          qt_s(ks)[lane] = pf_u32x4{pf_pack2(c[o + 0], c[o + 1]), pf_pack2(c[o + 2], c[o + 3]), pf_pack2(c[o + 4], c[o + 5]), pf_pack2(c[o + 6], c[o + 7])};
         }
       }
     }
     __syncthreads();
 #pragma unroll
-    for (int ks = 0; ks < RKS; ++ks) qtb[ks] = __builtin_bit_cast(pf_bf16x8, qt_s[ks][lane]);
+    for (int ks = 0; ks < RKS; ++ks) qtb[ks] = __builtin_bit_cast(pf_bf16x8, qt_s(ks)[lane]);
+    if constexpr (TIGHT) {
+      __syncthreads();  // (everyone has its operands)
+      lds_fence();
+      if (v_late && first < t1) issue_v(key_of(first));
+    }
   }
 
   // ---------------- per-lane LDS read offsets (see batch_tiles_body) ----------------
@@ -172,11 +191,8 @@ __global__ __launch_bounds__(256, 2) void batch_rows_kernel(BatchParams p) {
   const int a16 = lane & 15, dsel = (lane >> 4) & 1;
   const int vrow = 4 * g2 + (a16 >> 2);
   const int v_pre = K_BYTES + vrow * (D * 2) + ((((a16 & 3) >> 1) + 2 * dsel + pf_swz_v<D>(vrow)) << 4) + (a16 & 1) * 8;
-  int l_rd[RKS][2], lt_rd[RB][2];
-#pragma unroll
-  for (int ks = 0; ks < RKS; ++ks)
-#pragma unroll
-    for (int pc = 0; pc < 2; ++pc) l_rd[ks][pc] = 2 * K_BYTES + l32 * (RP * 2) + (((2 * ks + pc) ^ pf_swz_l<LCH>(l32)) << 4) + g2 * 8;
+  const int l_pre = 2 * K_BYTES + l32 * (RP * 2) + (pf_swz_l<LCH>(l32) << 4) + g2 * 8;  // (chunk c at l_pre ^ (c << 4))
+  int lt_rd[RB][2];
 #pragma unroll
   for (int b = 0; b < RB; ++b)
 #pragma unroll
@@ -213,10 +229,12 @@ __global__ __launch_bounds__(256, 2) void batch_rows_kernel(BatchParams p) {
       s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(pf_as_bf16x8(a), qb[ks], s, 0, 0, 0);
     }
     if constexpr (HAS_BK) {
+      int l_at = l_pre;
+      if constexpr (TIGHT) asm volatile("" : "+v"(l_at));  // (addresses formed again for each tile: held in registers they went to scratch memory)
 #pragma unroll
       for (int ks = 0; ks < RKS; ++ks) {
-        const uint2 x = *reinterpret_cast<const uint2*>(mine + l_rd[ks][0]);
-        const uint2 y = *reinterpret_cast<const uint2*>(mine + l_rd[ks][1]);
+        const uint2 x = *reinterpret_cast<const uint2*>(mine + (l_at ^ ((2 * ks) << 4)));
+        const uint2 y = *reinterpret_cast<const uint2*>(mine + (l_at ^ ((2 * ks + 1) << 4)));
         s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(pf_as_bf16x8(make_uint4(x.x, x.y, y.x, y.y)), qtb[ks], s, 0, 0, 0);
       }
     }
@@ -281,14 +299,18 @@ __global__ __launch_bounds__(256, 2) void batch_rows_kernel(BatchParams p) {
     }
     __builtin_amdgcn_s_waitcnt(0xc07f);  // V and L have been read
     lds_fence();
-    if (more) issue_lv(j_next);
+    if (more) {
+      issue_l(j_next);
+      issue_v(j_next);
+    }
   }
 
   // ---------------- the waves' states: two by two through LDS, wave 0 stores ----------------
   l_run += pf_partner32(l_run);
-  if (g2 == 0) m_s[wave][l32] = m_run;
+  if (g2 == 0) m_s(wave)[l32] = m_run;
   __syncthreads();
-  const float m_all = fmaxf(fmaxf(m_s[0][l32], m_s[1][l32]), fmaxf(m_s[2][l32], m_s[3][l32]));
+  const float m_all = fmaxf(fmaxf(m_s(0)[l32], m_s(1)[l32]), fmaxf(m_s(2)[l32], m_s(3)[l32]));
+  if constexpr (TIGHT) __syncthreads();  // (the states go where these were)
   const float wgt = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_all);
   l_run = m_run == -INFINITY ? l_run : l_run * wgt;  // (a sum of NaN stays one)
 #pragma unroll

@@ -1,0 +1,16 @@
+"""What the compiler reports for the kernels of the batch calls, against the workgroups per compute unit that their planner counts on."""
+from tests.test_kernel_resources_cpu import LDS, OCC, SCRATCH, table  # noqa: F401 (a fixture)
+
+
+def rows_of(table, kernel):  # noqa: F811
+    rows = {n: r for n, r in table.items() if kernel in n}
+    assert rows, kernel
+    return rows
+
+
+def test_few_rows_kernel_two_workgroups_per_compute_unit(table):  # noqa: F811
+    """Workgroups of four waves: two fit by registers (two waves per SIMD) and by LDS, at every head dimension and rank."""
+    rows = rows_of(table, "batch_rows_kernel")
+    assert len(rows) == 24
+    for name, row in rows.items():
+        assert row[SCRATCH] == 0 and row[OCC] >= 2 and row[LDS] <= 80 * 1024, (name, row)
