@@ -51,10 +51,26 @@ static void place_states(BatchPlan& pl, const lra_shape* sh) {
   pl.bytes = pl.off_adapter + aligned(static_cast<size_t>(pl.rows) * sizeof(int32_t));
 }
 
+// Key shares where a compute unit holds one workgroup (batch_tiles_kernel with a rotated key side at d = 128 and ranks above 32: 416
+// registers): those with the shortest sum of turns, up to four of the chip, a turn being its key tiles and what a prologue takes, five
+// tiles' time.  (Planned as two to a unit: 333 new tokens of 28 heads behind a window of 1000, rank 64, 90 us against 77; 4 agents on 16 k
+// tokens 119 against 107.  One turn always: 300 new tokens after 30 k in 3 shares 489 against 434 in 7.)
+static int64_t shares_by_turns(int64_t units, int64_t key_tiles) {
+  int64_t best = 1, least = INT64_MAX;
+  for (int64_t s = 1; s <= std::min<int64_t>((key_tiles + 1) / 2, 64) && (s == 1 || units * s <= 4 * kCUs); ++s) {
+    const int64_t time = (units * s + kCUs - 1) / kCUs * ((key_tiles + s - 1) / s + 5);
+    if (time < least) {
+      least = time;
+      best = s;
+    }
+  }
+  return best;
+}
+
 // A workgroup of batch_tiles_kernel takes 128 rows of one sequence; where a query's adapter decides what the keys or their
 // low-rank rows are (a rotated key side, a low-rank cache per adapter), and the queries of a sequence may have different ones,
 // one query.  The key tiles of a q tile are shared where there are fewer q tiles than the chip has places, two per compute
-// unit, and then so that they fill the places once; a share walks two tiles at least.
+// unit (but see shares_by_turns), and then so that they fill the places once; a share walks two tiles at least.
 static bool plan_tiles(BatchPlan& pl, const lra_shape* sh, const lra_cache* c, const lra_batch* b, bool rotary) {
   const int64_t G = sh->n_q_heads / sh->n_kv_heads;
   pl.tile_per_query = !b->causal && (rotary || c->l_adapter_stride > 0);
@@ -63,7 +79,10 @@ static bool plan_tiles(BatchPlan& pl, const lra_shape* sh, const lra_cache* c, c
   const int64_t q_tiles = pl.tile_per_query ? b->n_queries : std::max<int64_t>((b->n_queries * G + 127) / 128, std::min(c->n_seqs, b->n_queries));
   const int64_t chunk = b->causal ? std::min<int64_t>(b->max_queries_per_seq, 128 / G + 1) : 1;
   const int64_t key_tiles = (std::min<int64_t>(c->max_seq_len, keys_per_row(c, b) + chunk) + 63) / 64 + (b->window > 0 ? 2 : 0);
-  const int64_t shares = std::max<int64_t>(1, std::min<int64_t>({2 * kCUs / (q_tiles * sh->n_kv_heads), (key_tiles + 1) / 2, 64}));
+  const int64_t units = q_tiles * sh->n_kv_heads;
+  const bool one_per_unit = rotary && sh->head_dim == 128 && sh->rank > 32;
+  const int64_t shares = one_per_unit ? shares_by_turns(units, key_tiles)
+                                      : std::max<int64_t>(1, std::min<int64_t>({2 * kCUs / units, (key_tiles + 1) / 2, 64}));
   pl.tiles = true;
   pl.tile_places = static_cast<int>(places);
   pl.n_splits = static_cast<int>(shares);

@@ -20,3 +20,13 @@ def test_a_rotary_key_side_without_adapters_is_none(counts, causal, window, dtyp
     out = [Device(make(BatchCase(rope=theta, **same)), lra).attend() for theta in (0.0, 10000.0)]
     assert torch.equal(*out)
     check(BatchCase(rope=10000.0, **same))
+
+
+@pytest.mark.parametrize("heads,rank", [((8, 2, 128), 64), ((7, 1, 128), 40), ((4, 4, 128), 32), ((8, 2, 64), 64), ((4, 2, 64), 24)])
+@pytest.mark.parametrize("counts,causal,window", [([3, 1, 4], False, 0), ([3, 0, 2], False, 300), ([150, 1, 40], True, 0), ([33, 70, 5], True, 129)])
+@pytest.mark.parametrize("paged", [False, True])
+def test_rotated_key_sides_of_all_ranks(paged, counts, causal, window, heads, rank):
+    """Several key shares of a row, each beginning in the middle of a sequence: its first angles are formed there."""
+    lens = [1900, 75, 800]
+    n = 3 if paged else 1
+    check(BatchCase(lens[:n], counts[:n], causal, window, 5 if window else 0, heads, rank, BF16, paged=paged, rope=10000.0, seed=22))

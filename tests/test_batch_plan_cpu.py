@@ -67,3 +67,24 @@ def test_a_rotary_key_side_without_adapters_is_planned_as_none(planner, layer, c
         # the workspace is told before it is known whether the call has a B_K
         size = need(planner, *layer, 16, n, queries, theta=500000.0, **call)
         assert size == max(rotary["pages"], plan(planner, *layer, 16, n, queries, theta=500000.0, **call)["pages"])
+
+
+def test_a_rotated_key_side_at_high_ranks_has_one_workgroup_per_compute_unit(planner):
+    """Key shares of batch_tiles_kernel where one workgroup fits a compute unit (d = 128, ranks above 32): full turns of 256, not of 512."""
+    def workgroups(layer, r, n, queries, **kw):
+        pl = plan(planner, *layer, r, n, queries, theta=500000.0, **kw)
+        assert pl["tiles"] and not pl["few_rows"]
+        seqs = kw.get("seqs", 1)
+        tiles = pl["tile_places"] if pl["tile_per_query"] else max(-(-queries * seqs * layer[0] // layer[1] // 128), seqs)
+        return tiles * layer[1] * pl["n_splits"]
+
+    llama, qwen = (32, 8, 128), (28, 4, 128)
+    assert workgroups(llama, 64, 16000, 4) == 256 and workgroups(llama, 32, 16000, 4) == 512
+    assert workgroups(llama, 64, 16000, 128, causal=True) == 256
+    assert workgroups(qwen, 40, 30000, 300, causal=True) == 476            # two turns: one of 204 would leave fifty units without work
+    assert workgroups(llama, 64, 9000, 3, seqs=8) == 768                   # three full turns, not one of 192
+    for n in (1, 64, 129, 1000, 100000):
+        for queries in (1, 5, 60, 900):
+            for causal in (False, True):
+                pl = plan(planner, *llama, 64, n, queries, theta=500000.0, causal=causal)
+                assert 1 <= pl["n_splits"] <= 64 and (pl["n_splits"] == 1 or pl["n_splits"] <= (n + queries + 127) // 64)

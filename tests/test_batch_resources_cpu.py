@@ -1,5 +1,5 @@
 """What the compiler reports for the kernels of the batch calls, against the workgroups per compute unit that their planner counts on."""
-from tests.test_kernel_resources_cpu import LDS, OCC, SCRATCH, table  # noqa: F401 (a fixture)
+from tests.test_kernel_resources_cpu import LDS, OCC, SCRATCH, _args, table  # noqa: F401 (a fixture)
 
 
 def rows_of(table, kernel):  # noqa: F811
@@ -14,3 +14,15 @@ def test_few_rows_kernel_two_workgroups_per_compute_unit(table):  # noqa: F811
     assert len(rows) == 24
     for name, row in rows.items():
         assert row[SCRATCH] == 0 and row[OCC] >= 2 and row[LDS] <= 80 * 1024, (name, row)
+
+
+def test_tile_walking_kernel_two_workgroups_per_compute_unit(table):  # noqa: F811
+    """... but one of the rotated key side at d = 128 and ranks above 32, which the plan counts so."""
+    rows = rows_of(table, "batch_tiles_kernel")
+    one = 0
+    for name, row in rows.items():
+        d, rp, _, _, _, _, rope = _args(name)
+        two = not (rope and d == 128 and rp == 64)
+        one += not two
+        assert row[SCRATCH] == 0 and row[OCC] >= (2 if two else 1) and row[LDS] <= (80 if two else 160) * 1024, (name, row)
+    assert one == 3
