@@ -149,11 +149,13 @@ WeightsPlan plan_key_weights(const lra_shape* sh, const lra_cache* c, const lra_
   pl.off_qt = 0;
   const int64_t G = sh->n_q_heads / sh->n_kv_heads;
   const int64_t places = b->n_queries * G / 128 + c->n_seqs;
-  // statistics: workgroups of (kv head, 128 rows, share), three to a compute unit, each with two 64-key tiles at least; at most
-  // 32 shares, which the pass over them reads
+  // statistics: workgroups of (kv head, 128 rows, share), three to a compute unit (two by registers at d = 128 and ranks above 32: planned as
+  // three, 16 sequences of 4 agents took 455 us against 441, 100 rows of 18 k tokens 157 against 148), each with two 64-key tiles at least;
+  // at most 32 shares, which the pass over them reads
   const int64_t q_tiles = std::max<int64_t>((b->n_queries * G + 127) / 128, std::min(c->n_seqs, b->n_queries));
   const int64_t tiles = (std::min<int64_t>(c->max_seq_len, keys_per_row(c, b) + (b->causal ? std::min<int64_t>(b->max_queries_per_seq, 128 / G + 1) : 1)) + 63) / 64 + 1;
-  const int64_t shares = std::max<int64_t>(1, std::min<int64_t>({3 * kCUs / (q_tiles * sh->n_kv_heads), (tiles + 1) / 2, 32}));
+  const int64_t per_unit = sh->head_dim == 128 && sh->rank > 32 ? 2 : 3;
+  const int64_t shares = std::max<int64_t>(1, std::min<int64_t>({per_unit * kCUs / (q_tiles * sh->n_kv_heads), (tiles + 1) / 2, 32}));
   if (sh->dtype == LRA_BF16 && sh->rank % 8 == 0 && c->l_adapter_stride == 0 && tune.variant != 1 && mfma_fits(sh, c) &&
       places * shares * sh->n_kv_heads < (int64_t{1} << 24)) {
     pl.mfma = true;

@@ -18,3 +18,11 @@ extern "C" void batch_plan_query(const lra_shape* sh, const lra_cache* c, const 
 extern "C" int32_t batch_workspace_query(const lra_shape* sh, const lra_cache* c, const lra_batch* b, const lra_tuning* tuning) {
   return static_cast<int32_t>(lra::batch_workspace_bytes(sh, c, b, lra::resolve_tuning(tuning)) >> 8);
 }
+
+extern "C" void weights_plan_query(const lra_shape* sh, const lra_cache* c, const lra_batch* b, const lra_tuning* tuning, int32_t* out) {
+  const lra::WeightsPlan pl = lra::plan_key_weights(sh, c, b, lra::resolve_tuning(tuning));
+  out[0] = pl.mfma;
+  out[1] = pl.n_splits;
+  out[2] = pl.tile_places;
+  out[3] = pl.sum_groups;
+}

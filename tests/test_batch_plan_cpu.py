@@ -88,3 +88,17 @@ def test_a_rotated_key_side_at_high_ranks_has_one_workgroup_per_compute_unit(pla
             for causal in (False, True):
                 pl = plan(planner, *llama, 64, n, queries, theta=500000.0, causal=causal)
                 assert 1 <= pl["n_splits"] <= 64 and (pl["n_splits"] == 1 or pl["n_splits"] <= (n + queries + 127) // 64)
+
+
+def weights_plan(planner, *call, **kw):
+    out = (ctypes.c_int32 * 4)()
+    planner.weights_plan_query(*(ctypes.byref(x) for x in structs(*call, **kw)), out)
+    return dict(zip(("mfma", "n_splits", "tile_places", "sum_groups"), out))
+
+
+def test_weights_statistics_fill_the_places_that_there_are(planner):
+    """Three workgroups per compute unit, two at d = 128 and ranks above 32 (tests/test_batch_resources_cpu.py)."""
+    assert weights_plan(planner, 32, 8, 128, 32, 18432, 100, causal=True)["n_splits"] == 768 // (4 * 8)
+    assert weights_plan(planner, 32, 8, 128, 64, 18432, 100, causal=True)["n_splits"] == 512 // (4 * 8)
+    assert weights_plan(planner, 8, 8, 64, 64, 18432, 400, causal=True)["n_splits"] == 768 // (4 * 8)
+    assert weights_plan(planner, 32, 8, 128, 64, 8192, 4)["n_splits"] == 32

@@ -26,3 +26,14 @@ def test_tile_walking_kernel_two_workgroups_per_compute_unit(table):  # noqa: F8
         one += not two
         assert row[SCRATCH] == 0 and row[OCC] >= (2 if two else 1) and row[LDS] <= (80 if two else 160) * 1024, (name, row)
     assert one == 3
+
+
+def test_key_weights_kernels(table):  # noqa: F811
+    """Statistics: three workgroups of four waves per compute unit, two at d = 128 and ranks above 32; sums: two."""
+    for name, row in rows_of(table, "weights_stats_mfma_kernel").items():
+        d, rp = _args(name)[:2]
+        per_unit = 2 if (d, rp) == (128, 64) else 3
+        assert row[SCRATCH] == 0 and row[OCC] >= per_unit and row[LDS] * per_unit <= 160 * 1024, (name, row)
+    for kernel in ("weights_sum_mfma_kernel", "weights_sum_rows_kernel"):
+        for name, row in rows_of(table, kernel).items():
+            assert row[SCRATCH] == 0 and row[OCC] >= 2 and row[LDS] <= 80 * 1024, (name, row)
