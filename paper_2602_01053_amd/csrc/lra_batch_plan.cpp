@@ -157,7 +157,7 @@ WeightsPlan plan_key_weights(const lra_shape* sh, const lra_cache* c, const lra_
   const int64_t per_unit = sh->head_dim == 128 && sh->rank > 32 ? 2 : 3;
   const int64_t shares = std::max<int64_t>(1, std::min<int64_t>({per_unit * kCUs / (q_tiles * sh->n_kv_heads), (tiles + 1) / 2, 32}));
   if (sh->dtype == LRA_BF16 && sh->rank % 8 == 0 && c->l_adapter_stride == 0 && tune.variant != 1 && mfma_fits(sh, c) &&
-      places * shares * sh->n_kv_heads < (int64_t{1} << 24)) {
+      places * shares * sh->n_kv_heads < (int64_t{1} << 24) && (b->n_queries * G + 63) / 64 < (int64_t{1} << 24)) {  // (weights_lse_kernel's)
     pl.mfma = true;
     pl.n_splits = static_cast<int>(shares);
     pl.tile_places = static_cast<int>(places);

@@ -102,3 +102,11 @@ def test_weights_statistics_fill_the_places_that_there_are(planner):
     assert weights_plan(planner, 32, 8, 128, 64, 18432, 100, causal=True)["n_splits"] == 512 // (4 * 8)
     assert weights_plan(planner, 8, 8, 64, 64, 18432, 400, causal=True)["n_splits"] == 768 // (4 * 8)
     assert weights_plan(planner, 32, 8, 128, 64, 8192, 4)["n_splits"] == 32
+
+
+def test_the_largest_batch_of_weights_fits_the_grids(planner):
+    """2^30 query rows: a grid dimension holds fewer than 2^32 threads, four to a row in the pass over the statistics."""
+    fits = lambda q: (q * 16 + 63) // 64 * 256 < 1 << 32  # noqa: E731
+    for queries in ((1 << 26) - 4, (1 << 26) - 3, 1 << 26):
+        assert fits(queries) == (queries == (1 << 26) - 4)
+        assert weights_plan(planner, 16, 1, 64, 8, 1000, queries, causal=True)["mfma"] == fits(queries)
