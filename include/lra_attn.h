@@ -359,6 +359,9 @@ lra_status lra_attn_prefill(const lra_shape* shape, const lra_cache* cache,
  * rope_theta > 0 rotates the keys by the rotary position embedding in its rotate-half form
  * (pair (i, i + d/2) of the token at position j by the angle j * rope_theta^(-2i/d)) before
  * they are cached - the cached keys are the rotated ones (App. D.1); 0 stores them unrotated.
+ * Position is the token's index in the cache.  After an eviction (lra_cache_gather) the kept keys have the
+ * angles of their first positions and a new token's index is less than its position: append with rope_theta 0
+ * then, and turn the new rows of K_base by their positions before they are attended to.
  */
 typedef struct {
   const void* w;
@@ -502,7 +505,7 @@ lra_status lra_evict_select(const lra_cache* cache, const float* weights, int64_
  *                          src and dst
  * More than 65535 sequences or a max_seq_len of dst beyond 2^27 are LRA_ERR_UNSUPPORTED, and so is key_rope_theta > 0:
  * K_base may hold rotated keys (they keep the angles of their first positions), but an adapter's part that is rotated by
- * the token's index would turn with the move.
+ * the token's index would turn with the move.  Tokens appended behind the kept ones: see lra_projection's rope_theta.
  */
 lra_status lra_cache_gather(const lra_shape* shape, const lra_cache* src, int32_t n_adapters, const int32_t* kept,
                             int64_t kept_stride, const lra_cache* dst, const float* weights, int64_t weights_stride,
