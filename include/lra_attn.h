@@ -96,10 +96,12 @@ typedef struct {
                          The value side is unchanged.  bf16 with rank % 8 == 0 runs on MFMA
                          kernels (decode and prefills of a few tokens: the split-KV kernel
                          rotates L B_K per key tile in registers, once for every agent of the
-                         tile; other prefills complete each key tile in LDS), everything else
-                         on the vector-ALU kernels.  Those other prefills hold the completed
-                         keys as fp16 (a second rounding to bf16 would cost more accuracy than
-                         the rest of the call): key magnitudes must stay below 65504 there. */
+                         tile; other prefills, and every lra_attn_batch, decode steps too,
+                         complete each key tile in LDS), everything else on the vector-ALU
+                         kernels.  What completes tiles in LDS holds the completed keys, and Q
+                         beside them, as fp16 (a second rounding to bf16 would cost more accuracy
+                         than the rest of the call): their magnitudes must stay below 65504 there,
+                         and those of Q lose bits below 6.1e-5. */
 } lra_shape;
 
 /*
@@ -434,7 +436,9 @@ typedef struct {
 /*
  * Attention of such a batch, with the scores, adapters, rotary key side and caches of lra_attn_decode and
  * lra_attn_prefill: decode steps of several agents behind a window, chunks of new tokens of many sequences over
- * one paged cache, or both kinds in one call (causal, chunks of one token).  In lra_cache, seq_lens[t] may be 0
+ * one paged cache, or both kinds in one call (causal, chunks of one token).  With a rotated key side (a b_k and
+ * key_rope_theta > 0) keys and queries pass through fp16, see lra_shape, and every query of a decode step reads
+ * and completes the keys anew; lra_attn_decode does so once for all agents.  In lra_cache, seq_lens[t] may be 0
  * for a sequence without queries or whose queries see nothing, and seq_lens_host is not used.
  *
  *   q    DEVICE [n_queries][Hq][d]        out  DEVICE [n_queries][Hq][d]

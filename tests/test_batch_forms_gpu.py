@@ -3,8 +3,8 @@ import pytest
 import torch
 
 import paper_2602_01053_amd as lra
-from tests.batch_reference import BatchCase, Device, make
-from tests.test_batch_gpu import check
+from tests.batch_reference import BatchCase, Device, attention, make
+from tests.test_batch_gpu import TOL, check
 
 pytestmark = pytest.mark.gpu
 
@@ -30,3 +30,17 @@ def test_rotated_key_sides_of_all_ranks(paged, counts, causal, window, heads, ra
     lens = [1900, 75, 800]
     n = 3 if paged else 1
     check(BatchCase(lens[:n], counts[:n], causal, window, 5 if window else 0, heads, rank, BF16, paged=paged, rope=10000.0, seed=22))
+
+
+@pytest.mark.parametrize("counts,causal", [([3], False), ([60], True)])
+def test_rotated_key_sides_up_to_the_magnitudes_told(counts, causal):
+    """Completed keys are held as fp16: magnitudes of 2^15, within the 65504 of the header, with queries that keep the scores at a few units.
+    The keys' rounding (2^-11) adds 1e-3 to the error at most: scores of size 4 with 0.4 2^-11 in each."""
+    c = BatchCase([300], counts, causal, 0, 0, (8, 2, 128), 16, BF16, rope=10000.0, seed=23, poison=False)
+    x = make(c)
+    x.k.clamp_(-4, 4).mul_(2 ** 13)
+    x.q.mul_(2 ** -11)
+    got = Device(x, lra).attend().double().cpu()
+    ref = attention(x)
+    assert torch.isfinite(got).all()
+    assert float((got - ref).norm() / ref.norm()) <= TOL[BF16]
