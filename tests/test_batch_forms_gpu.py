@@ -3,8 +3,10 @@ import pytest
 import torch
 
 import paper_2602_01053_amd as lra
-from tests.batch_reference import BatchCase, Device, attention, make
+from tests.batch_reference import BatchCase, Device, attention, key_weights, make
 from tests.test_batch_gpu import TOL, check
+from tests.test_key_weights_gpu import TOL as WEIGHTS_TOL
+from tests.test_key_weights_gpu import run as weigh
 
 pytestmark = pytest.mark.gpu
 
@@ -44,3 +46,50 @@ def test_rotated_key_sides_up_to_the_magnitudes_told(counts, causal):
     ref = attention(x)
     assert torch.isfinite(got).all()
     assert float((got - ref).norm() / ref.norm()) <= TOL[BF16]
+
+
+@pytest.mark.parametrize("counts,causal,variant", [([3, 1], False, 0), ([3, 1], False, 2), ([3, 2], True, 0), ([90, 7], True, 2)])
+@pytest.mark.parametrize("heads,rank", [((8, 2, 64), 16), ((8, 2, 128), 64)])
+def test_share_counts_change_only_rounding(heads, rank, counts, causal, variant):
+    """Shares of a row go by the bound of the lengths: the same sequences under larger and larger ones, on the few-rows kernel and the
+    tile-walking one, with shares of several tiles, of one and of none."""
+    c = BatchCase([2000, 77], counts, causal, 0, 0, heads, rank, BF16, seed=24)
+    x = make(c)
+    ref, ref_w = attention(x), key_weights(x)
+    old = lra.lra_set_kernel_variant(variant)
+    sizes, sizes_w = [], []
+    try:
+        for bound in (2000, 3500, 12000, 60000):
+            d = Device(x, lra, max_seq_len=bound)
+            sizes.append(lra.lra_batch_workspace_bytes(d.shape, d.cache, d.batch))
+            sizes_w.append(lra.lra_key_weights_workspace_bytes(d.shape, d.cache, d.batch))
+            got = d.attend().double().cpu()
+            assert float((got - ref).norm() / ref.norm()) <= TOL[BF16], bound
+            w = weigh(d, 0.0, torch.zeros(2, bound, device="cuda")).double().cpu()[:, :2000]
+            assert float((w - ref_w).norm() / ref_w.norm()) <= WEIGHTS_TOL, bound
+    finally:
+        lra.lra_set_kernel_variant(old)
+    assert len(set(sizes)) >= 2 and sizes == sorted(sizes), sizes            # (at most 64 shares)
+    assert len(set(sizes_w)) >= 2, sizes_w    # (at most 32; the sums of groups of heads, which go by the bound too, get fewer)
+
+
+def test_shares_of_the_vector_kernels_change_only_rounding():
+    """decode_split_keys reaches the vector-ALU kernels, so a bf16 call has to ask for them."""
+    c = BatchCase([2000, 77], [3, 1], False, 0, 0, (8, 2, 64), 16, BF16, seed=25)
+    x = make(c)
+    ref = attention(x)
+    sizes = set()
+    old = lra.lra_set_kernel_variant(1)
+    try:
+        for keys in (64, 320, 4096):
+            before = lra.lra_set_decode_split_keys(keys)
+            try:
+                d = Device(x, lra)
+                sizes.add(lra.lra_batch_workspace_bytes(d.shape, d.cache, d.batch))
+                got = d.attend().double().cpu()
+            finally:
+                lra.lra_set_decode_split_keys(before)
+            assert float((got - ref).norm() / ref.norm()) <= TOL[BF16], keys
+    finally:
+        lra.lra_set_kernel_variant(old)
+    assert len(sizes) == 3
