@@ -422,6 +422,8 @@ size_t lra_append_workspace_bytes(const lra_shape* shape, const lra_cache* cache
  * Rows that no query of the call sees are not read: they may hold anything, NaN included, and block-table
  * entries of blocks that hold no visible token may be out of range (pages behind the window can be given back).
  * Rows that some queries of a sequence see and others do not must be finite (a weight of zero times NaN is NaN).
+ * Scores, scaled, are below 7e8 in magnitude, or far below that on the negative side (a key that is to get no weight may
+ * give minus infinity or come from the type's lowest value): those count as minus infinity.
  */
 typedef struct {
   const int32_t* seq_query_start; /* DEVICE int32 [n_seqs+1], non-decreasing, [0] = 0, [n_seqs] = n_queries */

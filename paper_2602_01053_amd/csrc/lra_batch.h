@@ -101,6 +101,10 @@ __device__ __forceinline__ bool batch_sees(const BatchParams& p, int pos, int j)
   return j <= pos && (p.window == 0 || j > pos - p.window || j < p.sinks);
 }
 
+// A tile's largest score in base-2 units; one below -2^30 (a mask of the type's lowest value) counts as minus infinity: as a reference, its
+// rounding alone would be more than exp2 of the differences to it can hold.
+__device__ __forceinline__ float tile_reference(float mx) { return mx < -0x1p30f ? -INFINITY : mx; }
+
 // Parameters of a call out of the ABI's structs (pointers of the workspace and of the outputs left NULL).
 BatchParams batch_params(const lra_shape* sh, const lra_cache* c, const lra_adapters* ad, const lra_batch* b, const void* q);
 

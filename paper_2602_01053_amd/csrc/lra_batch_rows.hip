@@ -259,7 +259,7 @@ __global__ __launch_bounds__(256, 2) void batch_rows_kernel(BatchParams p) {
     float mx = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[i]);
-    mx = fmaxf(mx, pf_partner32(mx)) * sc;
+    mx = tile_reference(fmaxf(mx, pf_partner32(mx)) * sc);
     if (__builtin_amdgcn_ballot_w64(mx > m_run) != 0) {
       const float m_new = fmaxf(m_run, mx);
       const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);

@@ -628,7 +628,7 @@ __device__ __forceinline__ void batch_tiles_body(const BatchParams p) {
     for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[kt][i]);
-    mx = fmaxf(mx, pf_partner32(mx)) * sc;
+    mx = tile_reference(fmaxf(mx, pf_partner32(mx)) * sc);
     if (__builtin_amdgcn_ballot_w64(mx > m_run + kSlack) != 0) {  // always on the first tile (m_run = -inf)
       const float m_new = fmaxf(m_run, mx);
       // (a row may have seen nothing yet)

@@ -276,7 +276,7 @@ __global__ __launch_bounds__(256, 2) void weights_stats_mfma_kernel(WeightsParam
     for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[kt][i]);
-    const float m_new = fmaxf(m, mx * sc);
+    const float m_new = fmaxf(m, tile_reference(mx * sc));
     const float nm = m_new == -INFINITY ? 0.f : -m_new;
     float sum = l * __builtin_amdgcn_exp2f(m + nm);
 #pragma unroll

@@ -93,3 +93,27 @@ def test_shares_of_the_vector_kernels_change_only_rounding():
     finally:
         lra.lra_set_kernel_variant(old)
     assert len(sizes) == 3
+
+
+@pytest.mark.parametrize("value", [-float("inf"), "lowest", -1e30, -1e12])
+@pytest.mark.parametrize("counts,causal", [([3], False), ([90], True)])
+@pytest.mark.parametrize("variant", [0, 1, 2])
+@pytest.mark.parametrize("dtype,d,rank", [(F32, 64, 8), (BF16, 64, 16), (BF16, 128, 64), (BF16, 128, 12)])
+def test_keys_of_no_weight(dtype, d, rank, variant, counts, causal, value):
+    """Keys that nothing is to attend to, by one member of the type's lowest value or a very negative one: first tiles of a row, whole
+    shares and a stretch in the middle hold no others."""
+    c = BatchCase([900], counts, causal, 0, 0, (4, 2, d), rank, dtype, key_side=False, seed=26)
+    x = make(c)
+    x.q.abs_().clamp_(min=0.5)
+    for lo, hi in ((0, 400), (600, 637)):
+        x.k[0, lo:hi, :, 5] = torch.finfo(dtype).min if value == "lowest" else value
+    old = lra.lra_set_kernel_variant(variant)
+    try:
+        dev = Device(x, lra)
+        got = dev.attend().double().cpu()
+        w = weigh(dev, 0.0, torch.empty(1, 900, device="cuda")).double().cpu()
+    finally:
+        lra.lra_set_kernel_variant(old)
+    ref, ref_w = attention(x), key_weights(x)
+    assert float((got - ref).norm() / ref.norm()) <= TOL[dtype]
+    assert (w[0, :400] == 0).all() and float((w - ref_w).norm() / ref_w.norm()) <= WEIGHTS_TOL
