@@ -423,7 +423,8 @@ size_t lra_append_workspace_bytes(const lra_shape* shape, const lra_cache* cache
  * entries of blocks that hold no visible token may be out of range (pages behind the window can be given back).
  * Rows that some queries of a sequence see and others do not must be finite (a weight of zero times NaN is NaN).
  * Scores, scaled, are below 7e8 in magnitude, or far below that on the negative side (a key that is to get no weight may
- * give minus infinity or come from the type's lowest value): those count as minus infinity.
+ * give minus infinity or come from the type's lowest value): those get no weight beside others.  A query that sees
+ * no others has no softmax: lra_attn_batch gives no number for it, lra_key_weights adds nothing.
  */
 typedef struct {
   const int32_t* seq_query_start; /* DEVICE int32 [n_seqs+1], non-decreasing, [0] = 0, [n_seqs] = n_queries */
@@ -461,9 +462,9 @@ size_t lra_batch_workspace_bytes(const lra_shape* shape, const lra_cache* cache,
  * cache that may not grow goes by when it lets tokens go.  For j < seq_lens[t]
  *     weights[t][j] = decay * weights[t][j] + sum over the queries of sequence t and the Hq heads of P[j],
  * P the softmax of the query's scores (as lra_attn_batch has them: same mask, scale and key-side adapters; zero where
- * the query does not see j; a query whose every visible score is minus infinity adds nothing).  One sum per token and not per head: the L row of a token serves every head and every
- * agent, so a token leaves the cache for all of them or for none.  For a prompt, the queries may be its last few
- * tokens only (causal): the batch need not hold every new token.
+ * the query does not see j, or sees only keys that get no weight).  One sum per token and not per head: the L row of a
+ * token serves every head and every agent, so a token leaves the cache for all of them or for none.  For a prompt, the
+ * queries may be its last few tokens only (causal): the batch need not hold every new token.
  *
  *   adapters   b_v is not used
  *   decay      finite; 0: the old values are not read, so they may hold anything

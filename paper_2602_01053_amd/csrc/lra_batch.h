@@ -101,7 +101,7 @@ __device__ __forceinline__ bool batch_sees(const BatchParams& p, int pos, int j)
   return j <= pos && (p.window == 0 || j > pos - p.window || j < p.sinks);
 }
 
-// A tile's largest score in base-2 units; one below -2^30 (a mask of the type's lowest value) counts as minus infinity: as a reference, its
+// A tile's (or a lane's) largest score in base-2 units; one below -2^30 (a mask of the type's lowest value) counts as minus infinity: as a reference, its
 // rounding alone would be more than exp2 of the differences to it can hold.
 __device__ __forceinline__ float tile_reference(float mx) { return mx < -0x1p30f ? -INFINITY : mx; }
 

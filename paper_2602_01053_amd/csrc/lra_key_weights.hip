@@ -126,7 +126,7 @@ __global__ __launch_bounds__(256) void weights_stats_kernel(WeightsParams p, int
     for (int k = static_cast<int>(static_cast<int64_t>(b.n_keys) * split / p.n_splits) + (tid & ~63); k < k1; k += 256) {
       float s = score<T, D>(p, b.t, h, b.adapter, q, qt, [&](int i) { return k + i >= k1 ? -1 : (k + i < b.n_sinks ? k + i : k + i + b.gap); });
       if (k + own >= k1) s = -INFINITY;
-      if (s == -INFINITY) continue;
+      if (tile_reference(s) == -INFINITY) continue;
       const float m_new = fmaxf(m, s);
       l = l * exp2f(m - m_new) + exp2f(s - m_new);
       m = m_new;

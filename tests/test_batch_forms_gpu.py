@@ -117,3 +117,22 @@ def test_keys_of_no_weight(dtype, d, rank, variant, counts, causal, value):
     ref, ref_w = attention(x), key_weights(x)
     assert float((got - ref).norm() / ref.norm()) <= TOL[dtype]
     assert (w[0, :400] == 0).all() and float((w - ref_w).norm() / ref_w.norm()) <= WEIGHTS_TOL
+
+
+@pytest.mark.parametrize("value", [-float("inf"), -1e30, "lowest"])
+@pytest.mark.parametrize("counts,causal", [([3], False), ([90], True)])
+@pytest.mark.parametrize("variant", [0, 1])
+@pytest.mark.parametrize("dtype,rank", [(F32, 8), (BF16, 16), (BF16, 12)])
+def test_rows_without_a_softmax_add_nothing(dtype, rank, variant, counts, causal, value):
+    c = BatchCase([300], counts, causal, 0, 0, (4, 2, 64), rank, dtype, key_side=False, seed=27)
+    x = make(c)
+    x.q.abs_().clamp_(min=0.5)
+    x.k[0, :, 0, 5] = torch.finfo(dtype).min if value == "lowest" else value   # one of two kv heads
+    old = lra.lra_set_kernel_variant(variant)
+    try:
+        w = weigh(Device(x, lra), 0.0, torch.empty(1, 300, device="cuda")).double().cpu()
+    finally:
+        lra.lra_set_kernel_variant(old)
+    x.k, x.q, x.case = x.k[:, :, 1:], x.q[:, 2:], BatchCase(**{**c.__dict__, "heads": (2, 1, 64)})  # the other head alone
+    ref = key_weights(x)
+    assert float((w - ref).norm() / ref.norm()) <= WEIGHTS_TOL
