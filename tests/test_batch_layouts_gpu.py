@@ -157,3 +157,24 @@ def test_contiguous_buffers_with_room_behind_the_sequence(counts, causal, window
             assert (w[:, n:] == 7).all() and float((w[:, :n].double() - ref).norm()) <= WEIGHTS_TOL * float(ref.norm())
     finally:
         lra.lra_set_kernel_variant(old)
+
+
+@pytest.mark.parametrize("rank,d,rope", [(16, 128, 0.0), (64, 64, 0.0), (32, 128, 10000.0)])
+@pytest.mark.parametrize("counts,causal", [([4, 1, 0, 3], False), ([40, 1, 0, 150], True)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (300, 0), (1999, 70), (300, 1100), (64, 1024), (1500, 1025)])
+def test_tile_walking_over_groups_of_pages(window, sinks, counts, causal, rank, d, rope):
+    """Block ids come 64 at a time, 1024 tokens: sinks that end in, at and behind such a group, windows that begin in a later one, shares
+    that begin anywhere."""
+    c = BatchCase([5000, 37, 900, 2311], counts, causal, window, sinks, (8, 2, d), rank, BF16, rope=rope, seed=81)
+    x = make(c)
+    ref = attention(x)
+    old = lra.lra_set_kernel_variant(2)
+    try:
+        got = Device(x, lra).attend().double().cpu()
+    finally:
+        lra.lra_set_kernel_variant(old)
+    assert torch.isfinite(got).all() and float((got - ref).norm() / ref.norm()) <= TOL[BF16]
+    if not rope:
+        ref = key_weights(x)
+        got = weigh(Device(x, lra), 0.0, torch.zeros(4, 5000, device="cuda")).double().cpu()
+        assert float((got - ref).norm() / ref.norm()) <= WEIGHTS_TOL
