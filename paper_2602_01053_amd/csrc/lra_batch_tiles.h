@@ -336,7 +336,6 @@ __device__ __forceinline__ void batch_tiles_body(const BatchParams p) {
     if (wave < E_WAVES) {
       const int64_t ldb = static_cast<int64_t>(Hkv) * D;
       const bf16_t* bkg = static_cast<const bf16_t*>(p.b_k) + static_cast<int64_t>(a_idx) * r * ldb + hk * D;
-      const bool has_b = p.b_k != nullptr;  // (a decode call may come without key-side adapters: nothing to add)
 #pragma unroll
       for (int sel = 0; sel < 2; ++sel)
 #pragma unroll
@@ -349,7 +348,7 @@ __device__ __forceinline__ void batch_tiles_body(const BatchParams p) {
             for (int x = 0; x < 2; ++x) {
               const int e = 2 * e2 + x;
               const int rho = 16 * ks + 8 * (e >> 2) + 4 * g2 + (e & 3);
-              const uint32_t v = (has_b && rho < r) ? bkg[rho * ldb + 32 * (sel == 0 ? fb_lo : fb_hi) + l32] : 0u;
+              const uint32_t v = rho < r ? bkg[rho * ldb + 32 * (sel == 0 ? fb_lo : fb_hi) + l32] : 0u;
               pair |= v << (16 * x);
             }
             w4[e2] = pair;
