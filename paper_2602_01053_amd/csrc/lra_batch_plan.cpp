@@ -51,13 +51,17 @@ static void place_states(BatchPlan& pl, const lra_shape* sh) {
   pl.bytes = pl.off_adapter + aligned(static_cast<size_t>(pl.rows) * sizeof(int32_t));
 }
 
-// Key shares where a compute unit holds one workgroup (batch_tiles_kernel with a rotated key side at d = 128 and ranks above 32: 416
-// registers): those with the shortest sum of turns, up to four of the chip, a turn being its key tiles and what a prologue takes, five
-// tiles' time.  (Planned as two to a unit: 333 new tokens of 28 heads behind a window of 1000, rank 64, 90 us against 77; 4 agents on 16 k
-// tokens 119 against 107.  One turn always: 300 new tokens after 30 k in 3 shares 489 against 434 in 7.)
-static int64_t shares_by_turns(int64_t units, int64_t key_tiles) {
+// Key shares where a compute unit holds one workgroup (batch_tiles_kernel with a rotated key side at d = 128 and ranks above 32: some 420
+// registers).  Units of about equal length: those with the shortest sum of turns, up to four of the chip, a turn being its key tiles and
+// what a prologue takes, five tiles' time.  Sequences of any lengths: four turns' worth, so that the short ones' places go on to others,
+// though beyond one turn's no share of less than ten tiles.
+// (Planned as two workgroups to a unit, one turn: 333 new tokens of 28 heads behind a window of 1000, rank 64, 90 us against 77; 4 agents on
+// 16 k tokens 119 against 107; 8 sequences of 1 k to 9 k, 4 agents, 446 against 366.  By turns whatever the lengths: the last 506.)
+static int64_t shares_by_turns(int64_t units, int64_t key_tiles, bool ragged) {
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>((key_tiles + 1) / 2, 64));
+  if (ragged) return std::max<int64_t>(1, std::min<int64_t>(std::max<int64_t>(std::min<int64_t>(4 * kCUs / units, key_tiles / 10), kCUs / units), most));
   int64_t best = 1, least = INT64_MAX;
-  for (int64_t s = 1; s <= std::min<int64_t>((key_tiles + 1) / 2, 64) && (s == 1 || units * s <= 4 * kCUs); ++s) {
+  for (int64_t s = 1; s <= most && (s == 1 || units * s <= 4 * kCUs); ++s) {
     const int64_t time = (units * s + kCUs - 1) / kCUs * ((key_tiles + s - 1) / s + 5);
     if (time < least) {
       least = time;
@@ -81,7 +85,9 @@ static bool plan_tiles(BatchPlan& pl, const lra_shape* sh, const lra_cache* c, c
   const int64_t key_tiles = (std::min<int64_t>(c->max_seq_len, keys_per_row(c, b) + chunk) + 63) / 64 + (b->window > 0 ? 2 : 0);
   const int64_t units = q_tiles * sh->n_kv_heads;
   const bool one_per_unit = rotary && sh->head_dim == 128 && sh->rank > 32;
-  const int64_t shares = one_per_unit ? shares_by_turns(units, key_tiles)
+  // (a window of half the longest sequence or less: most see all of it)
+  const bool ragged = c->n_seqs > 1 && 2 * keys_per_row(c, b) > c->max_seq_len;
+  const int64_t shares = one_per_unit ? shares_by_turns(units, key_tiles, ragged)
                                       : std::max<int64_t>(1, std::min<int64_t>({2 * kCUs / units, (key_tiles + 1) / 2, 64}));
   pl.tiles = true;
   pl.tile_places = static_cast<int>(places);

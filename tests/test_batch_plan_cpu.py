@@ -82,7 +82,9 @@ def test_a_rotated_key_side_at_high_ranks_has_one_workgroup_per_compute_unit(pla
     assert workgroups(llama, 64, 16000, 4) == 256 and workgroups(llama, 32, 16000, 4) == 512
     assert workgroups(llama, 64, 16000, 128, causal=True) == 256
     assert workgroups(qwen, 40, 30000, 300, causal=True) == 476            # two turns: one of 204 would leave fifty units without work
-    assert workgroups(llama, 64, 9000, 3, seqs=8) == 768                   # three full turns, not one of 192
+    assert workgroups(llama, 64, 9000, 3, seqs=8) == 960                   # lengths that may differ: about four turns, not one of 192
+    assert workgroups(llama, 64, 9000, 3, seqs=8, window=4000) == 768      # ... and hardly matter behind a window: three full ones
+    assert workgroups(llama, 64, 5000, 20, seqs=4, causal=True) == 32 * 8  # one turn, more would have shares of a few tiles
     for n in (1, 64, 129, 1000, 100000):
         for queries in (1, 5, 60, 900):
             for causal in (False, True):
