@@ -17,13 +17,15 @@ from .build import LIB_PATH, PYCALL_PATH
 
 LRA_OK = 0
 LRA_BF16, LRA_F32 = 0, 1
+LRA_E4M3, LRA_INT8 = 0, 1
 
 STATIC_WORKSPACE_BYTES = 64 << 20   # LRA_STATIC_WORKSPACE_BYTES of the header
 
 EXPORTS = ("lra_workspace_bytes", "lra_attn_decode", "lra_attn_decode_static", "lra_attn_prefill", "lra_status_string",
            "lra_cache_append", "lra_append_workspace_bytes", "lra_probe_stream_read", "lra_probe_mfma_bf16",
            "lra_attn_batch", "lra_batch_workspace_bytes", "lra_key_weights", "lra_key_weights_workspace_bytes",
-           "lra_evict_select", "lra_cache_gather")
+           "lra_evict_select", "lra_cache_gather", "lra_cache8_append", "lra_cache8_gather", "lra_attn_batch8",
+           "lra_batch8_workspace_bytes", "lra_quantize_rows", "lra_matmul_i8", "lra_matmul_i8_workspace_bytes")
 
 
 class LraShape(ctypes.Structure):
@@ -55,6 +57,27 @@ class LraBatch(ctypes.Structure):
     _fields_ = [("seq_query_start", ctypes.c_void_p), ("query_adapter", ctypes.c_void_p), ("n_queries", ctypes.c_int32),
                 ("max_queries_per_seq", ctypes.c_int32), ("causal", ctypes.c_int32), ("window", ctypes.c_int32),
                 ("sinks", ctypes.c_int32)]
+
+
+class LraCache8(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("l", ctypes.c_void_p), ("kv_block_stride", ctypes.c_int64), ("kv_head_stride", ctypes.c_int64),
+                ("scale_block_stride", ctypes.c_int64), ("l_row_stride", ctypes.c_int64), ("code", ctypes.c_int32),
+                ("max_blocks_per_seq", ctypes.c_int32), ("num_blocks", ctypes.c_int32), ("n_seqs", ctypes.c_int32),
+                ("block_table", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p), ("max_seq_len", ctypes.c_int32)]
+
+
+class LraNewRows(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("l", ctypes.c_void_p), ("k_token_stride", ctypes.c_int64),
+                ("v_token_stride", ctypes.c_int64), ("l_token_stride", ctypes.c_int64), ("seq_start", ctypes.c_void_p),
+                ("positions", ctypes.c_void_p), ("n_new", ctypes.c_int32), ("max_new_per_seq", ctypes.c_int32),
+                ("rope_theta", ctypes.c_float)]
+
+
+class LraI8Operands(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("w", ctypes.c_void_p), ("x_scale", ctypes.c_void_p), ("w_scale", ctypes.c_void_p),
+                ("x_stride", ctypes.c_int64), ("w_stride", ctypes.c_int64), ("m", ctypes.c_int32), ("n", ctypes.c_int32),
+                ("k", ctypes.c_int32)]
 
 
 class LraTuning(ctypes.Structure):
@@ -167,6 +190,21 @@ def load_library() -> ctypes.CDLL:
     lib.lra_evict_select.argtypes = [cp, vp, i64, i32, i32, i32, vp, i64, vp, vp]
     lib.lra_cache_gather.restype = ctypes.c_int
     lib.lra_cache_gather.argtypes = [sp, cp, i32, vp, i64, cp, vp, i64, vp, i64, vp]
+    c8 = ctypes.POINTER(LraCache8)
+    lib.lra_cache8_append.restype = ctypes.c_int
+    lib.lra_cache8_append.argtypes = [sp, c8, ctypes.POINTER(LraNewRows), vp]
+    lib.lra_cache8_gather.restype = ctypes.c_int
+    lib.lra_cache8_gather.argtypes = [sp, c8, vp, i64, cp, vp]
+    lib.lra_attn_batch8.restype = ctypes.c_int
+    lib.lra_attn_batch8.argtypes = [sp, c8, ap, bp, vp, vp, vp, ctypes.c_size_t, tp, vp]
+    lib.lra_batch8_workspace_bytes.restype = ctypes.c_size_t
+    lib.lra_batch8_workspace_bytes.argtypes = [sp, c8, bp, tp]
+    lib.lra_quantize_rows.restype = ctypes.c_int
+    lib.lra_quantize_rows.argtypes = [vp, i32, i64, i32, i32, vp, i64, vp, vp]
+    lib.lra_matmul_i8.restype = ctypes.c_int
+    lib.lra_matmul_i8.argtypes = [ctypes.POINTER(LraI8Operands), vp, i32, i64, vp, ctypes.c_size_t, vp]
+    lib.lra_matmul_i8_workspace_bytes.restype = ctypes.c_size_t
+    lib.lra_matmul_i8_workspace_bytes.argtypes = [i32, i32, i32, i32]
     lib.lra_probe_stream_read.restype = ctypes.c_int
     lib.lra_probe_stream_read.argtypes = [vp, ctypes.c_size_t, vp, vp]
     lib.lra_probe_mfma_bf16.restype = ctypes.c_int
@@ -506,3 +544,134 @@ def lra_cache_gather(shape: LraShape, cache: LraCache, kept: torch.Tensor, dst: 
     _check(load_library().lra_cache_gather(ctypes.byref(shape), ctypes.byref(cache), int(n_adapters), _ptr(kept), _row_stride(kept),
                                            ctypes.byref(dst), _ptr(weights), 0 if weights is None else _row_stride(weights),
                                            _ptr(dst_weights), 0 if weights is None else _row_stride(dst_weights), _stream_ptr(stream)))
+
+
+# ---- the layer path in 8 bits (lra_attn8.h) ----
+def _dense_i32(name: str, t: torch.Tensor, n: int) -> None:
+    if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.numel() != n:
+        raise LraError(2, f"{name} must be a dense int32 vector of {n}")
+
+
+def make_cache8(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, l: torch.Tensor, seq_lens: torch.Tensor,
+                max_seq_len: int, block_table: Optional[torch.Tensor] = None) -> LraCache8:
+    """Describe a cache of 8-bit codes held in torch tensors.
+
+    k [num_blocks][Hkv][16][d], v [num_blocks][Hkv][d][16] (by dimension), both float8_e4m3fn or both int8, the blocks and
+    heads at any strides, the same for both; k_scale, v_scale uint8 [num_blocks][Hkv], exponents with bias 127; l
+    [num_blocks][16][r] in the type of the queries.  block_table int32 [n_seqs][max_blocks], or None for one sequence whose
+    blocks lie in order."""
+    codes = {torch.float8_e4m3fn: LRA_E4M3, torch.int8: LRA_INT8}
+    if k.dtype not in codes or v.dtype != k.dtype:
+        raise LraError(3, f"codes must be float8_e4m3fn or int8, got {k.dtype} and {v.dtype}")
+    blocks, heads, _, d = k.shape
+    if tuple(k.shape) != (blocks, heads, 16, d) or tuple(v.shape) != (blocks, heads, d, 16):
+        raise LraError(2, "k must be [num_blocks][Hkv][16][d] and v [num_blocks][Hkv][d][16]")
+    if k.stride(3) != 1 or k.stride(2) != d or v.stride(3) != 1 or v.stride(2) != 16:
+        raise LraError(2, "a block's codes of one head must be dense")
+    block_stride, head_stride = (k.stride(i) if k.size(i) > 1 else max(k.stride(i), 16 * d) for i in (0, 1))
+    if any(k.size(i) > 1 and v.stride(i) != k.stride(i) for i in (0, 1)):
+        raise LraError(2, "k and v must share the strides of blocks and heads")
+    for s in (k_scale, v_scale):
+        if s.dtype != torch.uint8 or tuple(s.shape) != (blocks, heads) or (heads > 1 and s.stride(1) != 1) or s.stride(0) != k_scale.stride(0):
+            raise LraError(2, f"scales must be uint8 [{blocks}][{heads}], unit stride on the heads, one stride on the blocks")
+    if l.dim() != 3 or l.shape[:2] != (blocks, 16) or l.stride(-1) != 1 or l.stride(0) != 16 * l.stride(1):
+        raise LraError(2, "l must be [num_blocks][16][r] with the rows one row stride apart")
+    n_seqs = 1 if block_table is None else block_table.size(0)
+    if block_table is not None and (block_table.dtype != torch.int32 or block_table.dim() != 2 or not block_table.is_contiguous()):
+        raise LraError(2, "block_table must be a dense int32 [n_seqs][max_blocks]")
+    _dense_i32("seq_lens", seq_lens, n_seqs)
+    cache = LraCache8(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(l), block_stride, head_stride,
+                      k_scale.stride(0) if blocks > 1 else heads, l.stride(1), codes[k.dtype],
+                      0 if block_table is None else block_table.size(1), blocks, n_seqs, _ptr(block_table), _ptr(seq_lens), int(max_seq_len))
+    cache._tensors = (k, v, k_scale, v_scale, l, block_table, seq_lens)  # the struct holds raw pointers into them
+    cache._sizes = (heads, d, l.size(2), _dtype_code(l))
+    return cache
+
+
+def _check_cache8(shape: LraShape, cache: LraCache8) -> None:
+    if cache._sizes != (shape.n_kv_heads, shape.head_dim, shape.rank, shape.dtype):
+        raise LraError(2, "the cache's kv heads, head dimension, rank and type of l must be those of the shape")
+
+
+def lra_cache8_append(shape: LraShape, cache: LraCache8, seq_start: torch.Tensor, max_new_per_seq: int, k: torch.Tensor, v: torch.Tensor,
+                      l: Optional[torch.Tensor], rope_theta: float = 0.0, positions: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Write the new rows (the last tokens of every sequence, which seq_lens counts already) into the cache: keys rotated by
+    their positions if rope_theta > 0, keys and values quantized.  k, v: [n_new][Hkv][d] with dense rows, l: [n_new][r]; the
+    tokens may be strided, as the columns of one projection are.  seq_start: int32 [n_seqs+1]."""
+    _check_cache8(shape, cache)
+    n_new = k.size(0)
+    for t in (k, v):
+        if tuple(t.shape) != (n_new, shape.n_kv_heads, shape.head_dim) or not t[:1].is_contiguous() or _dtype_code(t) != shape.dtype:
+            raise LraError(2, f"k and v must be [{n_new}][{shape.n_kv_heads}][{shape.head_dim}] of the shape's dtype, dense but for the tokens")
+    if l is not None and (tuple(l.shape) != (n_new, shape.rank) or l.stride(1) != 1 or _dtype_code(l) != shape.dtype):
+        raise LraError(2, f"l must be [{n_new}][{shape.rank}] of the shape's dtype, unit stride on the rank")
+    _dense_i32("seq_start", seq_start, cache.n_seqs + 1)
+    if positions is not None:
+        _dense_i32("positions", positions, n_new)
+    stride = lambda t: t.stride(0) if n_new > 1 else t[0].numel()  # noqa: E731
+    rows = LraNewRows(_ptr(k), _ptr(v), _ptr(l), stride(k), stride(v), 0 if l is None else stride(l), _ptr(seq_start), _ptr(positions), n_new,
+                      int(max_new_per_seq), float(rope_theta))
+    _check(load_library().lra_cache8_append(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(rows), _stream_ptr(stream)))
+
+
+def lra_cache8_gather(shape: LraShape, cache: LraCache8, dst: LraCache, kept: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Row i of sequence t of the cache dst (make_cache) becomes the values of row kept[t][i] of `cache`, for i below dst's
+    lengths; without `kept` its last rows."""
+    _check_cache8(shape, cache)
+    if kept is not None:
+        _check_kept(dst, kept, dst.max_seq_len)
+    _check(load_library().lra_cache8_gather(ctypes.byref(shape), ctypes.byref(cache), _ptr(kept), 0 if kept is None else _row_stride(kept),
+                                            ctypes.byref(dst), _stream_ptr(stream)))
+
+
+def lra_batch8_workspace_bytes(shape: LraShape, cache: LraCache8, batch: LraBatch) -> int:
+    n = load_library().lra_batch8_workspace_bytes(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(batch), _tuning_ref)
+    if n == ctypes.c_size_t(-1).value:
+        raise LraError(2, "lra_batch8_workspace_bytes rejected the arguments")
+    return int(n)
+
+
+def lra_attn_batch8(shape: LraShape, cache: LraCache8, b_k: Optional[torch.Tensor], b_v: Optional[torch.Tensor], n_adapters: int,
+                    batch: LraBatch, q: torch.Tensor, out: torch.Tensor, workspace: Optional[torch.Tensor], stream=None) -> None:
+    """lra_attn_batch over a cache of 8-bit codes.  q, out: [n_queries][Hq][d]."""
+    _check_rows(batch, shape, q, out)
+    _check_cache8(shape, cache)
+    ad = LraAdapters(_ptr(b_k), _ptr(b_v), int(n_adapters))
+    _check(load_library().lra_attn_batch8(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(ad), ctypes.byref(batch), _ptr(q), _ptr(out),
+                                          *_workspace_args(workspace), _tuning_ref, _stream_ptr(stream)))
+
+
+def _check_codes(name: str, codes: torch.Tensor, scales: torch.Tensor) -> None:
+    if codes.dtype != torch.int8 or codes.dim() != 2 or codes.stride(1) != 1:
+        raise LraError(2, f"{name} must be int8 [rows][cols], unit stride on the columns")
+    if scales.dtype != torch.float32 or tuple(scales.shape) != (codes.size(0),) or not scales.is_contiguous():
+        raise LraError(2, f"the scales of {name} must be a dense float32 vector of {codes.size(0)}")
+
+
+def lra_quantize_rows(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, stream=None) -> None:
+    """Rows of x (bf16 or fp32) as 8-bit integers with a scale each: codes int8 of x's shape, scales float32 [rows]."""
+    _check_codes("codes", codes, scales)
+    if x.shape != codes.shape or x.stride(1) != 1:
+        raise LraError(2, "x must have the codes' shape and unit stride on the columns")
+    _check(load_library().lra_quantize_rows(_ptr(x), _dtype_code(x), _row_stride(x), x.size(0), x.size(1), _ptr(codes), _row_stride(codes),
+                                            _ptr(scales), _stream_ptr(stream)))
+
+
+def lra_matmul_i8_workspace_bytes(m: int, n: int, k: int, dtype: torch.dtype = torch.bfloat16) -> int:
+    size = load_library().lra_matmul_i8_workspace_bytes(int(m), int(n), int(k), _dtype_code(torch.empty(0, dtype=dtype)))
+    if size == ctypes.c_size_t(-1).value:
+        raise LraError(2, "lra_matmul_i8_workspace_bytes rejected the sizes")
+    return int(size)
+
+
+def lra_matmul_i8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, y: torch.Tensor,
+                  workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """y [m][n] (bf16 or fp32) = x_scale[i] w_scale[j] (x w^T)[i][j] for codes x int8 [m][k] and weights w int8 [n][k].
+    `workspace` (optional, lra_matmul_i8_workspace_bytes bytes) lets few tokens divide k over the chip."""
+    _check_codes("x", x, x_scale)
+    _check_codes("w", w, w_scale)
+    if x.size(1) != w.size(1) or tuple(y.shape) != (x.size(0), w.size(0)) or y.stride(1) != 1:
+        raise LraError(2, "x [m][k], w [n][k] and y [m][n] must agree, y with unit stride on the features")
+    ops = LraI8Operands(_ptr(x), _ptr(w), _ptr(x_scale), _ptr(w_scale), _row_stride(x), _row_stride(w), x.size(0), w.size(0), x.size(1))
+    _check(load_library().lra_matmul_i8(ctypes.byref(ops), _ptr(y), _dtype_code(y), _row_stride(y), *_workspace_args(workspace),
+                                        _stream_ptr(stream)))

@@ -1,0 +1,105 @@
+#include "lra_attn8_plan.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace lra {
+
+// What holds of a shape for every call, checked as for a paged cache of 16-bit rows.
+static lra_status check_shape8(const lra_shape* sh) {
+  if (sh->dtype != LRA_BF16 && sh->dtype != LRA_F32) return LRA_ERR_DTYPE;
+  if (sh->n_q_heads < 1 || sh->n_kv_heads < 1 || sh->head_dim < 1 || sh->rank < 1) return LRA_ERR_SHAPE;
+  if (sh->n_q_heads % sh->n_kv_heads) return LRA_ERR_SHAPE;
+  if (!(sh->scale >= 0.f) || std::isinf(sh->scale)) return LRA_ERR_SHAPE;
+  if (!(sh->key_rope_theta >= 0.f) || std::isinf(sh->key_rope_theta)) return LRA_ERR_SHAPE;
+  if (sh->head_dim != 64 && sh->head_dim != 128) return LRA_ERR_UNSUPPORTED;
+  if (sh->rank > 64 || sh->n_q_heads / sh->n_kv_heads > 16 || sh->n_q_heads > 4096) return LRA_ERR_UNSUPPORTED;
+  return LRA_OK;
+}
+
+lra_status check_cache8(const lra_shape* sh, const lra_cache8* c) {
+  if (!sh || !c) return LRA_ERR_NULL;
+  const lra_status st = check_shape8(sh);
+  if (st != LRA_OK) return st;
+  if (c->code != LRA_E4M3 && c->code != LRA_INT8) return LRA_ERR_DTYPE;
+  if (!c->k || !c->v || !c->k_scale || !c->v_scale || !c->l || !c->seq_lens) return LRA_ERR_NULL;
+  if (c->n_seqs < 1 || c->max_seq_len < 1 || c->num_blocks < 1) return LRA_ERR_SHAPE;
+  if (c->n_seqs > (1 << 20) || c->max_seq_len > (1 << 30)) return LRA_ERR_UNSUPPORTED;
+  const int64_t room = c->block_table ? c->max_blocks_per_seq : c->num_blocks;
+  if (room < 1 || room * 16 < c->max_seq_len) return LRA_ERR_SHAPE;
+  if (!c->block_table && c->n_seqs != 1) return LRA_ERR_SHAPE;
+  if (c->kv_head_stride < 16 * sh->head_dim || c->kv_block_stride < 16 * sh->head_dim) return LRA_ERR_SHAPE;
+  if ((c->kv_head_stride | c->kv_block_stride) & 15) return LRA_ERR_SHAPE;
+  if (c->kv_head_stride > (int64_t{1} << 40) || c->kv_block_stride > (int64_t{1} << 40) || c->num_blocks > (int64_t{1} << 60) / c->kv_block_stride)
+    return LRA_ERR_UNSUPPORTED;
+  if (c->scale_block_stride != 0 && c->scale_block_stride < sh->n_kv_heads) return LRA_ERR_SHAPE;
+  if (c->scale_block_stride > (int64_t{1} << 31)) return LRA_ERR_UNSUPPORTED;
+  if (c->l_row_stride < 0 || (c->l_row_stride != 0 && c->l_row_stride < sh->rank)) return LRA_ERR_SHAPE;
+  if (c->l_row_stride != sh->rank && (c->l_row_stride & 7)) return LRA_ERR_SHAPE;
+  if (c->l_row_stride > (int64_t{1} << 31) || (c->l_row_stride ? c->l_row_stride : sh->rank) > (int64_t{1} << 56) / c->num_blocks)
+    return LRA_ERR_UNSUPPORTED;
+  if ((reinterpret_cast<uintptr_t>(c->k) | reinterpret_cast<uintptr_t>(c->v) | reinterpret_cast<uintptr_t>(c->l)) & 15) return LRA_ERR_SHAPE;
+  return LRA_OK;
+}
+
+lra_status check_batch8(const lra_shape* sh, const lra_cache8* c, const lra_batch* b) {
+  const lra_status st = check_cache8(sh, c);
+  if (st != LRA_OK) return st;
+  if (!b || !b->seq_query_start || !b->query_adapter) return LRA_ERR_NULL;
+  if (b->n_queries < 1 || b->max_queries_per_seq < 1 || b->max_queries_per_seq > b->n_queries) return LRA_ERR_SHAPE;
+  if (b->window < 0 || b->sinks < 0) return LRA_ERR_SHAPE;
+  if (static_cast<int64_t>(b->n_queries) * sh->n_q_heads > (int64_t{1} << 30)) return LRA_ERR_UNSUPPORTED;
+  return LRA_OK;
+}
+
+lra_status check_new_rows(const lra_shape* sh, const lra_cache8* c, const lra_new_rows* n) {
+  const lra_status st = check_cache8(sh, c);
+  if (st != LRA_OK) return st;
+  if (!n || !n->k || !n->v || !n->seq_start) return LRA_ERR_NULL;
+  if (n->n_new < 1 || n->max_new_per_seq < 1 || n->max_new_per_seq > n->n_new) return LRA_ERR_SHAPE;
+  if (!(n->rope_theta >= 0.f) || std::isinf(n->rope_theta)) return LRA_ERR_SHAPE;
+  const int64_t row = static_cast<int64_t>(sh->n_kv_heads) * sh->head_dim, es = sh->dtype == LRA_BF16 ? 2 : 4;
+  if (n->k_token_stride < row || n->v_token_stride < row || (n->l && n->l_token_stride < sh->rank)) return LRA_ERR_SHAPE;
+  if (n->k_token_stride > (int64_t{1} << 31) || n->v_token_stride > (int64_t{1} << 31) || n->l_token_stride > (int64_t{1} << 31))
+    return LRA_ERR_UNSUPPORTED;
+  if (((n->k_token_stride | n->v_token_stride) * es) & 15) return LRA_ERR_SHAPE;
+  if ((reinterpret_cast<uintptr_t>(n->k) | reinterpret_cast<uintptr_t>(n->v)) & 15) return LRA_ERR_SHAPE;
+  if (reinterpret_cast<uintptr_t>(n->l) & static_cast<uintptr_t>(es - 1)) return LRA_ERR_SHAPE;
+  return LRA_OK;
+}
+
+static size_t aligned(size_t bytes) { return (bytes + 255) & ~static_cast<size_t>(255); }
+
+static void place_states(Attn8Plan& pl, const lra_shape* sh) {
+  // (the merge kernels: 128 to 1024 threads per row where there are more than 65535 queries)
+  if (pl.rows / sh->n_q_heads > 65535 && static_cast<int64_t>(pl.rows) * (pl.n_splits <= 8 ? 128 : 1024) >= (int64_t{1} << 32)) {
+    pl.launchable = false;
+    return;
+  }
+  const size_t states = static_cast<size_t>(pl.rows) * static_cast<size_t>(pl.n_splits);
+  pl.states = true;
+  pl.off_ml = 0;
+  pl.off_o = aligned(states * 2 * sizeof(float));
+  pl.off_lr = pl.off_o + aligned(states * sh->head_dim * sizeof(float));
+  pl.off_adapter = pl.off_lr + aligned(states * sh->rank * sizeof(float));
+  pl.bytes = pl.off_adapter + aligned(static_cast<size_t>(pl.rows) * sizeof(int32_t));
+}
+
+// The most keys that one query sees.
+static int64_t keys_per_row(const lra_cache8* c, const lra_batch* b) {
+  return b->window > 0 ? std::min<int64_t>(c->max_seq_len, static_cast<int64_t>(b->window) + b->sinks) : c->max_seq_len;
+}
+
+Attn8Plan plan_attn8(const lra_shape* sh, const lra_cache8* c, const lra_batch* b, const Tuning& tune) {
+  Attn8Plan pl{};
+  const int64_t rows = static_cast<int64_t>(b->n_queries) * sh->n_q_heads, keys = keys_per_row(c, b);
+  pl.rows = static_cast<int>(rows);
+  pl.launchable = true;
+  // vector-ALU kernel: one workgroup per row and share, three to a compute unit; a share of 256 keys at least
+  pl.n_splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({3 * kCUs / rows, (keys + 255) / 256, 64})));
+  pl.launchable = rows < (int64_t{1} << 24);  // (a grid dimension holds fewer than 2^32 threads)
+  if (pl.launchable) place_states(pl, sh);
+  return pl;
+}
+
+}  // namespace lra

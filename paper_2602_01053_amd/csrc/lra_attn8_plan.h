@@ -1,0 +1,21 @@
+// Host-side argument checks and launch planning of the 8-bit calls (lra_attn8.h); plain C++ like lra_plan.h.
+#pragma once
+
+#include "lra_attn8.h"
+#include "lra_plan.h"
+
+namespace lra {
+
+lra_status check_cache8(const lra_shape* sh, const lra_cache8* c);
+lra_status check_batch8(const lra_shape* sh, const lra_cache8* c, const lra_batch* b);
+lra_status check_new_rows(const lra_shape* sh, const lra_cache8* c, const lra_new_rows* n);
+
+struct Attn8Plan {
+  bool launchable;
+  bool few_rows, tiles, states;
+  int rows, n_splits, row_tiles, tile_places;
+  size_t off_ml, off_o, off_lr, off_adapter, bytes;
+};
+Attn8Plan plan_attn8(const lra_shape* sh, const lra_cache8* c, const lra_batch* b, const Tuning& tune);
+
+}  // namespace lra

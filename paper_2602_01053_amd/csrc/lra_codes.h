@@ -1,0 +1,62 @@
+// Caches of 8-bit codes (lra_attn8.h): kernel parameters, codes and their scales.
+#pragma once
+
+#include "lra_attn8.h"
+#include "lra_batch.h"
+#include "lra_prefill_util.h"
+
+namespace lra {
+
+// k_base, v_base: codes; kv_block_stride, kv_head_stride: bytes
+struct Batch8Params : BatchParams {
+  const uint8_t *k_scale, *v_scale;
+  int64_t scale_block_stride;
+  int32_t code;
+};
+
+// Block b of sequence t.
+__device__ __forceinline__ int block8(const int32_t* table, int max_blocks_per_seq, int t, int b) {
+  return table ? table[static_cast<int64_t>(t) * max_blocks_per_seq + b] : b;
+}
+
+// 2^(s - 127); 255 is not a number, 0 the denormal 2^-127
+__device__ __forceinline__ float scale8(int s) {
+  return s == 255 ? __uint_as_float(0x7fc00000u) : (s == 0 ? __uint_as_float(0x00400000u) : __uint_as_float(static_cast<uint32_t>(s) << 23));
+}
+
+// Exponent byte of the least power of two (2^-126 at least) that brings a value with these bits (sign cleared) to 448 = 1.75 x 2^8
+// or 127 = 1.984375 x 2^6 at most: one more than the value's own exponent less 8 or 6 where its mantissa is larger than theirs.
+template <int CODE>
+__device__ __forceinline__ int least_scale8(uint32_t bits) {
+  if (bits >= 0x7f800000u) return 255;
+  const int e = CODE == LRA_E4M3 ? static_cast<int>((bits + 0x1fffffu) >> 23) - 8 : static_cast<int>((bits + 0x01ffffu) >> 23) - 6;
+  return max(e, 1);
+}
+
+// The four codes of a word as floats.
+template <int CODE>
+__device__ __forceinline__ void decode4(uint32_t w, float (&x)[4]) {
+  if constexpr (CODE == LRA_E4M3) {
+    const pf_f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(w), false), b = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(w), true);
+    x[0] = a[0], x[1] = a[1], x[2] = b[0], x[3] = b[1];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = static_cast<float>(static_cast<signed char>(w >> (8 * i)));
+  }
+}
+
+// Four scaled values (at most 448 or 127 in magnitude) rounded to codes, to nearest, ties to even.
+template <int CODE>
+__device__ __forceinline__ uint32_t encode4(const float (&x)[4]) {
+  if constexpr (CODE == LRA_E4M3) {
+    int r = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
+    return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], r, true));
+  } else {
+    uint32_t r = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r |= (static_cast<uint32_t>(static_cast<int>(rintf(x[i]))) & 255u) << (8 * i);
+    return r;
+  }
+}
+
+}  // namespace lra

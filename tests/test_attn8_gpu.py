@@ -1,0 +1,175 @@
+"""Attention of a batch over 8-bit codes (lra_attn_batch8) against float64 on the values that the codes stand for."""
+import pytest
+import torch
+
+import paper_2602_01053_amd as lra
+from tests.attn8_reference import Case8, Device8, attention_with_bound, close_enough, make8
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+
+CASES = [
+    Case8([1], [1]),
+    Case8([1], [1], code="int8", dtype=F32, rank=1),
+    Case8([17], [3], dtype=F32, rank=5, code="e4m3", heads=(3, 3, 64)),
+    Case8([700], [2], window=256, sinks=4, dtype=F32, code="int8", heads=(4, 4, 64)),
+    Case8([15, 16, 17, 63, 64, 65], [1, 2, 3, 1, 2, 3], code="int8"),
+    Case8([700, 33, 250], [4, 4, 4], heads=(8, 2, 128), rank=16),
+    Case8([700, 33, 250], [4, 1, 3], heads=(28, 4, 128), rank=32, code="int8"),
+    Case8([1300], [4], heads=(16, 1, 128), rank=64),
+    Case8([1300], [4], heads=(16, 1, 64), rank=24, code="int8"),
+    Case8([900], [8], heads=(4, 4, 128), rank=12),                         # a rank of the vector kernel
+    Case8([300, 0, 5], [2, 1, 0], key_side=False),
+    Case8([300, 77], [2, 3], value_side=False, code="int8", heads=(8, 2, 128)),
+    Case8([300, 77], [2, 3], key_side=False, value_side=False, heads=(8, 2, 128), rank=16),
+    # chunks: longer than a tile, of one token, longer than their sequence, none
+    Case8([400, 129, 64, 9, 31], [150, 1, 64, 12, 0], causal=True, heads=(8, 2, 128), rank=16),
+    Case8([400, 129, 64, 9, 31], [150, 1, 64, 12, 0], causal=True, heads=(8, 2, 64), rank=8, code="int8"),
+    Case8([333], [333], causal=True, heads=(7, 1, 128), rank=32, code="int8"),
+    Case8([600, 450], [70, 200], causal=True, heads=(4, 1, 128), rank=64),
+    Case8([260], [200], causal=True, heads=(3, 3, 64), rank=48, key_side=False),
+    Case8([100, 40], [20, 30], causal=True, dtype=F32, rank=12, code="int8"),
+    # windows, with sinks that end inside a block, beside the window, or none
+    Case8([1000, 90], [4, 2], window=100, sinks=5, heads=(8, 2, 128), rank=16),
+    Case8([1000, 700], [4, 4], window=1, sinks=0, heads=(8, 2, 128), rank=16, code="int8"),
+    Case8([1000, 700], [4, 4], window=17, sinks=70, heads=(4, 2, 64)),
+    Case8([900, 500], [150, 40], causal=True, window=130, sinks=4, heads=(8, 2, 128), rank=16),
+    Case8([900, 500], [150, 40], causal=True, window=33, sinks=0, heads=(4, 2, 64), rank=16, code="int8"),
+    Case8([900], [60], causal=True, window=64, sinks=900, heads=(4, 2, 64), dtype=F32, rank=8),
+    # layouts
+    Case8([500], [4], table=False, heads=(8, 2, 128), rank=16),
+    Case8([500, 90, 33], [2, 2, 2], layout="pool", heads=(8, 2, 128), rank=16, code="int8"),
+    Case8([500, 90], [100, 20], causal=True, layout="pool", heads=(8, 2, 64), rank=24),
+    Case8([200], [3], table=False, layout="pool", dtype=F32, rank=10, code="int8"),
+    Case8([350], [2], scale=0.02, heads=(8, 2, 128), rank=16),
+]
+
+
+@pytest.mark.parametrize("c", CASES, ids=lambda c: c.label())
+def test_against_float64(c):
+    x = make8(c)
+    want, bound = attention_with_bound(x)
+    dev = Device8(x, lra)
+    got = dev.attend()
+    close_enough(got, want, bound, c.label())
+    assert torch.equal(got, dev.attend())          # equal arguments, equal bits
+
+
+@pytest.mark.parametrize("variant", [1, 2])
+@pytest.mark.parametrize("c", [Case8([700, 33], [4, 2], heads=(8, 2, 128), rank=16),
+                               Case8([400, 129, 9], [150, 1, 12], causal=True, window=90, sinks=3, heads=(8, 2, 64), rank=24, code="int8")],
+                         ids=lambda c: c.label())
+def test_kernel_variants(c, variant):
+    x = make8(c)
+    want, bound = attention_with_bound(x)
+    old = lra.lra_set_kernel_variant(variant)
+    try:
+        got = Device8(x, lra).attend()
+    finally:
+        lra.lra_set_kernel_variant(old)
+    close_enough(got, want, bound, c.label())
+
+
+def test_longer_bound_than_lengths():
+    c = Case8([200, 7], [3, 3], heads=(8, 2, 128), rank=16)
+    x = make8(c)
+    want, bound = attention_with_bound(x)
+    close_enough(Device8(x, lra, max_seq_len=5000).attend(), want, bound)
+
+
+def test_lengths_beyond_the_bound_end_there():
+    """A device-side length beyond max_seq_len is treated as max_seq_len."""
+    c = Case8([200, 90], [2, 2], heads=(8, 2, 128), rank=16)
+    x = make8(c)
+    want, bound = attention_with_bound(x)
+    dev = Device8(x, lra)
+    dev.lens[0] = 4000
+    close_enough(dev.attend(), want, bound)
+
+
+def test_scales_at_their_ends():
+    """Exponent bytes of the smallest and of large values; a block whose keys have the scale 255 (not a number) gives NaN."""
+    c = Case8([64], [2], heads=(4, 2, 64), rank=8, key_side=False, poison=False)
+    x = make8(c)
+    kc, ks, vc, vs = x.codes
+    vs[0, 0], vs[0, 1], vs[0, 2] = 1, 190, 120
+    ks[0, 3] = 1
+    from tests.attn8_reference import values_of
+    x.v = values_of(vc, vs[..., None, None]).transpose(2, 3).reshape(1, -1, 2, 64)
+    x.k = values_of(kc, ks[..., None, None]).transpose(2, 3).reshape(1, -1, 2, 64)
+    want, bound = attention_with_bound(x)
+    dev = Device8(x, lra)
+    close_enough(dev.attend(), want, bound)
+    dev.k_scale[:] = 255
+    assert bool(torch.isnan(dev.attend()).all())
+
+
+@pytest.mark.parametrize("causal", [False, True])
+def test_pool_beyond_32_bit_offsets(causal):
+    """Blocks some 6 GB apart."""
+    c = Case8([150, 40], [4, 30] if causal else [4, 2], causal=causal, heads=(8, 2, 128), rank=16, poison=False)
+    x = make8(c)
+    want, bound = attention_with_bound(x)
+    dev = Device8(x, lra, spare=0)
+    nb, hkv, _, d = dev.k.shape
+    far = (6 << 30) // nb // 16 * 16
+    pool = torch.empty(2, nb * far, dtype=torch.uint8, device="cuda")
+    k = pool[0].as_strided((nb, hkv, 16, d), (far, 16 * d, d, 1))
+    v = pool[1].as_strided((nb, hkv, d, 16), (far, 16 * d, 16, 1))
+    k.copy_(dev.k.view(torch.uint8))
+    v.copy_(dev.v.view(torch.uint8))
+    dev.k, dev.v = k.view(torch.float8_e4m3fn), v.view(torch.float8_e4m3fn)
+    dev.cache = lra.make_cache8(dev.k, dev.v, dev.k_scale, dev.v_scale, dev.l, dev.lens, max(c.lens), dev.table)
+    close_enough(dev.attend(), want, bound)
+
+
+def test_graph_replays_with_other_lengths_and_inputs():
+    c = Case8([300, 120], [4, 4], heads=(8, 2, 128), rank=16, poison=False)
+    x = make8(c)
+    dev = Device8(x, lra)
+    ws, out = dev.workspace(), torch.empty_like(dev.q)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        dev.call(out, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        dev.call(out, ws)
+    for lens in ([300, 120], [17, 100], [1, 0], [256, 64], [300, 120]):
+        dev.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        dev.q.add_(0.125)
+        out.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = torch.empty_like(out)
+        dev.call(want, dev.workspace())
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), lens
+        assert bool(torch.isfinite(out).all())
+
+
+def test_two_calls_at_once_on_two_streams():
+    a, b = (Device8(make8(Case8([900, 300], [4, 4], heads=(8, 2, 128), rank=16, seed=s)), lra) for s in (1, 2))
+    alone = [a.attend(), b.attend()]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs, spaces = [torch.empty_like(a.q), torch.empty_like(b.q)], [a.workspace(), b.workspace()]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for dev, s, out, ws in zip((a, b), streams, outs, spaces):
+            dev.call(out, ws, stream=s)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], alone[0]) and torch.equal(outs[1], alone[1])
+
+
+def test_output_and_workspace_ends_are_respected():
+    c = Case8([500, 33], [3, 5], heads=(8, 2, 128), rank=16)
+    dev = Device8(make8(c), lra)
+    want = dev.attend()
+    n = lra.lra_batch8_workspace_bytes(dev.shape, dev.cache, dev.batch)
+    ws = torch.full((n + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+    buf = torch.full((dev.q.numel() + 512,), -7.0, dtype=dev.q.dtype, device="cuda")
+    out = buf[256:256 + dev.q.numel()].view(dev.q.shape)
+    dev.call(out, ws[:n])
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+    assert bool((buf[:256] == -7).all()) and bool((buf[256 + dev.q.numel():] == -7).all()) and bool((ws[n:] == 0xA5).all())

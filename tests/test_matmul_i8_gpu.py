@@ -1,0 +1,127 @@
+"""Quantized rows and products of 8-bit integers against exact integers."""
+import pytest
+import torch
+
+import paper_2602_01053_amd as lra
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def strided(rows, cols, pad, dtype, fill=0):
+    return torch.full((rows, cols + pad), fill, dtype=dtype, device="cuda")[:, :cols]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,cols", [(1, 16), (3, 256), (5, 4096), (2, 4112), (17, 3584), (2, 20000), (300, 512), (1, 1 << 17)])
+def test_quantize_rows(dtype, rows, cols):
+    g = torch.Generator().manual_seed(rows * cols)
+    x = (torch.randn(rows, cols, generator=g) * 10.0 ** torch.randint(-8, 8, (rows, 1), generator=g)).to(dtype)
+    x[0, cols // 2:] = 0
+    src, codes, scales = strided(rows, cols, 32, dtype, 9), strided(rows, cols, 16, torch.int8, 77), torch.full((rows + 1,), -1.0, device="cuda")
+    src.copy_(x)
+    lra.lra_quantize_rows(src, codes, scales[:rows])
+    torch.cuda.synchronize()
+    got, s = codes.cpu().double(), scales.cpu().double()
+    top = x.double().abs().amax(1)
+    # a division's rounding, half a step of fp32
+    assert bool(((s[:rows] - top / 127).abs() <= 2.0 ** -24 * top / 127).all()) and s[rows] == -1
+    # a quotient and a product rounded in fp32, 2^-23 of at most 127, before the code's own half step
+    assert bool(((got - x.double() * 127 / top[:, None]).abs() <= 0.5 + 127 * 2.0 ** -23).all())
+    assert int(got.abs().max()) == 127
+
+
+def test_quantize_rows_of_zeros_and_of_no_numbers():
+    x = torch.randn(6, 64, generator=torch.Generator().manual_seed(1)).clamp(-3, 3).cuda()  # (times 1e38: within fp32)
+    x[1] = 0
+    x[2, 7] = float("nan")
+    x[3, 9] = -float("inf")
+    x[4] = 1e-41
+    x[5] *= 1e38
+    codes, scales = torch.full((6, 64), 55, dtype=torch.int8, device="cuda"), torch.empty(6, device="cuda")
+    lra.lra_quantize_rows(x, codes, scales)
+    torch.cuda.synchronize()
+    assert scales[1] == 0 and bool((codes[1] == 0).all()) and bool(torch.isnan(scales[2:4]).all()) and bool(torch.isfinite(scales[4:]).all())
+    assert int(codes[0].abs().max()) == 127 and int(codes[5].abs().max()) == 127
+    y = torch.empty(6, 64, device="cuda")
+    lra.lra_matmul_i8(codes, scales, torch.eye(64, dtype=torch.int8, device="cuda"), torch.ones(64, device="cuda"), y)
+    torch.cuda.synchronize()
+    assert bool(torch.isnan(y[2:4]).all()) and bool((y[1] == 0).all()) and bool(torch.isfinite(y[[0, 1, 4, 5]]).all())
+
+
+def operands(m, n, k, seed=0, pad=16):
+    g = torch.Generator().manual_seed(seed + m + 7 * n + 13 * k)
+    x = torch.randint(-128, 128, (m, k), generator=g, dtype=torch.int64)
+    w = torch.randint(-128, 128, (n, k), generator=g, dtype=torch.int64)
+    x[0], w[0] = -128, -128                       # the largest sum
+    sx, sw = torch.rand(m, generator=g) + 0.01, torch.rand(n, generator=g) * 0.01 + 1e-4
+    dx, dw = strided(m, k, pad, torch.int8, 99), strided(n, k, pad, torch.int8, 99)
+    dx.copy_(x.to(torch.int8))
+    dw.copy_(w.to(torch.int8))
+    want = (x.double() @ w.double().t()) * sx.double()[:, None] * sw.double()
+    return (dx, sx.cuda(), dw, sw.cuda()), want
+
+
+SIZES = [(1, 1, 16), (1, 2064, 4096), (4, 100, 48), (3, 17, 80), (16, 64, 64), (17, 65, 144), (33, 130, 512), (64, 1056, 3584), (65, 257, 1040),
+         (100, 2064, 4096), (128, 128, 128), (129, 300, 2000), (333, 1056, 3584), (600, 520, 272), (1025, 2064, 1040), (2048, 700, 64), (5, 5000, 96),
+         (300, 33, 16384), (7, 9, (1 << 17) - 16)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("m,n,k", SIZES)
+def test_matmul_i8(dtype, m, n, k):
+    ops, want = operands(m, n, k)
+    size = lra.lra_matmul_i8_workspace_bytes(m, n, k, dtype)
+    # (16-bit words of a NaN in the workspace; rows of y wider than n)
+    ws = torch.full((size + 256,), 255, dtype=torch.uint8, device="cuda")
+    outs = []
+    for workspace in (ws[:size] if size else None, None):
+        buf = torch.full((m + 2, n + 3), -3.0, dtype=dtype, device="cuda")
+        y = buf.flatten()[:(m + 1) * (n + 3)].view(m + 1, n + 3)[:m, :n]
+        lra.lra_matmul_i8(*ops, y, workspace)
+        torch.cuda.synchronize()
+        assert bool((buf[:m, n:] == -3).all()) and bool((buf[m:] == -3).all())
+        outs.append(y.clone())
+    assert torch.equal(*outs) and bool((ws[size:] == 255).all())
+    # the sum's rounding to fp32, two products, and the output's own
+    steps = 3 * 2.0 ** -24 + (2.0 ** -8 if dtype == BF16 else 0)
+    assert bool(((outs[0].cpu().double() - want).abs() <= want.abs() * steps * (1 + 2.0 ** -8)).all())
+
+
+def test_matmul_i8_rows_beyond_32_bit_offsets():
+    """Token rows 2^27 bytes apart, output rows 2^26 elements."""
+    m, n, k = 40, 96, 256
+    (x, sx, w, sw), want = operands(m, n, k, pad=0)
+    far = torch.empty(m * (1 << 27), dtype=torch.int8, device="cuda").as_strided((m, k), (1 << 27, 1))
+    far.copy_(x)
+    y = torch.empty(m * (1 << 26), dtype=F32, device="cuda").as_strided((m, n), (1 << 26, 1))
+    lra.lra_matmul_i8(far, sx, w, sw, y)
+    torch.cuda.synchronize()
+    assert bool(((y.cpu().double() - want).abs() <= want.abs() * 3.1 * 2.0 ** -24).all())
+
+
+def test_matmul_i8_in_a_graph_and_on_two_streams():
+    (x, sx, w, sw), want = operands(4, 2064, 4096)
+    make = lambda: (torch.empty(4, 2064, device="cuda"), torch.empty(max(lra.lra_matmul_i8_workspace_bytes(4, 2064, 4096, F32), 256), dtype=torch.uint8, device="cuda"))  # noqa: E731
+    (y, ws), (y2, ws2) = make(), make()
+    lra.lra_matmul_i8(x, sx, w, sw, y, ws)
+    torch.cuda.synchronize()
+    first = y.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lra.lra_matmul_i8(x, sx, w, sw, y, ws)
+    for i in range(4):
+        y.zero_()
+        x.neg_()                                   # (-128 wraps onto itself: row 0's sums stay those of a minimum)
+        graph.replay()
+        torch.cuda.synchronize()
+        lra.lra_matmul_i8(x, sx, w, sw, y2, ws2)
+        torch.cuda.synchronize()
+        assert torch.equal(y, y2), i
+    assert torch.equal(y, first)
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(5):
+        lra.lra_matmul_i8(x, sx, w, sw, y, ws, stream=a)
+        lra.lra_matmul_i8(x, sx, w, sw, y2, ws2, stream=b)
+    torch.cuda.synchronize()
+    assert torch.equal(y, first) and torch.equal(y2, first)
