@@ -248,7 +248,11 @@ lra_status lra_attn_batch8(const lra_shape* shape, const lra_cache8* cache, cons
   }
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bool bf16 = shape->dtype == LRA_BF16;
-  if (launch_attn8_vector(p, bf16, pl.rows, s) != hipSuccess) return LRA_ERR_HIP;
+  if (pl.few_rows) {
+    if ((p.code == LRA_E4M3 ? launch_attn8_rows_e4m3 : launch_attn8_rows_int8)(p, pl.row_tiles, s) != hipSuccess) return LRA_ERR_HIP;
+  } else if (launch_attn8_vector(p, bf16, pl.rows, s) != hipSuccess) {
+    return LRA_ERR_HIP;
+  }
   if (pl.states && launch_merge(p, bf16, pl.rows, s) != hipSuccess) return LRA_ERR_HIP;
   return LRA_OK;
 }

@@ -90,11 +90,29 @@ static int64_t keys_per_row(const lra_cache8* c, const lra_batch* b) {
   return b->window > 0 ? std::min<int64_t>(c->max_seq_len, static_cast<int64_t>(b->window) + b->sinks) : c->max_seq_len;
 }
 
+// 64 rows at most per sequence and kv head: workgroups of (kv head, key share, sequence), two to a compute unit, whose waves have a
+// tile of 64 keys each at least (4, 2 or 1 of them divide the tiles).
+static bool plan_few_rows(Attn8Plan& pl, const lra_shape* sh, const lra_cache8* c, const lra_batch* b) {
+  const int64_t G = sh->n_q_heads / sh->n_kv_heads, most = b->max_queries_per_seq * G;
+  if (most > 64 || c->n_seqs > 65535) return false;
+  pl.row_tiles = most <= 16 ? 1 : (most <= 32 ? 2 : 4);
+  const int64_t units = static_cast<int64_t>(sh->n_kv_heads) * std::min(c->n_seqs, b->n_queries);
+  const int64_t chunk = b->causal ? b->max_queries_per_seq : 1;
+  const int64_t key_tiles = (std::min<int64_t>(c->max_seq_len, keys_per_row(c, b) + chunk) + 63) / 64 + (b->window > 0 ? 2 : 0);
+  pl.few_rows = true;
+  pl.n_splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({2 * kCUs / units, (key_tiles * pl.row_tiles + 3) / 4, 64})));
+  place_states(pl, sh);
+  return true;
+}
+
 Attn8Plan plan_attn8(const lra_shape* sh, const lra_cache8* c, const lra_batch* b, const Tuning& tune) {
   Attn8Plan pl{};
   const int64_t rows = static_cast<int64_t>(b->n_queries) * sh->n_q_heads, keys = keys_per_row(c, b);
   pl.rows = static_cast<int>(rows);
   pl.launchable = true;
+  if (sh->dtype == LRA_BF16 && sh->rank % 8 == 0 && tune.variant != 1) {
+    if (tune.variant == 0 && plan_few_rows(pl, sh, c, b)) return pl;
+  }
   // vector-ALU kernel: one workgroup per row and share, three to a compute unit; a share of 256 keys at least
   pl.n_splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({3 * kCUs / rows, (keys + 255) / 256, 64})));
   pl.launchable = rows < (int64_t{1} << 24);  // (a grid dimension holds fewer than 2^32 threads)

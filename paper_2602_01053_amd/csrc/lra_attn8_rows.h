@@ -1,0 +1,409 @@
+// Attention over 8-bit codes for sequences with few query rows (bf16, gfx950): 64 at most per kv head, a decode step of some
+// agents or a few tokens, through a window and sinks or not.
+//
+// One workgroup streams a share of one (sequence, kv head)'s visible keys for all its rows: 16 rows to a wave, the four waves (or pairs
+// of them with up to 32 rows, or with more one of them) taking 64-key tiles in turn, four blocks each.  They are on their own from the
+// first tile to the last:
+//   S^T = K Q^T + L Qt^T,   online softmax along keys,   O^T += V^T P^T,   Olr^T += L^T P^T      (v_mfma_f32_16x16x32_bf16)
+// Nothing passes through LDS on the way: the layout of the cache is that of the operands.  Which key stands in which row of a product
+// is free, as long as the next product agrees, and so is the order of the dimension that a product sums over:
+//   row rho of key tile t (of four) is token 4t + rho % 4 of block rho / 4.  A lane of the A operand then takes a quarter of one
+//     token's K row, 32 bytes in a piece, with Q's dimensions in the same order;
+//   lane group g of the result S^T holds all sixteen tokens of block g, which is what the B operand of V^T P^T wants of it: its A
+//     operand is sixteen tokens of one dimension, the 16 bytes that the cache holds together;
+//   L is transposed by a product with the identity: the result layout of L I is the operand layout of L^T.
+// A code becomes bf16 with its block's scale in one instruction per pair (e4m3) or by itself (integers, whose scores and weights take
+// the scales instead, exactly): the codes of a tile cost a wave some 500 cycles, the 16 KB that they stand for 2000 of the memory's.
+// K of a wave's next tile is requested as soon as its scores are taken, V and L as soon as the products are: with eight waves to a
+// compute unit some hundred KB are on their way.
+#pragma once
+
+#include "lra_codes.h"
+#include "lra_decode_util.h"
+
+namespace lra {
+
+typedef short s16x4v __attribute__((ext_vector_type(4)));
+
+// Eight codes (two words) as bf16, times a power of two where CODE is e4m3.
+template <int CODE>
+__device__ __forceinline__ bf16x8 codes_to_bf16(uint32_t lo, uint32_t hi, float scale) {
+  uint32_t o[4];
+  if constexpr (CODE == LRA_E4M3) {
+    o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false));
+    o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true));
+    o[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false));
+    o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true));
+  } else {
+    // (integers of up to eight bits: exact in the upper half of a float)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t w = i < 2 ? lo : hi;
+      const float a = static_cast<float>(static_cast<signed char>(w >> (16 * (i & 1)))), b = static_cast<float>(static_cast<signed char>(w >> (16 * (i & 1) + 8)));
+      o[i] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+    }
+  }
+  return as_bf16x8(make_uint4(o[0], o[1], o[2], o[3]));
+}
+
+// RT: row tiles of a workgroup (1, 2 or 4).
+template <int D, int RT, int RP, bool HAS_BK, int CODE>
+__global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
+  constexpr int NS = 4 / RT;   // waves that divide the tiles of one row tile
+  constexpr int KS = D / 32;   // k-steps of S^T over the head dimension
+  constexpr int DB = D / 16;   // 16-row blocks of O^T
+  constexpr int RB = RP / 16;  // 16-row blocks of Olr^T
+  constexpr int KW = D / 64;   // 16-byte pieces of a lane's quarter of a K row
+  constexpr int SLOT = ((DB + RB) * 4 + 1) * 64 * 4;  // a wave's state, lane by lane
+  constexpr int QT_BYTES = HAS_BK ? RT * RB * 64 * 8 : 0;
+  constexpr int SMEM = 2 * SLOT > QT_BYTES ? 2 * SLOT : QT_BYTES;
+  __shared__ __align__(16) unsigned char smem[SMEM];
+  __shared__ float m_s[4][16];
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int Hq = p.n_q_heads, Hkv = p.n_kv_heads, G = p.group, r = p.rank;
+  const int split = blockIdx.x / Hkv, h = blockIdx.x - split * Hkv, t = blockIdx.y;
+  const int n_t = min(p.seq_lens[t], p.max_seq_len);
+  const int c0 = t > 0 ? min(max(p.seq_query_start[t], 0), p.n_queries) : 0;
+  const int c1 = t + 1 < p.n_seqs ? min(max(p.seq_query_start[t + 1], c0), p.n_queries) : p.n_queries;
+  const int n_rows = min((c1 - c0) * G, 16 * RT);
+  if (n_rows == 0) return;
+  const int first_pos = p.causal ? n_t - (c1 - c0) : n_t - 1, pos_last = n_t - 1;
+  const int rt = wave % RT, stream = wave / RT;
+  // this lane's row (the last one again past the end)
+  const int at_row = min(16 * rt + l16, n_rows - 1), tok = at_row / G;
+  const int row = (c0 + tok) * Hq + h * G + (at_row - tok * G), pos = first_pos + (p.causal ? tok : 0);
+  const bool live = 16 * rt + l16 < n_rows;
+  const bool has_rows = 16 * rt < n_rows;  // (uniform)
+  const int lo = p.window > 0 ? max(0, first_pos - p.window + 1) : 0, sinks = min(p.sinks, lo);
+  const int sink_tiles = (sinks + 63) / 64, gap = max(0, lo / 64 - sink_tiles);
+  const int n_tiles = n_t <= 0 ? 0 : (n_t - 1) / 64 + 1 - gap;
+  const int t0 = static_cast<int>(static_cast<int64_t>(n_tiles) * split / p.n_splits);
+  const int t1 = static_cast<int>(static_cast<int64_t>(n_tiles) * (split + 1) / p.n_splits);
+  const int a_first = min(max(p.query_adapter[c0], 0), p.n_adapters - 1);
+  const int64_t slot = static_cast<int64_t>(row) * p.n_splits + split;
+  auto adapter_of_row = [&]() __attribute__((always_inline)) -> int { return p.causal ? a_first : p.query_adapter[c0 + tok]; };
+  if (t0 >= t1) {
+    // an empty state, all the merge kernel looks at; for a row that sees nothing at all share 0 leaves one that gives zeros
+    if (stream == 0 && live) {
+      const bool nothing = split == 0 && pos < 0;
+      if (g == 0) {
+        p.part_ml[slot * 2 + 0] = nothing ? 0.f : -INFINITY;
+        p.part_ml[slot * 2 + 1] = nothing ? 1.f : 0.f;
+        if (split == 0) p.part_adapter[row] = adapter_of_row();
+      }
+      if (nothing) {
+        for (int c = g; c < D; c += 4) p.part_o[slot * D + c] = 0.f;
+        for (int c = g; c < r; c += 4) p.part_lr[slot * r + c] = 0.f;
+      }
+    }
+    return;
+  }
+  auto key_of = [&](int tile) __attribute__((always_inline)) -> int { return (tile < sink_tiles ? tile : tile + gap) * 64; };
+  // (some query of the sequence sees it)
+  auto kept = [&](int key) __attribute__((always_inline)) -> bool { return key < n_t && (key < sinks || key >= lo); };
+  // whether all tokens of the tile are
+  auto whole = [&](int j) __attribute__((always_inline)) -> bool { return j + 64 <= n_t && (j + 64 <= sinks || j >= lo); };
+
+  // ---------------- a tile's requests ----------------
+  const int my_block = l16 >> 2, my_token = l16 & 3;  // of the A operands of S^T: row l16
+  const uint8_t* const kh = static_cast<const uint8_t*>(p.k_base) + h * p.kv_head_stride + my_token * D + g * (D / 4);
+  const uint8_t* const vh = static_cast<const uint8_t*>(p.v_base) + h * p.kv_head_stride + l16 * 16;
+  const bf16_t* const lh = static_cast<const bf16_t*>(p.l) + my_token * p.l_row_stride + 4 * g;
+  // id of block g of the tile; a block that nobody sees may have any: the one of the last token stands in, weighted zero
+  auto look_up = [&](int j) __attribute__((always_inline)) -> int {
+    const int j0 = j + 16 * g;
+    const bool any = j0 < n_t && (j0 < sinks || j0 + 15 >= lo);
+    return block8(p.block_table, p.max_blocks_per_seq, t, (any ? j0 : n_t - 1) >> 4);
+  };
+  uint4 kc[4][KW], vc[DB];
+  uint2 lc[4][RB];
+  int ks_raw, vs_raw;
+  auto issue_k = [&](int id) __attribute__((always_inline)) {
+    const uint8_t* src = kh + __shfl(id, my_block * 16, kWave) * p.kv_block_stride;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int w = 0; w < KW; ++w) kc[i][w] = *reinterpret_cast<const uint4*>(src + i * 4 * D + w * 16);
+    ks_raw = p.k_scale[id * p.scale_block_stride + h];
+  };
+  auto issue_l = [&](int id) __attribute__((always_inline)) {
+    const bf16_t* src = lh + __shfl(id, my_block * 16, kWave) * static_cast<int64_t>(16) * p.l_row_stride;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int b = 0; b < RB; ++b) lc[i][b] = 16 * b + 4 * g < r ? *reinterpret_cast<const uint2*>(src + 4 * i * p.l_row_stride + 16 * b) : make_uint2(0u, 0u);
+  };
+  auto issue_v = [&](int id) __attribute__((always_inline)) {
+    const uint8_t* src = vh + id * p.kv_block_stride;
+#pragma unroll
+    for (int b = 0; b < DB; ++b) vc[b] = *reinterpret_cast<const uint4*>(src + b * 256);
+    vs_raw = p.v_scale[id * p.scale_block_stride + h];
+  };
+  const int first = has_rows ? t0 + stream : t1;
+  int id_next = 0;
+  if (first < t1) {
+    const int id = look_up(key_of(first));
+    issue_k(id);
+    issue_l(id);
+    issue_v(id);
+    id_next = look_up(key_of(min(first + NS, t1 - 1)));
+  }
+
+  // ---------------- prologue: Q operands, Qt = Q B_K^T ----------------
+  bf16x8 qb[KS];
+  {
+    const bf16_t* qr = static_cast<const bf16_t*>(p.q) + static_cast<int64_t>(row) * D + g * (D / 4);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qb[ks] = as_bf16x8(*reinterpret_cast<const uint4*>(qr + ks * 8));
+  }
+  // Qt^T, ranks by rows: register e of block b is rank 16b + 4g + e, the operand that L Qt^T takes (k = 16: four ranks a lane group).
+  // The waves of a row tile divide its queries (each with its adapter, or the chunk's one) and hand the operands round in LDS.
+  s16x4v qtb[HAS_BK ? RB : 1];
+  if constexpr (HAS_BK) {
+    const int64_t ldb = static_cast<int64_t>(Hkv) * D;
+    const int it0 = p.causal ? 0 : 16 * rt / G, it1 = !has_rows ? it0 : (p.causal ? 1 : (min(16 * rt + 16, n_rows) - 1) / G + 1);
+    uint2* const qt_s = reinterpret_cast<uint2*>(smem) + rt * RB * 64;
+#pragma unroll 1
+    for (int it = it0 + stream; it < it1; it += NS) {
+      const int a = p.causal ? a_first : min(max(p.query_adapter[c0 + it], 0), p.n_adapters - 1);
+      const bf16_t* src = static_cast<const bf16_t*>(p.b_k) + static_cast<int64_t>(a) * r * ldb + h * D + g * (D / 4);
+#pragma unroll
+      for (int b = 0; b < RB; ++b) {
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const uint4 bk = 16 * b + l16 < r ? *reinterpret_cast<const uint4*>(src + (16 * b + l16) * ldb + ks * 8) : make_uint4(0u, 0u, 0u, 0u);
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(bk), qb[ks], acc, 0, 0, 0);
+        }
+        if (p.causal || tok == it) qt_s[b * 64 + lane] = make_uint2(pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3]));
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int b = 0; b < RB; ++b) qtb[b] = __builtin_bit_cast(s16x4v, qt_s[b * 64 + lane]);
+    __syncthreads();  // (the states go where these were)
+  }
+  // the identity as B operand: lane (column l16), element e <-> row 4g + e
+  s16x4v eye;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) eye[e] = 4 * g + e == l16 ? 0x3f80 : 0;
+
+  // ---------------- main loop ----------------
+  const f32x4 zero4 = {0.f, 0.f, 0.f, 0.f};
+  f32x4 o_acc[DB], lr_acc[RB];
+#pragma unroll
+  for (int b = 0; b < DB; ++b) o_acc[b] = zero4;
+#pragma unroll
+  for (int b = 0; b < RB; ++b) lr_acc[b] = zero4;
+  float m_run = -INFINITY, l_run = 0.f;
+  const float sc = p.scale * 1.44269504088896340736f;
+  for (int tile = first; tile < t1; tile += NS) {
+    const int j = key_of(tile);
+    const bool more = tile + NS < t1;
+    const bool all = whole(j);
+    // S^T: element (i, e) of this lane is token 4i + e of block g
+    f32x4 s[4];
+    {
+      const float ks_mine = scale8(ks_raw), ks_row = __shfl(ks_mine, my_block * 16, kWave);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s[i] = zero4;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const uint4 c = kc[i][ks >> 1];
+          s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_to_bf16<CODE>(ks & 1 ? c.z : c.x, ks & 1 ? c.w : c.y, ks_row), qb[ks], s[i], 0, 0, 0);
+        }
+        if constexpr (CODE == LRA_INT8) s[i] *= ks_mine;
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    const int id_now = id_next;
+    if (more) {
+      issue_k(id_now);
+      id_next = look_up(key_of(min(tile + 2 * NS, t1 - 1)));
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    // L: rows that nobody sees are zeros
+    if (!all) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool in = kept(j + 16 * my_block + 4 * i + my_token);
+#pragma unroll
+        for (int b = 0; b < RB; ++b) lc[i][b] = in ? lc[i][b] : make_uint2(0u, 0u);
+      }
+    }
+    if constexpr (HAS_BK) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int b = 0; b < RB; ++b) s[i] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4v, lc[i][b]), qtb[b], s[i], 0, 0, 0);
+    }
+    if (j + 63 > first_pos) {  // some row does not see the last key
+      const int last = pos - j - 16 * g;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (4 * i + e > last) s[i][e] = -INFINITY;
+    }
+    if (p.window > 0 && j + p.window <= pos_last && j + 64 > p.sinks) {  // some row's window starts behind the first key
+      const int from = p.sinks - j - 16 * g;
+      const uint32_t hidden = static_cast<uint32_t>(max(0, pos - p.window + 1 - p.sinks));
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (static_cast<uint32_t>(4 * i + e - from) < hidden) s[i][e] = -INFINITY;
+    }
+    // (the accumulators are rescaled only where some row's maximum grows; the probabilities, at most 1, round to bf16 for the
+    // matrix cores, their sum is taken in fp32 before)
+    const float vs_mine = scale8(vs_raw);
+    uint32_t wl[8], wv[8];  // weights for L, and for V: with the block's scale, where that is not in V's operand
+    {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[i][e]);
+      mx = tile_reference(max_over_lane_groups(mx) * sc);
+      if (__builtin_amdgcn_ballot_w64(mx > m_run) != 0) {
+        const float m_new = fmaxf(m_run, mx);
+        const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+        m_run = m_new;
+        l_run *= alpha;
+#pragma unroll
+        for (int b = 0; b < DB; ++b) o_acc[b] *= alpha;
+#pragma unroll
+        for (int b = 0; b < RB; ++b) lr_acc[b] *= alpha;
+      }
+      const float nm = m_run == -INFINITY ? 0.f : -m_run;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[e] = __builtin_amdgcn_exp2f(fmaf(s[i][e], sc, nm));
+          l_run += x[e];
+        }
+        wl[2 * i] = pack_bf16x2(x[0], x[1]), wl[2 * i + 1] = pack_bf16x2(x[2], x[3]);
+        // (a power of two: the same rounding as without it)
+        if constexpr (CODE == LRA_INT8) wv[2 * i] = pack_bf16x2(x[0] * vs_mine, x[1] * vs_mine), wv[2 * i + 1] = pack_bf16x2(x[2] * vs_mine, x[3] * vs_mine);
+        else wv[2 * i] = wl[2 * i], wv[2 * i + 1] = wl[2 * i + 1];
+      }
+    }
+    auto half = [](const uint32_t (&w)[8], int hf) __attribute__((always_inline)) { return as_bf16x8(make_uint4(w[4 * hf], w[4 * hf + 1], w[4 * hf + 2], w[4 * hf + 3])); };
+    // O^T += V^T P^T: half hf of the sixteen tokens of every block
+    if (!all) {  // codes of tokens that nobody sees may be no numbers: zeros
+      uint32_t mask[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        mask[c] = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mask[c] |= kept(j + 16 * g + 4 * c + e) ? 0xffu << (8 * e) : 0u;
+      }
+#pragma unroll
+      for (int b = 0; b < DB; ++b) vc[b] = make_uint4(vc[b].x & mask[0], vc[b].y & mask[1], vc[b].z & mask[2], vc[b].w & mask[3]);
+    }
+#pragma unroll
+    for (int b = 0; b < DB; ++b) {
+      o_acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_to_bf16<CODE>(vc[b].x, vc[b].y, vs_mine), half(wv, 0), o_acc[b], 0, 0, 0);
+      o_acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_to_bf16<CODE>(vc[b].z, vc[b].w, vs_mine), half(wv, 1), o_acc[b], 0, 0, 0);
+    }
+#pragma unroll
+    for (int b = 0; b < RB; ++b)
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        // (bf16 values in fp32: their upper halves)
+        auto pair = [](float x, float y) { return __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u); };
+        const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4v, lc[2 * hf][b]), eye, zero4, 0, 0, 0);
+        const f32x4 y = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4v, lc[2 * hf + 1][b]), eye, zero4, 0, 0, 0);
+        const bf16x8 a = as_bf16x8(make_uint4(pair(x[0], x[1]), pair(x[2], x[3]), pair(y[0], y[1]), pair(y[2], y[3])));
+        lr_acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, half(wl, hf), lr_acc[b], 0, 0, 0);
+      }
+    __builtin_amdgcn_sched_barrier(0);
+    if (more) {
+      issue_l(id_now);
+      issue_v(id_now);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+
+  // ---------------- the states of a row tile's waves: two by two through LDS, the first of them stores ----------------
+  l_run = sum_over_lane_groups(l_run);
+  float m_all = m_run;
+  if constexpr (NS > 1) {
+    if (g == 0) m_s[wave][l16] = m_run;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NS; ++i) m_all = fmaxf(m_all, m_s[i * RT + rt][l16]);
+    const float wgt = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_all);
+    l_run = m_run == -INFINITY ? l_run : l_run * wgt;  // (a sum of NaN stays one)
+#pragma unroll
+    for (int b = 0; b < DB; ++b) o_acc[b] *= wgt;
+#pragma unroll
+    for (int b = 0; b < RB; ++b) lr_acc[b] *= wgt;
+#pragma unroll
+    for (int stride = NS / 2; stride >= 1; stride >>= 1) {
+      if (stream >= stride && stream < 2 * stride) {
+        float* dst = reinterpret_cast<float*>(smem + (wave - stride * RT) * SLOT) + lane;
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) dst[(b * 4 + i) * 64] = o_acc[b][i];
+#pragma unroll
+        for (int b = 0; b < RB; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) dst[((DB + b) * 4 + i) * 64] = lr_acc[b][i];
+        dst[(DB + RB) * 4 * 64] = l_run;
+      }
+      __syncthreads();
+      if (stream < stride) {
+        const float* src = reinterpret_cast<const float*>(smem + wave * SLOT) + lane;
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o_acc[b][i] += src[(b * 4 + i) * 64];
+#pragma unroll
+        for (int b = 0; b < RB; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) lr_acc[b][i] += src[((DB + b) * 4 + i) * 64];
+        l_run += src[(DB + RB) * 4 * 64];
+      }
+      __syncthreads();
+    }
+  }
+  if (stream != 0 || !live) return;
+  if (g == 0) {
+    const bool nothing = split == 0 && pos < 0;  // (such a row's O and O_lr are zeros)
+    p.part_ml[slot * 2 + 0] = nothing ? 0.f : m_all * 0.69314718055994530942f;  // natural-log units
+    p.part_ml[slot * 2 + 1] = nothing ? 1.f : l_run;
+    if (split == 0) p.part_adapter[row] = adapter_of_row();
+  }
+#pragma unroll
+  for (int b = 0; b < DB; ++b) *reinterpret_cast<f32x4*>(p.part_o + slot * D + 16 * b + 4 * g) = o_acc[b];
+#pragma unroll
+  for (int b = 0; b < RB; ++b)
+    if (16 * b + 4 * g < r) *reinterpret_cast<f32x4*>(p.part_lr + slot * r + 16 * b + 4 * g) = lr_acc[b];  // (the rank is a multiple of 8)
+}
+
+template <int D, int CODE>
+static hipError_t launch_attn8_rows(const Batch8Params& p, int row_tiles, hipStream_t s) {
+  const dim3 grid(p.n_kv_heads * p.n_splits, p.n_seqs);
+  auto launch = [&](auto rt_c, auto rp_c) {
+    constexpr int RT = decltype(rt_c)::value, RP = decltype(rp_c)::value;
+    if (p.b_k != nullptr) hipLaunchKernelGGL((attn8_rows_kernel<D, RT, RP, true, CODE>), grid, dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((attn8_rows_kernel<D, RT, RP, false, CODE>), grid, dim3(256), 0, s, p);
+  };
+  auto by_rank = [&](auto rt_c) {
+    if (p.rank <= 16) launch(rt_c, std::integral_constant<int, 16>{});
+    else if (p.rank <= 32) launch(rt_c, std::integral_constant<int, 32>{});
+    else launch(rt_c, std::integral_constant<int, 64>{});
+  };
+  if (row_tiles <= 1) by_rank(std::integral_constant<int, 1>{});
+  else if (row_tiles <= 2) by_rank(std::integral_constant<int, 2>{});
+  else by_rank(std::integral_constant<int, 4>{});
+  return hipGetLastError();
+}
+
+}  // namespace lra

@@ -59,4 +59,7 @@ __device__ __forceinline__ uint32_t encode4(const float (&x)[4]) {
   }
 }
 
+hipError_t launch_attn8_rows_e4m3(const Batch8Params& p, int row_tiles, hipStream_t s);
+hipError_t launch_attn8_rows_int8(const Batch8Params& p, int row_tiles, hipStream_t s);
+
 }  // namespace lra
