@@ -50,7 +50,7 @@ typedef struct {
   int64_t kv_block_stride;    /* bytes, multiples of 16 */
   int64_t kv_head_stride;
   int64_t scale_block_stride; /* bytes, >= Hkv; 0: Hkv */
-  int64_t l_row_stride;       /* elements; 0: rank.  A multiple of 8, or the rank */
+  int64_t l_row_stride;       /* elements; 0: rank.  A multiple of 8, or the rank; at most 2^24 */
   int32_t code;               /* lra_code */
   int32_t max_blocks_per_seq; /* row length of block_table (of no effect without one) */
   int32_t num_blocks;

@@ -17,7 +17,7 @@ PYCALL_PATH = os.path.join(PKG_DIR, "_lra_pycall" + (sysconfig.get_config_var("E
 # what the compiler reports per kernel (registers, scratch, LDS, occupancy), written by every build
 RESOURCES_PATH = os.path.join(PKG_DIR, "kernel_resources.json")
 
-SOURCES = ["lra_plan.cpp", "lra_batch_plan.cpp", "lra_attn8_plan.cpp", "lra_api.hip", "lra_batch.hip", "lra_batch_rows.hip", "lra_batch_tiles_d64.hip", "lra_batch_tiles_d128.hip", "lra_key_weights.hip", "lra_key_weights_mfma.hip", "lra_evict.hip", "lra_cache8.hip", "lra_attn8.hip", "lra_attn8_rows_e4m3.hip", "lra_attn8_rows_int8.hip", "lra_matmul_i8.hip", "lra_generic.hip", "lra_decode_mfma.hip", "lra_decode_batch.hip", "lra_decode_stream.hip", "lra_prefill_mfma.hip", "lra_prefill_rows.hip", "lra_append.hip", "lra_probe.hip"]
+SOURCES = ["lra_plan.cpp", "lra_batch_plan.cpp", "lra_attn8_plan.cpp", "lra_api.hip", "lra_batch.hip", "lra_batch_rows.hip", "lra_batch_tiles_d64.hip", "lra_batch_tiles_d128.hip", "lra_key_weights.hip", "lra_key_weights_mfma.hip", "lra_evict.hip", "lra_cache8.hip", "lra_attn8.hip", "lra_attn8_rows_e4m3.hip", "lra_attn8_rows_int8.hip", "lra_attn8_tiles_e4m3.hip", "lra_attn8_tiles_int8.hip", "lra_matmul_i8.hip", "lra_generic.hip", "lra_decode_mfma.hip", "lra_decode_batch.hip", "lra_decode_stream.hip", "lra_prefill_mfma.hip", "lra_prefill_rows.hip", "lra_append.hip", "lra_probe.hip"]
 
 HIPCC_FLAGS = [
     "-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC",

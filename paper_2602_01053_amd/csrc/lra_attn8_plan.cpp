@@ -36,7 +36,7 @@ lra_status check_cache8(const lra_shape* sh, const lra_cache8* c) {
   if (c->scale_block_stride > (int64_t{1} << 31)) return LRA_ERR_UNSUPPORTED;
   if (c->l_row_stride < 0 || (c->l_row_stride != 0 && c->l_row_stride < sh->rank)) return LRA_ERR_SHAPE;
   if (c->l_row_stride != sh->rank && (c->l_row_stride & 7)) return LRA_ERR_SHAPE;
-  if (c->l_row_stride > (int64_t{1} << 31) || (c->l_row_stride ? c->l_row_stride : sh->rank) > (int64_t{1} << 56) / c->num_blocks)
+  if (c->l_row_stride > (int64_t{1} << 24) || (c->l_row_stride ? c->l_row_stride : sh->rank) > (int64_t{1} << 56) / c->num_blocks)
     return LRA_ERR_UNSUPPORTED;
   if ((reinterpret_cast<uintptr_t>(c->k) | reinterpret_cast<uintptr_t>(c->v) | reinterpret_cast<uintptr_t>(c->l)) & 15) return LRA_ERR_SHAPE;
   return LRA_OK;
@@ -105,6 +105,24 @@ static bool plan_few_rows(Attn8Plan& pl, const lra_shape* sh, const lra_cache8* 
   return true;
 }
 
+// A workgroup of attn8_tiles_kernel takes 128 rows of one sequence.  The key tiles of a q tile are shared where there are fewer q tiles
+// than the chip has places, two per compute unit, and then so that they fill the places once; a share walks two tiles at least.
+static bool plan_tiles(Attn8Plan& pl, const lra_shape* sh, const lra_cache8* c, const lra_batch* b) {
+  const int64_t G = sh->n_q_heads / sh->n_kv_heads;
+  const int64_t places = b->n_queries * G / 128 + c->n_seqs;
+  if (places * sh->n_kv_heads >= (int64_t{1} << 24)) return false;  // (a grid dimension holds fewer than 2^32 threads)
+  const int64_t q_tiles = std::max<int64_t>((b->n_queries * G + 127) / 128, std::min(c->n_seqs, b->n_queries));
+  const int64_t chunk = b->causal ? std::min<int64_t>(b->max_queries_per_seq, 128 / G + 1) : 1;
+  const int64_t key_tiles = (std::min<int64_t>(c->max_seq_len, keys_per_row(c, b) + chunk) + 63) / 64 + (b->window > 0 ? 2 : 0);
+  pl.tiles = true;
+  pl.tile_places = static_cast<int>(places);
+  pl.n_splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({2 * kCUs / (q_tiles * sh->n_kv_heads), (key_tiles + 1) / 2, 64})));
+  // states also where the rows of a tile have adapters of their own (the merge kernel applies B_V row by row), and at d = 128 and ranks
+  // above 32 (with the product by B_V behind its loop the kernel goes to scratch memory)
+  if (pl.n_splits > 1 || !b->causal || (sh->head_dim == 128 && sh->rank > 32)) place_states(pl, sh);
+  return true;
+}
+
 Attn8Plan plan_attn8(const lra_shape* sh, const lra_cache8* c, const lra_batch* b, const Tuning& tune) {
   Attn8Plan pl{};
   const int64_t rows = static_cast<int64_t>(b->n_queries) * sh->n_q_heads, keys = keys_per_row(c, b);
@@ -112,6 +130,7 @@ Attn8Plan plan_attn8(const lra_shape* sh, const lra_cache8* c, const lra_batch* 
   pl.launchable = true;
   if (sh->dtype == LRA_BF16 && sh->rank % 8 == 0 && tune.variant != 1) {
     if (tune.variant == 0 && plan_few_rows(pl, sh, c, b)) return pl;
+    if (plan_tiles(pl, sh, c, b)) return pl;
   }
   // vector-ALU kernel: one workgroup per row and share, three to a compute unit; a share of 256 keys at least
   pl.n_splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({3 * kCUs / rows, (keys + 255) / 256, 64})));

@@ -46,6 +46,33 @@ __device__ __forceinline__ bf16x8 codes_to_bf16(uint32_t lo, uint32_t hi, float 
   return as_bf16x8(make_uint4(o[0], o[1], o[2], o[3]));
 }
 
+// Eight codes as the bf16 values that they stand for.
+template <int CODE>
+__device__ __forceinline__ uint4 codes_to_values(uint32_t lo, uint32_t hi, float scale) {
+  if constexpr (CODE == LRA_E4M3) {
+    return __builtin_bit_cast(uint4, codes_to_bf16<CODE>(lo, hi, scale));
+  } else {
+    uint32_t o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t w = i < 2 ? lo : hi;
+      const float a = static_cast<float>(static_cast<signed char>(w >> (16 * (i & 1)))) * scale;
+      const float b = static_cast<float>(static_cast<signed char>(w >> (16 * (i & 1) + 8))) * scale;
+      o[i] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+    }
+    return make_uint4(o[0], o[1], o[2], o[3]);
+  }
+}
+
+// Byte masks of the sixteen tokens from j0 on, four to a word: ones for those below n and outside [cut_lo, cut_hi).
+__device__ __forceinline__ uint4 token_masks(int j0, int n, int cut_lo, int cut_hi) {
+  auto below = [](int k) __attribute__((always_inline)) -> uint32_t { return (1u << min(max(k, 0), 16)) - 1u; };
+  const uint32_t bits = below(n - j0) & ~(below(cut_hi - j0) & ~below(cut_lo - j0));
+  auto word = [&](int c) __attribute__((always_inline)) -> uint32_t { return (((bits >> (4 * c)) & 15u) * 0x00204081u & 0x01010101u) * 255u; };
+  return make_uint4(word(0), word(1), word(2), word(3));
+}
+__device__ __forceinline__ uint4 masked(uint4 v, uint4 m) { return make_uint4(v.x & m.x, v.y & m.y, v.z & m.z, v.w & m.w); }
+
 // RT: row tiles of a workgroup (1, 2 or 4).
 template <int D, int RT, int RP, bool HAS_BK, int CODE>
 __global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
@@ -295,15 +322,9 @@ __global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
     auto half = [](const uint32_t (&w)[8], int hf) __attribute__((always_inline)) { return as_bf16x8(make_uint4(w[4 * hf], w[4 * hf + 1], w[4 * hf + 2], w[4 * hf + 3])); };
     // O^T += V^T P^T: half hf of the sixteen tokens of every block
     if (!all) {  // codes of tokens that nobody sees may be no numbers: zeros
-      uint32_t mask[4];
+      const uint4 mask = token_masks(j + 16 * g, n_t, sinks, lo);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        mask[c] = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) mask[c] |= kept(j + 16 * g + 4 * c + e) ? 0xffu << (8 * e) : 0u;
-      }
-#pragma unroll
-      for (int b = 0; b < DB; ++b) vc[b] = make_uint4(vc[b].x & mask[0], vc[b].y & mask[1], vc[b].z & mask[2], vc[b].w & mask[3]);
+      for (int b = 0; b < DB; ++b) vc[b] = masked(vc[b], mask);
     }
 #pragma unroll
     for (int b = 0; b < DB; ++b) {

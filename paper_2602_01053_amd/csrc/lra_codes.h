@@ -61,5 +61,8 @@ __device__ __forceinline__ uint32_t encode4(const float (&x)[4]) {
 
 hipError_t launch_attn8_rows_e4m3(const Batch8Params& p, int row_tiles, hipStream_t s);
 hipError_t launch_attn8_rows_int8(const Batch8Params& p, int row_tiles, hipStream_t s);
+// part_ml NULL: no states, the outputs themselves (n_splits 1)
+hipError_t launch_attn8_tiles_e4m3(const Batch8Params& p, hipStream_t s);
+hipError_t launch_attn8_tiles_int8(const Batch8Params& p, hipStream_t s);
 
 }  // namespace lra
