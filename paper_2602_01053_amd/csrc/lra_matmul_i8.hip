@@ -86,30 +86,287 @@ __device__ __forceinline__ void store_scaled(const I8Params& p, int i, int j, in
   static_cast<T*>(p.y)[i * p.y_stride + j] = from_f32<T>(static_cast<float>(sum) * p.x_scale[i] * p.w_scale[j]);
 }
 
-// A wave per 16 features and 16 tokens: W x^T by v_mfma_i32_16x16x64_i8, operands straight from memory.
-template <typename T>
-__global__ __launch_bounds__(256) void matmul_i8_kernel(I8Params p) {
+// The sums' order does not matter (integers), the scaling is the same everywhere: all kernels below give the same bits.
+
+// Few tokens (64 at most): the weights are read once and nothing else counts.  A workgroup of eight waves takes 16 features and all
+// tokens, a wave every eighth 64-wide piece of k, eight pieces of its weights requested at a time; operands straight from memory
+// (v_mfma_i32_16x16x64_i8: a lane's 16 bytes of a row are its operand), the waves' sums meet in LDS.  RT: token tiles of 16.
+template <typename T, int RT>
+__global__ __launch_bounds__(512) void matmul_i8_stream_kernel(I8Params p) {
+  constexpr int U = RT == 4 ? 4 : 8;
+  __shared__ int sums[8][RT][4][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, g = lane >> 4;
-  const int j0 = (static_cast<int>(blockIdx.x) * 4 + wave) * 16, i0 = static_cast<int>(blockIdx.y) * 16;
+  const int j0 = static_cast<int>(blockIdx.x) * 16;
+  const int8_t* wr = p.w + min(j0 + l16, p.n - 1) * p.w_stride + 16 * g;
+  const int8_t* xr[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) xr[rt] = p.x + min(16 * rt + l16, p.m - 1) * p.x_stride + 16 * g;
+  i32x4 acc[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) acc[rt] = i32x4{0, 0, 0, 0};
+  for (int c0 = wave * 64; c0 < p.k; c0 += 8 * 64 * U) {
+    i32x4 a[U], b[U][RT];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int c = c0 + u * 512;
+      const bool in = c + 16 * g < p.k;
+      a[u] = in ? *reinterpret_cast<const i32x4*>(wr + c) : i32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) b[u][rt] = in ? *reinterpret_cast<const i32x4*>(xr[rt] + c) : i32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) acc[rt] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[u], b[u][rt], acc[rt], 0, 0, 0);
+  }
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sums[wave][rt][e][lane] = acc[rt][e];
+  __syncthreads();
+  // register e: feature j0 + 4g + e of token 16 rt + l16; neighbouring threads take neighbouring features
+  for (int i = threadIdx.x; i < RT * 256; i += 512) {
+    const int f = i & 15, tok = i >> 4;
+    if (tok >= p.m || j0 + f >= p.n) continue;
+    int sum = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) sum += sums[w][tok >> 4][f & 3][(f >> 2) * 16 + (tok & 15)];
+    store_scaled<T>(p, tok, j0 + f, sum);
+  }
+}
+
+// The scaled sums of a 32 x 32 block: register i of a lane is feature f0 + 8 (i / 4) + 4 g2 + i % 4 of token `tok`.
+typedef int i32x16 __attribute__((ext_vector_type(16)));
+template <typename T>
+__device__ __forceinline__ void store_block(const I8Params& p, const i32x16& acc, int tok, int f0, int g2) {
+  if (tok >= p.m) return;
+  const float xs = p.x_scale[tok];
+  T* row = static_cast<T*>(p.y) + tok * p.y_stride;
+  const bool whole = (p.y_stride & 3) == 0;  // (four features lie together and aligned)
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int f = f0 + 8 * q + 4 * g2;
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = static_cast<float>(acc[4 * q + e]) * xs * p.w_scale[min(f + e, p.n - 1)];
+    if (whole && f + 4 <= p.n) {
+      if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(row + f) = make_uint2(pf_pack2(v[0], v[1]), pf_pack2(v[2], v[3]));
+      else *reinterpret_cast<float4*>(row + f) = make_float4(v[0], v[1], v[2], v[3]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (f + e < p.n) row[f + e] = from_f32<T>(v[e]);
+    }
+  }
+}
+
+// Workgroup -> tile.  Consecutive workgroups go to consecutive XCDs: an XCD takes an eighth of the tiles, one after the other, token
+// tiles in fours and the feature tiles of a four in turn, so that what it works on at a time shares its L2.
+__device__ __forceinline__ bool tile_of(int n_tt, int n_ct, int& tt, int& ct) {
+  const int total = n_tt * n_ct, per = (total + 7) / 8;
+  const int i = static_cast<int>(blockIdx.x) >> 3, tile = (static_cast<int>(blockIdx.x) & 7) * per + i;
+  if (i >= per || tile >= total) return false;
+  const int grp = tile / (4 * n_ct), r = tile - grp * 4 * n_ct, high = min(4, n_tt - 4 * grp);
+  ct = r / high;
+  tt = 4 * grp + r - ct * high;
+  return true;
+}
+
+// 64 features x 64 tokens by eight waves, two of which divide k of each of the four 32 x 32 blocks.  Steps of 256 bytes of k, four
+// stages in LDS (a step's 32 KB are asked for three steps ahead: a tile is a chain of k / 256 steps with nothing else to hide their
+// latency).  A row of a stage is 256 bytes, its 16-byte chunks exchanged by row (xor), so that sixteen rows' reads spread over the banks.
+template <typename T>
+__global__ __launch_bounds__(512, 2) void matmul_i8_quarter_kernel(I8Params p) {
+  constexpr int BK = 256, NS = 4, TILE = 64 * BK, STAGE = 2 * TILE;
+  __shared__ __align__(16) unsigned char smem[NS * STAGE];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l32 = lane & 31, g2 = lane >> 5;
+  int tt, ct;
+  if (!tile_of((p.m + 63) / 64, (p.n + 63) / 64, tt, ct)) return;
+  const int tok0 = tt * 64, feat0 = ct * 64;
+  const uint32_t ldw = static_cast<uint32_t>(p.w_stride), ldx = static_cast<uint32_t>(p.x_stride);  // (at most 2^22)
+  const pf_u32x4 rs_w = pf_rsrc(p.w + feat0 * p.w_stride, (min(64, p.n - feat0) - 1u) * ldw + p.k);
+  const pf_u32x4 rs_x = pf_rsrc(p.x + tok0 * p.x_stride, (min(64, p.m - tok0) - 1u) * ldx + p.k);
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(PF_LDS_AS(unsigned char, smem)));
+  // request i of sixteen per tile fills rows 4i .. 4i + 3; wave w has i = w and w + 8 (the same rows mod 16: 4w .. 4w + 3)
+  const int row = lane >> 4, chunk = (lane & 15) ^ ((4 * wave + row) & 15);
+  const int n_steps = (p.k + BK - 1) / BK;
+  auto issue = [&](int step) __attribute__((always_inline)) {
+    const bool in = step * BK + chunk * 16 < p.k;  // (behind the last column: zeros)
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int r = 4 * (wave + 8 * q) + row;
+      const uint32_t dst = lds0 + (step % NS) * STAGE + (wave + 8 * q) * 1024;
+      pf_load16_to_lds(rs_w, dst, in ? r * ldw + chunk * 16 : kPfOob, step * BK);
+      pf_load16_to_lds(rs_x, dst + TILE, in ? r * ldx + chunk * 16 : kPfOob, step * BK);
+    }
+  };
+  for (int s = 0; s < NS - 1; ++s)
+    if (s < n_steps) issue(s);
+  const int kh = wave >> 2, fb = wave & 1, tb = (wave >> 1) & 1;
+  const int a_row = (32 * fb + l32) * BK, b_row = TILE + (32 * tb + l32) * BK, x15 = (l32 & 15);
+  i32x16 acc;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) acc[i] = 0;
+  for (int s = 0; s < n_steps; ++s) {
+    // this step's four requests of the wave are here, those of the two behind it may be on their way
+    if (s + 2 < n_steps) asm volatile("s_waitcnt vmcnt(8)");
+    else if (s + 1 < n_steps) asm volatile("s_waitcnt vmcnt(4)");
+    else pf_wait_vm0();
+    __syncthreads();  // ... and everybody's; and everybody has read the stage that is filled next
+    if (s + NS - 1 < n_steps) issue(s + NS - 1);
+    const unsigned char* st = smem + (s % NS) * STAGE;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+      const int c = ((8 * kh + 2 * ks + g2) ^ x15) << 4;
+      const i32x4 a = *reinterpret_cast<const i32x4*>(st + a_row + c), b = *reinterpret_cast<const i32x4*>(st + b_row + c);
+      acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, acc, 0, 0, 0);
+    }
+  }
+  __syncthreads();
+  int* other = reinterpret_cast<int*>(smem) + (wave & 3) * 1024 + lane;
+  if (kh == 1) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) other[i * 64] = acc[i];
+  }
+  __syncthreads();
+  if (kh == 1) return;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) acc[i] += other[i * 64];
+  store_block<T>(p, acc, tok0 + 32 * tb + l32, feat0 + 32 * fb, g2);
+}
+
+// 256 features x 256 tokens by eight waves of 128 x 64 (eight 32 x 32 accumulators): six operand reads for eight products, 64 KB into
+// LDS for 16.8 M multiply-adds.  Steps of 128 bytes of k, two stages, one workgroup per compute unit; the two waves of a SIMD cover each
+// other's reads and requests.
+template <typename T>
+__global__ __launch_bounds__(512, 2) void matmul_i8_wide_kernel(I8Params p) {
+  constexpr int BK = 128, TILE = 256 * BK, STAGE = 2 * TILE;
+  __shared__ __align__(16) unsigned char smem[2 * STAGE];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l32 = lane & 31, g2 = lane >> 5;
+  const int wr = wave >> 2, wc = wave & 3;
+  int tt, ct;
+  if (!tile_of((p.m + 255) / 256, (p.n + 255) / 256, tt, ct)) return;
+  const int tok0 = tt * 256, feat0 = ct * 256;
+  const uint32_t ldw = static_cast<uint32_t>(p.w_stride), ldx = static_cast<uint32_t>(p.x_stride);  // (at most 2^22)
+  const pf_u32x4 rs_w = pf_rsrc(p.w + feat0 * p.w_stride, (min(256, p.n - feat0) - 1u) * ldw + p.k);
+  const pf_u32x4 rs_x = pf_rsrc(p.x + tok0 * p.x_stride, (min(256, p.m - tok0) - 1u) * ldx + p.k);
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(PF_LDS_AS(unsigned char, smem)));
+  // request i of thirty-two per tile fills rows 8i .. 8i + 7, wave w has i = w + 8 part; chunk c of row r at c ^ (r / 2) % 8
+  const int chunk = (lane & 7) ^ ((4 * wave + (lane >> 4)) & 7);
+  const uint32_t w_off = static_cast<uint32_t>(lane >> 3) * ldw + chunk * 16, x_off = static_cast<uint32_t>(lane >> 3) * ldx + chunk * 16;
+  auto issue = [&](int step, int st, int part) __attribute__((always_inline)) {
+    const int i = wave + 8 * part;
+    const uint32_t dst = lds0 + st * STAGE + i * 1024;
+    const bool in = step * BK + chunk * 16 < p.k;  // (behind the last column: zeros)
+    pf_load16_to_lds(rs_w, dst, in ? w_off : kPfOob, 8u * i * ldw + step * BK);
+    pf_load16_to_lds(rs_x, dst + TILE, in ? x_off : kPfOob, 8u * i * ldx + step * BK);
+  };
+  const int n_steps = (p.k + BK - 1) / BK;
+#pragma unroll
+  for (int part = 0; part < 4; ++part) issue(0, 0, part);
+  const int pre = l32 * BK + (((l32 >> 1) & 7) << 4);
+  const int fbase = 4 * wr, tbase = 2 * wc;
+  i32x16 acc[4][2];
+#pragma unroll
+  for (int a = 0; a < 4; ++a)
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[a][b][i] = 0;
+  // the tiles have landed, everybody is done with the other stage; the requests of the next step go out beside the products of the first
+  // two slices, the operands of a slice are read under the products of the one before
+  auto k_step = [&](int step, auto st_c, bool more) __attribute__((always_inline)) {
+    constexpr int ST = decltype(st_c)::value;
+    constexpr int KS = BK / 32;
+    pf_wait_vm0();
+    __syncthreads();
+    const unsigned char* wt = smem + ST * STAGE + fbase * 32 * BK;
+    const unsigned char* xt = smem + ST * STAGE + TILE + tbase * 32 * BK;
+    i32x4 a[2][4], b[2][2];
+    auto read_slice = [&](int ks, int buf) __attribute__((always_inline)) {
+      const int off = pre ^ ((2 * ks + g2) << 4);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) b[buf][j] = *reinterpret_cast<const i32x4*>(xt + off + j * 32 * BK);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[buf][i] = *reinterpret_cast<const i32x4*>(wt + off + i * 32 * BK);
+    };
+    read_slice(0, 0);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const int cur = ks & 1;
+      __builtin_amdgcn_sched_barrier(0);
+      if (more && ks < 2) {
+        issue(step + 1, ST ^ 1, 2 * ks);
+        issue(step + 1, ST ^ 1, 2 * ks + 1);
+      }
+      if (ks + 1 < KS) read_slice(ks + 1, cur ^ 1);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(a[cur][i], b[cur][j], acc[i][j], 0, 0, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  for (int step = 0; step < n_steps; step += 2) {
+    k_step(step, std::integral_constant<int, 0>{}, step + 1 < n_steps);
+    if (step + 1 < n_steps) k_step(step + 1, std::integral_constant<int, 1>{}, step + 2 < n_steps);
+  }
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int a = 0; a < 4; ++a) {
+      const int f0 = feat0 + 32 * (fbase + a);
+      if (f0 < p.n) store_block<T>(p, acc[a][b], tok0 + 32 * (tbase + b) + l32, f0, g2);
+    }
+}
+
+// Rows too far apart for the other kernels' offsets: a wave per 16 features and 16 tokens, operands straight from memory.
+template <typename T>
+__global__ __launch_bounds__(256) void matmul_i8_far_kernel(I8Params p) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l16 = lane & 15, g = lane >> 4;
+  const int j0 = (static_cast<int>(blockIdx.x) * 4 + wave) * 16;
   if (j0 >= p.n) return;
   const int8_t* wr = p.w + min(j0 + l16, p.n - 1) * p.w_stride + 16 * g;
-  const int8_t* xr = p.x + min(i0 + l16, p.m - 1) * p.x_stride + 16 * g;
-  i32x4 acc = {0, 0, 0, 0};
-  for (int c = 0; c < p.k; c += 64) {
-    i32x4 a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
-    if (c + 16 * g < p.k) {
-      a = *reinterpret_cast<const i32x4*>(wr + c);
-      b = *reinterpret_cast<const i32x4*>(xr + c);
+  for (int i0 = static_cast<int>(blockIdx.y) * 16; i0 < p.m; i0 += gridDim.y * 16) {
+    const int8_t* xr = p.x + min(i0 + l16, p.m - 1) * p.x_stride + 16 * g;
+    i32x4 acc = {0, 0, 0, 0};
+    for (int c = 0; c < p.k; c += 64) {
+      i32x4 a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
+      if (c + 16 * g < p.k) {
+        a = *reinterpret_cast<const i32x4*>(wr + c);
+        b = *reinterpret_cast<const i32x4*>(xr + c);
+      }
+      acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, acc, 0, 0, 0);
     }
-    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, acc, 0, 0, 0);
-  }
-  // register e: feature j0 + 4g + e of token i0 + l16
-  const int i = i0 + l16;
-  if (i >= p.m) return;
+    const int i = i0 + l16;
+    if (i >= p.m) continue;
 #pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (j0 + 4 * g + e < p.n) store_scaled<T>(p, i, j0 + 4 * g + e, acc[e]);
+    for (int e = 0; e < 4; ++e)
+      if (j0 + 4 * g + e < p.n) store_scaled<T>(p, i, j0 + 4 * g + e, acc[e]);
+  }
+}
+
+template <typename T>
+static void launch_matmul(const I8Params& p, hipStream_t s) {
+  constexpr int64_t kNear = int64_t{1} << 22;  // 256 rows within 32-bit offsets below the one that stands for "outside"
+  if (p.m <= 64) {
+    const dim3 grid((p.n + 15) / 16);
+    if (p.m <= 16) hipLaunchKernelGGL((matmul_i8_stream_kernel<T, 1>), grid, dim3(512), 0, s, p);
+    else if (p.m <= 32) hipLaunchKernelGGL((matmul_i8_stream_kernel<T, 2>), grid, dim3(512), 0, s, p);
+    else hipLaunchKernelGGL((matmul_i8_stream_kernel<T, 4>), grid, dim3(512), 0, s, p);
+    return;
+  }
+  if (p.x_stride > kNear || p.w_stride > kNear) {
+    hipLaunchKernelGGL((matmul_i8_far_kernel<T>), dim3((p.n + 63) / 64, min((p.m + 15) / 16, 65535)), dim3(256), 0, s, p);
+    return;
+  }
+  const int64_t wide = static_cast<int64_t>((p.m + 255) / 256) * ((p.n + 255) / 256), quarter = static_cast<int64_t>((p.m + 63) / 64) * ((p.n + 63) / 64);
+  if (wide >= 128) hipLaunchKernelGGL((matmul_i8_wide_kernel<T>), dim3(static_cast<unsigned>((wide + 7) / 8 * 8)), dim3(512), 0, s, p);
+  else hipLaunchKernelGGL((matmul_i8_quarter_kernel<T>), dim3(static_cast<unsigned>((quarter + 7) / 8 * 8)), dim3(512), 0, s, p);
 }
 
 }  // namespace lra
@@ -159,10 +416,8 @@ lra_status lra_matmul_i8(const lra_i8_operands* ops, void* y, int32_t dtype, int
   (void)workspace, (void)workspace_bytes;
   const I8Params p{ops->x, ops->w, ops->x_scale, ops->w_scale, y, ops->x_stride, ops->w_stride, y_stride, ops->m, ops->n, ops->k};
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const dim3 grid((ops->n + 63) / 64, (ops->m + 15) / 16);
-  if (grid.y > 65535) return LRA_ERR_UNSUPPORTED;
-  if (dtype == LRA_BF16) hipLaunchKernelGGL((matmul_i8_kernel<bf16_t>), grid, dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((matmul_i8_kernel<float>), grid, dim3(256), 0, s, p);
+  if (dtype == LRA_BF16) launch_matmul<bf16_t>(p, s);
+  else launch_matmul<float>(p, s);
   return hipGetLastError() == hipSuccess ? LRA_OK : LRA_ERR_HIP;
 }
 
