@@ -89,7 +89,8 @@ typedef struct {
  * belongs to one sequence (blocks that are full may be shared).  Calling again with the same rows changes nothing.
  * K and V must be finite: a value that is not makes the block's rows of that head unspecified.
  * Nothing is written for a sequence whose device-side length exceeds max_seq_len; tokens before the sequence's first (c_t
- * larger than its length) and blocks whose table entry is out of range are passed over.
+ * larger than its length) and blocks whose table entry is out of range are passed over.  More than 2^31 (block with new tokens,
+ * pair of kv heads) of a sequence are LRA_ERR_UNSUPPORTED, and so are as many (sixteen rows, pair) in lra_cache8_gather.
  */
 lra_status lra_cache8_append(const lra_shape* shape, const lra_cache8* cache, const lra_new_rows* rows, void* stream);
 

@@ -64,13 +64,6 @@ __device__ __forceinline__ uint4 codes_to_values(uint32_t lo, uint32_t hi, float
   }
 }
 
-// Byte masks of the sixteen tokens from j0 on, four to a word: ones for those below n and outside [cut_lo, cut_hi).
-__device__ __forceinline__ uint4 token_masks(int j0, int n, int cut_lo, int cut_hi) {
-  auto below = [](int k) __attribute__((always_inline)) -> uint32_t { return (1u << min(max(k, 0), 16)) - 1u; };
-  const uint32_t bits = below(n - j0) & ~(below(cut_hi - j0) & ~below(cut_lo - j0));
-  auto word = [&](int c) __attribute__((always_inline)) -> uint32_t { return (((bits >> (4 * c)) & 15u) * 0x00204081u & 0x01010101u) * 255u; };
-  return make_uint4(word(0), word(1), word(2), word(3));
-}
 __device__ __forceinline__ uint4 masked(uint4 v, uint4 m) { return make_uint4(v.x & m.x, v.y & m.y, v.z & m.z, v.w & m.w); }
 
 // RT: row tiles of a workgroup (1, 2 or 4).

@@ -1,4 +1,6 @@
 // The cache of 8-bit codes: new rows written into it, rows read back (declarations and contracts in lra_attn8.h).
+#include <cmath>
+
 #include "lra_attn8_plan.h"
 #include "lra_codes.h"
 
@@ -10,10 +12,20 @@ struct Append8Params {
   void* lc;
   const int32_t *block_table, *seq_lens, *seq_start, *positions;
   int64_t k_token_stride, v_token_stride, l_token_stride, kv_block_stride, kv_head_stride, scale_block_stride, l_row_stride;
-  int64_t items;
-  int32_t n_kv_heads, rank, n_seqs, max_seq_len, max_blocks_per_seq, num_blocks, n_new, blocks_per_seq;
-  float rope_theta;
+  uint32_t places;  // (block with new tokens, pair of kv heads) of a sequence
+  int32_t n_kv_heads, rank, n_seqs, max_seq_len, max_blocks_per_seq, num_blocks, n_new;
+  int32_t rotate;
+  double first_rate, rate_powers[6];  // turns per position of pair 0; theta^(-2^(i+1) / d), i < 6
 };
+
+// Turns per position of pair i < 64: theta^(-2i / d) / 2 pi, from the powers that i's bits select.  (Left to the device's exp2 and log2
+// in double precision, the rates took longer than the angles.)
+__device__ __forceinline__ double rate_of(const Append8Params& p, int i) {
+  double r = p.first_rate;
+#pragma unroll
+  for (int b = 0; b < 6; ++b) r *= i >> b & 1 ? p.rate_powers[b] : 1.0;
+  return r;
+}
 
 __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
 #pragma unroll
@@ -91,14 +103,15 @@ __global__ __launch_bounds__(256) void cache8_append_kernel(Append8Params p) {
   __shared__ float2 turn[16][H];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int pairs = (p.n_kv_heads + 1) / 2;
-  for (int64_t item = blockIdx.x; item < p.items; item += gridDim.x) {
-    const int pair = static_cast<int>(item % pairs);
-    const int64_t rest = item / pairs;
-    const int t = static_cast<int>(rest / p.blocks_per_seq), bi = static_cast<int>(rest - static_cast<int64_t>(t) * p.blocks_per_seq);
-    const int n = p.seq_lens[t];
-    const int c0 = t > 0 ? min(max(p.seq_start[t], 0), p.n_new) : 0;
-    const int c1 = t + 1 < p.n_seqs ? min(max(p.seq_start[t + 1], c0), p.n_new) : p.n_new;
+  const uint32_t pairs = static_cast<uint32_t>(p.n_kv_heads + 1) / 2;
+  const double rate = p.rotate ? rate_of(p, tid % H) : 0.0;
+  for (int t = blockIdx.y; t < p.n_seqs; t += gridDim.y)
+  for (uint32_t place = blockIdx.x; place < p.places; place += gridDim.x) {
+    const int bi = static_cast<int>(place / pairs), pair = static_cast<int>(place - static_cast<uint32_t>(bi) * pairs);
+    // (three requests, one round trip)
+    const int n = p.seq_lens[t], at = p.seq_start[t], end = p.seq_start[t + 1];
+    const int c0 = t > 0 ? min(max(at, 0), p.n_new) : 0;
+    const int c1 = t + 1 < p.n_seqs ? min(max(end, c0), p.n_new) : p.n_new;
     if (n > p.max_seq_len || c1 <= c0) continue;
     const int first = n - (c1 - c0);  // (negative: rows before the sequence)
     const int b = (max(first, 0) >> 4) + bi, j0 = b * 16;
@@ -107,8 +120,7 @@ __global__ __launch_bounds__(256) void cache8_append_kernel(Append8Params p) {
     if (id < 0 || id >= p.num_blocks) continue;
     const int lo = max(first - j0, 0), hi = min(16, n - j0);  // slots [0, lo) are held already, [lo, hi) are new
     const int row0 = c0 + j0 - first;                          // row of slot 0
-    if (p.rope_theta > 0.f) {
-      const double rate = rope_rate_rev(tid % H, D, p.rope_theta);
+    if (p.rotate) {
       for (int s = tid / H; s < hi; s += 256 / H)
         if (s >= lo) {
           const int pos = p.positions ? p.positions[row0 + s] : j0 + s;
@@ -126,47 +138,52 @@ __global__ __launch_bounds__(256) void cache8_append_kernel(Append8Params p) {
       if (wave < 2) {
         const int s = lane >> 2, part = (lane & 3) * PP;
         const bool fresh = s >= lo && s < hi;
+        // (slots that get no row: the nearest that does, zeroed; everything is requested before anything is waited for)
+        const T* src = static_cast<const T*>(p.k) + (row0 + min(max(s, lo), hi - 1)) * p.k_token_stride + static_cast<int64_t>(h) * D + part;
+        uint8_t* const dst = p.kc + off + s * D + part;
         float x[PP], y[PP];
+        load_values<T, PP>(src, x);
+        load_values<T, PP>(src + H, y);
+        uint32_t wx[PP / 4], wy[PP / 4];  // codes of earlier tokens
+        int had = 0;
+        if (lo > 0) {
+          had = p.k_scale[soff];
 #pragma unroll
-        for (int i = 0; i < PP; ++i) x[i] = y[i] = 0.f;
-        uint32_t most = 0;
-        if (fresh) {
-          const T* src = static_cast<const T*>(p.k) + (row0 + s) * p.k_token_stride + static_cast<int64_t>(h) * D + part;
-          load_values<T, PP>(src, x);
-          load_values<T, PP>(src + H, y);
+          for (int i = 0; i < PP / 4; ++i) wx[i] = reinterpret_cast<const uint32_t*>(dst)[i], wy[i] = reinterpret_cast<const uint32_t*>(dst + H)[i];
+        }
+        if (p.rotate) {
 #pragma unroll
           for (int i = 0; i < PP; ++i) {
-            if (p.rope_theta > 0.f) {
-              const float2 cs = turn[s][part + i];
-              const float a = x[i], c = y[i];
-              // (each product rounded, as the definition has it, and not one of the two fused into the difference)
-              x[i] = __fsub_rn(__fmul_rn(a, cs.x), __fmul_rn(c, cs.y));
-              y[i] = __fadd_rn(__fmul_rn(c, cs.x), __fmul_rn(a, cs.y));
-            }
-            most = max(most, max(__float_as_uint(x[i]) & 0x7fffffffu, __float_as_uint(y[i]) & 0x7fffffffu));
+            const float2 cs = turn[s][part + i];  // (of slots that get no row: anything)
+            const float a = x[i], c = y[i];
+            // (each product rounded, as the definition has it, and not one of the two fused into the difference)
+            x[i] = __fsub_rn(__fmul_rn(a, cs.x), __fmul_rn(c, cs.y));
+            y[i] = __fadd_rn(__fmul_rn(c, cs.x), __fmul_rn(a, cs.y));
           }
         }
-        uint8_t* dst = p.kc + off + s * D + part;
-        const int had = lo > 0 ? p.k_scale[soff] : 0;
-        const int e = block_scale<CODE>(most, lo > 0, had);
-        uint32_t cx[PP / 4], cy[PP / 4];
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < PP; ++i) most = max(most, max(__float_as_uint(x[i]) & 0x7fffffffu, __float_as_uint(y[i]) & 0x7fffffffu));
+        const int e = block_scale<CODE>(fresh ? most : 0u, lo > 0, had);
         const bool anew = s < lo && e != had;
-        if (anew) {
+        int by = 127 - e;
+        if (lo > 0) {  // (uniform)
+          if (s < lo) by = had - e;
 #pragma unroll
           for (int i = 0; i < PP / 4; ++i) {
             float u[4], w[4];
-            decode4<CODE>(reinterpret_cast<const uint32_t*>(dst)[i], u);
-            decode4<CODE>(reinterpret_cast<const uint32_t*>(dst + H)[i], w);
+            decode4<CODE>(wx[i], u);
+            decode4<CODE>(wy[i], w);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) x[4 * i + c] = ldexpf(u[c], had - e), y[4 * i + c] = ldexpf(w[c], had - e);
+            for (int c = 0; c < 4; ++c) x[4 * i + c] = s < lo ? u[c] : x[4 * i + c], y[4 * i + c] = s < lo ? w[c] : y[4 * i + c];
           }
-        } else {
-#pragma unroll
-          for (int i = 0; i < PP; ++i) x[i] = ldexpf(x[i], 127 - e), y[i] = ldexpf(y[i], 127 - e);
         }
+        uint32_t cx[PP / 4], cy[PP / 4];
 #pragma unroll
         for (int i = 0; i < PP / 4; ++i) {
-          const float u[4] = {x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]}, w[4] = {y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]};
+          float u[4], w[4];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) u[c] = ldexpf(x[4 * i + c], by), w[c] = ldexpf(y[4 * i + c], by);
           cx[i] = encode4<CODE>(u), cy[i] = encode4<CODE>(w);
         }
         if (fresh || anew) {
@@ -181,49 +198,60 @@ __global__ __launch_bounds__(256) void cache8_append_kernel(Append8Params p) {
         if (lane == 0) p.k_scale[soff] = static_cast<uint8_t>(e);
       } else {
         const T* src = static_cast<const T*>(p.v) + row0 * p.v_token_stride + static_cast<int64_t>(h) * D + lane * DV;
+        uint4* const dst = reinterpret_cast<uint4*>(p.vc + off + lane * DV * 16);
         float x[16][DV];
-        uint32_t most = 0;
 #pragma unroll
-        for (int s = 0; s < 16; ++s) {
+        for (int s = 0; s < 16; ++s) load_values<T, DV>(src + min(max(s, lo), hi - 1) * p.v_token_stride, x[s]);
+        uint4 was[DV];
+        int had = 0;
+        if (lo > 0 || hi < 16) {
+          if (lo > 0) had = p.v_scale[soff];
 #pragma unroll
-          for (int c = 0; c < DV; ++c) x[s][c] = 0.f;
-          if (s >= lo && s < hi) load_values<T, DV>(src + s * p.v_token_stride, x[s]);
+          for (int c = 0; c < DV; ++c) was[c] = dst[c];
+        } else {
+#pragma unroll
+          for (int c = 0; c < DV; ++c) was[c] = make_uint4(0u, 0u, 0u, 0u);
+        }
+        uint32_t most = 0;  // (rows requested twice count once)
+#pragma unroll
+        for (int s = 0; s < 16; ++s)
 #pragma unroll
           for (int c = 0; c < DV; ++c) most = max(most, __float_as_uint(x[s][c]) & 0x7fffffffu);
-        }
-        const int had = lo > 0 ? p.v_scale[soff] : 0;
         const int e = block_scale<CODE>(most, lo > 0, had);
+        // bytes from the first that changes to hi (earlier tokens keep their codes where the scale stays)
+        const uint4 mask = byte_masks(((1u << hi) - 1u) & ~((1u << (e != had ? 0 : lo)) - 1u));
+        const uint32_t ms[4] = {mask.x, mask.y, mask.z, mask.w};
 #pragma unroll
         for (int c = 0; c < DV; ++c) {
-          uint4* dst = reinterpret_cast<uint4*>(p.vc + off + (lane * DV + c) * 16);
-          uint32_t was[4] = {0u, 0u, 0u, 0u};
-          if (lo > 0 || hi < 16) {
-            const uint4 w = *dst;
-            was[0] = w.x, was[1] = w.y, was[2] = w.z, was[3] = w.w;
-          }
+          const uint32_t old[4] = {was[c].x, was[c].y, was[c].z, was[c].w};
           uint32_t out[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            float u[4], z[4];
-            decode4<CODE>(was[i], u);
+            float z[4];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) z[q] = 4 * i + q < lo ? ldexpf(u[q], had - e) : ldexpf(x[4 * i + q][c], 127 - e);
-            const uint32_t now = encode4<CODE>(z);
-            // bytes from the first that changes to hi (earlier tokens keep their codes where the scale stays)
-            const int f = min(max((e != had ? 0 : lo) - 4 * i, 0), 4), g = min(max(hi - 4 * i, 0), 4);
-            const uint32_t mask = g <= f ? 0u : (g == 4 ? 0xffffffffu : (1u << (8 * g)) - 1u) & (f == 0 ? 0xffffffffu : f == 4 ? 0u : ~((1u << (8 * f)) - 1u));
-            out[i] = (now & mask) | (was[i] & ~mask);
+            for (int q = 0; q < 4; ++q) z[q] = ldexpf(x[4 * i + q][c], 127 - e);
+            if (lo > 4 * i) {  // (uniform)
+              float u[4];
+              decode4<CODE>(old[i], u);
+#pragma unroll
+              for (int q = 0; q < 4; ++q) z[q] = 4 * i + q < lo ? ldexpf(u[q], had - e) : z[q];
+            }
+            out[i] = (encode4<CODE>(z) & ms[i]) | (old[i] & ~ms[i]);
           }
-          *dst = make_uint4(out[0], out[1], out[2], out[3]);
+          dst[c] = make_uint4(out[0], out[1], out[2], out[3]);
         }
         if (lane == 0) p.v_scale[soff] = static_cast<uint8_t>(e);
       }
     }
     if (pair == 0 && p.l != nullptr) {
-      const int r = p.rank, cnt = (hi - lo) * r;
-      for (int i = tid; i < cnt; i += 256) {
-        const int s = lo + i / r, c = i - i / r * r;
-        static_cast<T*>(p.lc)[(static_cast<int64_t>(id) * 16 + s) * p.l_row_stride + c] = static_cast<const T*>(p.l)[(row0 + s) * p.l_token_stride + c];
+      const int c = min(lane, p.rank - 1);
+      T x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = static_cast<const T*>(p.l)[(row0 + min(max(4 * i + wave, lo), hi - 1)) * p.l_token_stride + c];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int s = 4 * i + wave;
+        if (s >= lo && s < hi && lane < p.rank) static_cast<T*>(p.lc)[(static_cast<int64_t>(id) * 16 + s) * p.l_row_stride + c] = x[i];
       }
     }
     __syncthreads();  // (the angles of the next item)
@@ -237,8 +265,8 @@ struct Gather8Params {
   int64_t kv_block_stride, kv_head_stride, scale_block_stride, l_row_stride, kept_stride;
   int32_t max_blocks_per_seq, num_blocks, max_seq_len;
   Params dst;  // k_base, v_base, l and their layout, seq_lens, max_seq_len, n_kv_heads, rank
-  int64_t items;
-  int32_t units;  // of sixteen rows, per sequence
+  uint32_t places;  // (sixteen rows, pair of kv heads) of a sequence
+  int32_t n_seqs;
 };
 
 template <typename T, int N>
@@ -264,36 +292,47 @@ __global__ __launch_bounds__(256) void cache8_gather_kernel(Gather8Params p) {
   constexpr int PK = D / 4, DV = D / 64;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int Hkv = p.dst.n_kv_heads, pairs = (Hkv + 1) / 2;
-  for (int64_t item = blockIdx.x; item < p.items; item += gridDim.x) {
-    const int pair = static_cast<int>(item % pairs);
-    const int64_t rest = item / pairs;
-    const int t = static_cast<int>(rest / p.units), i0 = 16 * static_cast<int>(rest - static_cast<int64_t>(t) * p.units);
-    const int m = min(p.dst.seq_lens[t], p.dst.max_seq_len), n = min(p.seq_lens[t], p.max_seq_len);
+  const int Hkv = p.dst.n_kv_heads;
+  const uint32_t pairs = static_cast<uint32_t>(Hkv + 1) / 2;
+  for (int t = blockIdx.y; t < p.n_seqs; t += gridDim.y)
+  for (uint32_t place = blockIdx.x; place < p.places; place += gridDim.x) {
+    const uint32_t unit = place / pairs;
+    const int pair = static_cast<int>(place - unit * pairs), i0 = static_cast<int>(unit) * 16;
+    const int m_all = p.dst.seq_lens[t], n_all = p.seq_lens[t];
+    const int dst_id = p.dst.block_size == 0 ? 0 : p.dst.block_table[static_cast<int64_t>(t) * p.dst.max_blocks_per_seq + static_cast<int>(unit)];
+    const int m = min(m_all, p.dst.max_seq_len), n = min(n_all, p.max_seq_len);
     if (i0 >= m) continue;
+    // (the sixteen rows lie in one block of dst; looked up row by row, behind the stores, the ids took most of the kernel's time)
+    const int64_t dst_block = dst_id;
+    const int64_t kv_base = p.dst.block_size == 0 ? i0 * p.dst.kv_token_stride : dst_block * p.dst.kv_block_stride;
+    const int64_t l_base = (p.dst.block_size == 0 ? i0 : dst_block * 16) * p.dst.l_row_stride;
     // row s of the sixteen: its source token, negative where there is none, and the block of that
     const int row = i0 + (lane & 15);
-    int tok = row < m ? (p.kept ? p.kept[static_cast<int64_t>(t) * p.kept_stride + row] : row + n - p.dst.seq_lens[t]) : -1;
+    int tok = row < m ? (p.kept ? p.kept[static_cast<int64_t>(t) * p.kept_stride + row] : row + n - m_all) : -1;
     if (tok >= n) tok = -1;
     int id = 0;
     if (tok >= 0) {
       id = block8(p.block_table, p.max_blocks_per_seq, t, tok >> 4);
-      if (id < 0 || id >= p.num_blocks) tok = -1;
+      if (id < 0 || id >= p.num_blocks) tok = -1, id = 0;
     }
     const int h = 2 * pair + (wave & 1);
     if (h < Hkv) {
+      // (the scale of this lane's row: one request for the sixteen)
+      const int scale_byte = (wave < 2 ? p.k_scale : p.v_scale)[id * p.scale_block_stride + h];
       const int64_t hoff = static_cast<int64_t>(h) * p.kv_head_stride;
       if (wave < 2) {
         const int s = lane >> 2, part = (lane & 3) * PK;
-        const int j = __shfl(tok, s, kWave), blk = __shfl(id, s, kWave);
+        const int j = __shfl(tok, s, kWave), blk = __shfl(id, s, kWave);  // (a row without a source: block 0, of which nothing is stored)
+        const uint4* src = reinterpret_cast<const uint4*>(p.kc + blk * p.kv_block_stride + hoff + (j & 15) * D + part);
+        uint4 v[PK / 16];
+#pragma unroll
+        for (int i = 0; i < PK / 16; ++i) v[i] = src[i];
+        const float sc = scale8(__shfl(scale_byte, s, kWave));
+        T* dst = static_cast<T*>(const_cast<void*>(p.dst.k_base)) + kv_base + s * p.dst.kv_token_stride + h * p.dst.kv_head_stride + part;
         if (j >= 0) {
-          const uint4* src = reinterpret_cast<const uint4*>(p.kc + blk * p.kv_block_stride + hoff + (j & 15) * D + part);
-          const float sc = scale8(p.k_scale[blk * p.scale_block_stride + h]);
-          T* dst = static_cast<T*>(const_cast<void*>(p.dst.k_base)) + kv_offset(p.dst, t, i0 + s, h) + part;
 #pragma unroll
           for (int i = 0; i < PK / 16; ++i) {
-            const uint4 v = src[i];
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
             float x[16];
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
@@ -306,32 +345,50 @@ __global__ __launch_bounds__(256) void cache8_gather_kernel(Gather8Params p) {
           }
         }
       } else {
+        // sixteen tokens of a lane's dimensions for every row (rows of one block: from the cache near the unit), of which one byte
+        // counts; eight rows at a time
+        T* const dst = static_cast<T*>(const_cast<void*>(p.dst.v_base)) + kv_base + h * p.dst.kv_head_stride + lane * DV;
+#pragma unroll 1
+        for (int s0 = 0; s0 < 16; s0 += 8) {
+          uint4 v[8][DV];
 #pragma unroll
-        for (int s = 0; s < 16; ++s) {
-          const int j = __builtin_amdgcn_readlane(tok, s), blk = __builtin_amdgcn_readlane(id, s);
-          if (j < 0) continue;
-          const uint8_t* src = p.vc + blk * p.kv_block_stride + hoff + lane * DV * 16 + (j & 15);
-          const float sc = scale8(p.v_scale[blk * p.scale_block_stride + h]);
-          float x[DV];
+          for (int q = 0; q < 8; ++q) {
+            const int blk = __builtin_amdgcn_readlane(id, s0 + q);
+            const uint4* src = reinterpret_cast<const uint4*>(p.vc + blk * p.kv_block_stride + hoff) + lane * DV;
 #pragma unroll
-          for (int c = 0; c < DV; ++c) {
-            float u[4];
-            decode4<CODE>(src[c * 16], u);
-            x[c] = u[0] * sc;
+            for (int c = 0; c < DV; ++c) v[q][c] = src[c];
           }
-          store_values<T, DV>(static_cast<T*>(const_cast<void*>(p.dst.v_base)) + kv_offset(p.dst, t, i0 + s, h) + lane * DV, x);
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            const int j = __builtin_amdgcn_readlane(tok, s0 + q);
+            if (j < 0) continue;
+            const float sc = scale8(__builtin_amdgcn_readlane(scale_byte, s0 + q));
+            float x[DV];
+#pragma unroll
+            for (int c = 0; c < DV; ++c) {
+              const uint32_t four = j & 8 ? (j & 4 ? v[q][c].w : v[q][c].z) : (j & 4 ? v[q][c].y : v[q][c].x);
+              float u[4];
+              decode4<CODE>(four >> (8 * (j & 3)), u);
+              x[c] = u[0] * sc;
+            }
+            store_values<T, DV>(dst + (s0 + q) * p.dst.kv_token_stride, x);
+          }
         }
       }
     }
     if (pair == 0) {
-      const int r = p.dst.rank;
-      for (int i = tid; i < 16 * 64; i += 256) {
-        const int s = i >> 6, c = i & 63;
-        const int j = __shfl(tok, s, kWave), blk = __shfl(id, s, kWave);
-        if (j < 0 || c >= r) continue;
-        static_cast<T*>(const_cast<void*>(p.dst.l))[l_offset(p.dst, t, i0 + s, 0) + c] =
-            static_cast<const T*>(p.lc)[(static_cast<int64_t>(blk) * 16 + (j & 15)) * p.l_row_stride + c];
+      const int r = p.dst.rank, c = min(lane, r - 1);
+      T x[4];
+      int js[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int s = 4 * i + wave, blk = __shfl(id, s, kWave);
+        js[i] = __shfl(tok, s, kWave);
+        x[i] = static_cast<const T*>(p.lc)[(static_cast<int64_t>(blk) * 16 + (js[i] & 15)) * p.l_row_stride + c];
       }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (js[i] >= 0 && lane < r) static_cast<T*>(const_cast<void*>(p.dst.l))[l_base + (4 * i + wave) * p.dst.l_row_stride + c] = x[i];
     }
   }
 }
@@ -350,7 +407,14 @@ static void by_type(const lra_shape* sh, int code, F launch) {
   else with_dim(float{});
 }
 
-constexpr int64_t kMostWorkgroups = 1 << 20;  // (further items in turns)
+// The grid of `units` by pairs of kv heads (x) and sequences (y), what is beyond its bounds in turns; false: too many for 32 bits.
+static bool place_grid(int64_t units, int n_kv_heads, int n_seqs, uint32_t& places, dim3& grid) {
+  const int64_t n = units * ((n_kv_heads + 1) / 2);
+  if (n > (int64_t{1} << 31)) return false;
+  places = static_cast<uint32_t>(n);
+  grid = dim3(static_cast<unsigned>(n < (1 << 20) ? n : (1 << 20)), n_seqs < 4096 ? n_seqs : 4096);
+  return true;
+}
 
 }  // namespace lra
 
@@ -388,12 +452,15 @@ lra_status lra_cache8_append(const lra_shape* shape, const lra_cache8* cache, co
   p.max_blocks_per_seq = cache->max_blocks_per_seq;
   p.num_blocks = cache->num_blocks;
   p.n_new = rows->n_new;
-  p.rope_theta = rows->rope_theta;
+  p.rotate = rows->rope_theta > 0.f;
+  if (p.rotate) {
+    p.first_rate = 0.15915494309189533577;  // 1 / 2 pi
+    for (int i = 0; i < 6; ++i) p.rate_powers[i] = std::pow(static_cast<double>(rows->rope_theta), -2.0 * (1 << i) / shape->head_dim);
+  }
   // c tokens touch (c + 30) / 16 blocks at most
   const int most = rows->max_new_per_seq < cache->max_seq_len ? rows->max_new_per_seq : cache->max_seq_len;
-  p.blocks_per_seq = static_cast<int32_t>((static_cast<int64_t>(most) + 30) / 16);
-  p.items = static_cast<int64_t>(cache->n_seqs) * p.blocks_per_seq * ((shape->n_kv_heads + 1) / 2);
-  const dim3 grid(static_cast<unsigned>(p.items < kMostWorkgroups ? p.items : kMostWorkgroups));
+  dim3 grid;
+  if (!place_grid((static_cast<int64_t>(most) + 30) / 16, shape->n_kv_heads, cache->n_seqs, p.places, grid)) return LRA_ERR_UNSUPPORTED;
   hipStream_t s = static_cast<hipStream_t>(stream);
   by_type(shape, cache->code, [&](auto t_c, auto d_c, auto code_c) {
     hipLaunchKernelGGL((cache8_append_kernel<decltype(t_c), decltype(d_c)::value, decltype(code_c)::value>), grid, dim3(256), 0, s, p);
@@ -442,9 +509,9 @@ lra_status lra_cache8_gather(const lra_shape* shape, const lra_cache8* src, cons
   p.dst.l_row_stride = dst->l_row_stride ? dst->l_row_stride : shape->rank;
   p.dst.n_kv_heads = shape->n_kv_heads;
   p.dst.rank = shape->rank;
-  p.units = static_cast<int32_t>((static_cast<int64_t>(dst->max_seq_len) + 15) / 16);
-  p.items = static_cast<int64_t>(dst->n_seqs) * p.units * ((shape->n_kv_heads + 1) / 2);
-  const dim3 grid(static_cast<unsigned>(p.items < kMostWorkgroups ? p.items : kMostWorkgroups));
+  p.n_seqs = dst->n_seqs;
+  dim3 grid;
+  if (!place_grid((static_cast<int64_t>(dst->max_seq_len) + 15) / 16, shape->n_kv_heads, dst->n_seqs, p.places, grid)) return LRA_ERR_UNSUPPORTED;
   hipStream_t s = static_cast<hipStream_t>(stream);
   by_type(shape, src->code, [&](auto t_c, auto d_c, auto code_c) {
     hipLaunchKernelGGL((cache8_gather_kernel<decltype(t_c), decltype(d_c)::value, decltype(code_c)::value>), grid, dim3(256), 0, s, p);

@@ -19,9 +19,11 @@ __device__ __forceinline__ int block8(const int32_t* table, int max_blocks_per_s
   return table ? table[static_cast<int64_t>(t) * max_blocks_per_seq + b] : b;
 }
 
-// 2^(s - 127); 255 is not a number, 0 the denormal 2^-127
+// 2^(s - 127); 255 is not a number, 0 the denormal 2^-127: the exponent field, and the upper mantissa bit for those two.  (Without a
+// branch: behind one, every load of a scale was waited for by itself.)
 __device__ __forceinline__ float scale8(int s) {
-  return s == 255 ? __uint_as_float(0x7fc00000u) : (s == 0 ? __uint_as_float(0x00400000u) : __uint_as_float(static_cast<uint32_t>(s) << 23));
+  const uint32_t u = static_cast<uint32_t>(s);
+  return __uint_as_float(u << 23 | (((u + 1u) & 255u) < 2u ? 0x00400000u : 0u));
 }
 
 // Exponent byte of the least power of two (2^-126 at least) that brings a value with these bits (sign cleared) to 448 = 1.75 x 2^8
@@ -31,6 +33,17 @@ __device__ __forceinline__ int least_scale8(uint32_t bits) {
   if (bits >= 0x7f800000u) return 255;
   const int e = CODE == LRA_E4M3 ? static_cast<int>((bits + 0x1fffffu) >> 23) - 8 : static_cast<int>((bits + 0x01ffffu) >> 23) - 6;
   return max(e, 1);
+}
+
+// Sixteen bits as byte masks, four to a word.
+__device__ __forceinline__ uint4 byte_masks(uint32_t bits) {
+  auto word = [&](int c) __attribute__((always_inline)) -> uint32_t { return (((bits >> (4 * c)) & 15u) * 0x00204081u & 0x01010101u) * 255u; };
+  return make_uint4(word(0), word(1), word(2), word(3));
+}
+// ... of the sixteen tokens from j0 on: ones for those below n and outside [cut_lo, cut_hi).
+__device__ __forceinline__ uint4 token_masks(int j0, int n, int cut_lo, int cut_hi) {
+  auto below = [](int k) __attribute__((always_inline)) -> uint32_t { return (1u << min(max(k, 0), 16)) - 1u; };
+  return byte_masks(below(n - j0) & ~(below(cut_hi - j0) & ~below(cut_lo - j0)));
 }
 
 // The four codes of a word as floats.
