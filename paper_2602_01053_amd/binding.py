@@ -1,4 +1,4 @@
-"""Thin binding over liblra_attn.so (ctypes; the three per-layer entry points through a CPython module of
+"""Thin binding over liblra_attn.so (ctypes; the per-layer entry points through a CPython module of
 their own, csrc/lra_pycall.cpp, where it is built): argument marshalling only.
 
 Every step of the attention path runs inside the library's HIP kernels.  There is
@@ -104,6 +104,7 @@ class LraError(RuntimeError):
 
 _lib = None
 _calls = None   # the CPython module, bound to _lib, or the same three calls by ctypes
+_calls8 = None  # ... and the 8-bit calls
 
 
 # The raw handle of the current stream, without the Stream object torch.cuda.current_stream() builds around it: a
@@ -151,7 +152,7 @@ class _CtypesCalls:
 
 def load_library() -> ctypes.CDLL:
     """dlopen the in-tree library.  Raises if it has not been built."""
-    global _lib, _calls
+    global _lib, _calls, _calls8
     if _lib is not None:
         return _lib
     if not os.path.exists(LIB_PATH):
@@ -213,9 +214,11 @@ def load_library() -> ctypes.CDLL:
         from . import _lra_pycall
         entry = [ctypes.cast(f, vp).value for f in (lib.lra_attn_decode, lib.lra_attn_prefill, lib.lra_cache_append)]
         _lra_pycall.bind(*entry, ctypes.addressof(_tuning), LraShape, LraCache, _current_device, _raw_stream, torch.cuda.is_initialized)
-        _calls = _lra_pycall
+        eight = (lib.lra_quantize_rows, lib.lra_matmul_i8, lib.lra_cache8_append, lib.lra_cache8_gather, lib.lra_attn_batch8)
+        _lra_pycall.bind8(*[ctypes.cast(f, vp).value for f in eight], LraCache8, LraBatch, torch.bfloat16, torch.float32, torch.int8, torch.int32)
+        _calls, _calls8 = _lra_pycall, _lra_pycall
     else:
-        _calls = _CtypesCalls(lib.lra_attn_decode, lib.lra_attn_prefill, lib.lra_cache_append)
+        _calls, _calls8 = _CtypesCalls(lib.lra_attn_decode, lib.lra_attn_prefill, lib.lra_cache_append), _CtypesCalls8(lib)
     _lib = lib
     return lib
 
@@ -588,9 +591,119 @@ def make_cache8(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale
     return cache
 
 
+class _CtypesCalls8:
+    """The 8-bit calls of the CPython module, for an interpreter that it is not built for.  Both answer -1 for tensors that are
+    not as documented, or a status."""
+
+    def __init__(self, lib):
+        self._lib = lib
+
+    def quantize(self, x, codes, scales, stream):
+        try:
+            _check_quantize(x, codes, scales)
+        except LraError:
+            return -1
+        return self._lib.lra_quantize_rows(_ptr(x), _dtype_code(x), _row_stride(x), x.size(0), x.size(1), _ptr(codes), _row_stride(codes),
+                                           _ptr(scales), _stream_ptr(stream))
+
+    def matmul(self, x, x_scale, w, w_scale, y, workspace, stream):
+        try:
+            _check_matmul(x, x_scale, w, w_scale, y)
+        except LraError:
+            return -1
+        ops = LraI8Operands(_ptr(x), _ptr(w), _ptr(x_scale), _ptr(w_scale), _row_stride(x), _row_stride(w), x.size(0), w.size(0), x.size(1))
+        return self._lib.lra_matmul_i8(ctypes.byref(ops), _ptr(y), _dtype_code(y), _row_stride(y), *_workspace_args(workspace), _stream_ptr(stream))
+
+    def append8(self, shape, cache, seq_start, max_new_per_seq, k, v, l, rope_theta, positions, stream):
+        try:
+            _check_new_rows(shape, cache, seq_start, k, v, l, positions)
+        except LraError:
+            return -1
+        stride = lambda t: t.stride(0) if t.size(0) > 1 else t[0].numel()  # noqa: E731
+        rows = LraNewRows(_ptr(k), _ptr(v), _ptr(l), stride(k), stride(v), 0 if l is None else stride(l), _ptr(seq_start), _ptr(positions),
+                          k.size(0), int(max_new_per_seq), float(rope_theta))
+        return self._lib.lra_cache8_append(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(rows), _stream_ptr(stream))
+
+    def gather8(self, shape, cache, dst, kept, stream):
+        try:
+            _check_gather8(shape, cache, dst, kept)
+        except LraError:
+            return -1
+        return self._lib.lra_cache8_gather(ctypes.byref(shape), ctypes.byref(cache), _ptr(kept), 0 if kept is None else _row_stride(kept),
+                                           ctypes.byref(dst), _stream_ptr(stream))
+
+    def attend8(self, shape, cache, b_k, b_v, n_adapters, batch, q, out, workspace, stream):
+        try:
+            _check_attend8(shape, cache, batch, q, out)
+        except LraError:
+            return -1
+        ad = LraAdapters(_ptr(b_k), _ptr(b_v), int(n_adapters))
+        return self._lib.lra_attn_batch8(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(ad), ctypes.byref(batch), _ptr(q), _ptr(out),
+                                         *_workspace_args(workspace), _tuning_ref, _stream_ptr(stream))
+
+
+def _entry_points8():
+    load_library()
+    return _calls8
+
+
+def _check8(status: int, check, *args) -> None:
+    """A status that is not LRA_OK; for -1 the check that says what is not as documented."""
+    if status < 0:
+        check(*args)
+        status = 2
+    _check(status)
+
+
 def _check_cache8(shape: LraShape, cache: LraCache8) -> None:
     if cache._sizes != (shape.n_kv_heads, shape.head_dim, shape.rank, shape.dtype):
         raise LraError(2, "the cache's kv heads, head dimension, rank and type of l must be those of the shape")
+
+
+def _check_new_rows(shape, cache, seq_start, k, v, l, positions) -> None:
+    _check_cache8(shape, cache)
+    n_new = k.size(0)
+    for t in (k, v):
+        if tuple(t.shape) != (n_new, shape.n_kv_heads, shape.head_dim) or not t[:1].is_contiguous() or _dtype_code(t) != shape.dtype:
+            raise LraError(2, f"k and v must be [{n_new}][{shape.n_kv_heads}][{shape.head_dim}] of the shape's dtype, dense but for the tokens")
+    if l is not None and (tuple(l.shape) != (n_new, shape.rank) or (shape.rank > 1 and l.stride(1) != 1) or _dtype_code(l) != shape.dtype):
+        raise LraError(2, f"l must be [{n_new}][{shape.rank}] of the shape's dtype, unit stride on the rank")
+    _dense_i32("seq_start", seq_start, cache.n_seqs + 1)
+    if positions is not None:
+        _dense_i32("positions", positions, n_new)
+
+
+def _check_gather8(shape, cache, dst, kept) -> None:
+    _check_cache8(shape, cache)
+    if kept is not None:
+        _check_kept(dst, kept, dst.max_seq_len)
+
+
+def _check_attend8(shape, cache, batch, q, out) -> None:
+    _check_rows(batch, shape, q, out)
+    _check_cache8(shape, cache)
+
+
+def _check_codes(name: str, codes: torch.Tensor, scales: torch.Tensor) -> None:
+    if codes.dtype != torch.int8 or codes.dim() != 2 or codes.stride(1) != 1:
+        raise LraError(2, f"{name} must be int8 [rows][cols], unit stride on the columns")
+    if scales.dtype != torch.float32 or tuple(scales.shape) != (codes.size(0),) or not scales.is_contiguous():
+        raise LraError(2, f"the scales of {name} must be a dense float32 vector of {codes.size(0)}")
+
+
+def _check_quantize(x, codes, scales) -> None:
+    _check_codes("codes", codes, scales)
+    _dtype_code(x)
+    if x.shape != codes.shape or x.stride(1) != 1:
+        raise LraError(2, "x must have the codes' shape and unit stride on the columns")
+
+
+def _check_matmul(x, x_scale, w, w_scale, y) -> None:
+    _check_codes("x", x, x_scale)
+    _check_codes("w", w, w_scale)
+    _dtype_code(y)
+    if x.size(1) != w.size(1) or tuple(y.shape) != (x.size(0), w.size(0)) or (y.size(1) > 1 and y.stride(1) != 1):
+        raise LraError(2, "x [m][k], w [n][k] and y [m][n] must agree, y with unit stride on the features")
 
 
 def lra_cache8_append(shape: LraShape, cache: LraCache8, seq_start: torch.Tensor, max_new_per_seq: int, k: torch.Tensor, v: torch.Tensor,
@@ -598,30 +711,17 @@ def lra_cache8_append(shape: LraShape, cache: LraCache8, seq_start: torch.Tensor
     """Write the new rows (the last tokens of every sequence, which seq_lens counts already) into the cache: keys rotated by
     their positions if rope_theta > 0, keys and values quantized.  k, v: [n_new][Hkv][d] with dense rows, l: [n_new][r]; the
     tokens may be strided, as the columns of one projection are.  seq_start: int32 [n_seqs+1]."""
-    _check_cache8(shape, cache)
-    n_new = k.size(0)
-    for t in (k, v):
-        if tuple(t.shape) != (n_new, shape.n_kv_heads, shape.head_dim) or not t[:1].is_contiguous() or _dtype_code(t) != shape.dtype:
-            raise LraError(2, f"k and v must be [{n_new}][{shape.n_kv_heads}][{shape.head_dim}] of the shape's dtype, dense but for the tokens")
-    if l is not None and (tuple(l.shape) != (n_new, shape.rank) or l.stride(1) != 1 or _dtype_code(l) != shape.dtype):
-        raise LraError(2, f"l must be [{n_new}][{shape.rank}] of the shape's dtype, unit stride on the rank")
-    _dense_i32("seq_start", seq_start, cache.n_seqs + 1)
-    if positions is not None:
-        _dense_i32("positions", positions, n_new)
-    stride = lambda t: t.stride(0) if n_new > 1 else t[0].numel()  # noqa: E731
-    rows = LraNewRows(_ptr(k), _ptr(v), _ptr(l), stride(k), stride(v), 0 if l is None else stride(l), _ptr(seq_start), _ptr(positions), n_new,
-                      int(max_new_per_seq), float(rope_theta))
-    _check(load_library().lra_cache8_append(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(rows), _stream_ptr(stream)))
+    status = (_calls8 or _entry_points8()).append8(shape, cache, seq_start, max_new_per_seq, k, v, l, rope_theta, positions, stream)
+    if status:
+        _check8(status, _check_new_rows, shape, cache, seq_start, k, v, l, positions)
 
 
 def lra_cache8_gather(shape: LraShape, cache: LraCache8, dst: LraCache, kept: Optional[torch.Tensor] = None, stream=None) -> None:
     """Row i of sequence t of the cache dst (make_cache) becomes the values of row kept[t][i] of `cache`, for i below dst's
     lengths; without `kept` its last rows."""
-    _check_cache8(shape, cache)
-    if kept is not None:
-        _check_kept(dst, kept, dst.max_seq_len)
-    _check(load_library().lra_cache8_gather(ctypes.byref(shape), ctypes.byref(cache), _ptr(kept), 0 if kept is None else _row_stride(kept),
-                                            ctypes.byref(dst), _stream_ptr(stream)))
+    status = (_calls8 or _entry_points8()).gather8(shape, cache, dst, kept, stream)
+    if status:
+        _check8(status, _check_gather8, shape, cache, dst, kept)
 
 
 def lra_batch8_workspace_bytes(shape: LraShape, cache: LraCache8, batch: LraBatch) -> int:
@@ -634,27 +734,16 @@ def lra_batch8_workspace_bytes(shape: LraShape, cache: LraCache8, batch: LraBatc
 def lra_attn_batch8(shape: LraShape, cache: LraCache8, b_k: Optional[torch.Tensor], b_v: Optional[torch.Tensor], n_adapters: int,
                     batch: LraBatch, q: torch.Tensor, out: torch.Tensor, workspace: Optional[torch.Tensor], stream=None) -> None:
     """lra_attn_batch over a cache of 8-bit codes.  q, out: [n_queries][Hq][d]."""
-    _check_rows(batch, shape, q, out)
-    _check_cache8(shape, cache)
-    ad = LraAdapters(_ptr(b_k), _ptr(b_v), int(n_adapters))
-    _check(load_library().lra_attn_batch8(ctypes.byref(shape), ctypes.byref(cache), ctypes.byref(ad), ctypes.byref(batch), _ptr(q), _ptr(out),
-                                          *_workspace_args(workspace), _tuning_ref, _stream_ptr(stream)))
-
-
-def _check_codes(name: str, codes: torch.Tensor, scales: torch.Tensor) -> None:
-    if codes.dtype != torch.int8 or codes.dim() != 2 or codes.stride(1) != 1:
-        raise LraError(2, f"{name} must be int8 [rows][cols], unit stride on the columns")
-    if scales.dtype != torch.float32 or tuple(scales.shape) != (codes.size(0),) or not scales.is_contiguous():
-        raise LraError(2, f"the scales of {name} must be a dense float32 vector of {codes.size(0)}")
+    status = (_calls8 or _entry_points8()).attend8(shape, cache, b_k, b_v, n_adapters, batch, q, out, workspace, stream)
+    if status:
+        _check8(status, _check_attend8, shape, cache, batch, q, out)
 
 
 def lra_quantize_rows(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, stream=None) -> None:
     """Rows of x (bf16 or fp32) as 8-bit integers with a scale each: codes int8 of x's shape, scales float32 [rows]."""
-    _check_codes("codes", codes, scales)
-    if x.shape != codes.shape or x.stride(1) != 1:
-        raise LraError(2, "x must have the codes' shape and unit stride on the columns")
-    _check(load_library().lra_quantize_rows(_ptr(x), _dtype_code(x), _row_stride(x), x.size(0), x.size(1), _ptr(codes), _row_stride(codes),
-                                            _ptr(scales), _stream_ptr(stream)))
+    status = (_calls8 or _entry_points8()).quantize(x, codes, scales, stream)
+    if status:
+        _check8(status, _check_quantize, x, codes, scales)
 
 
 def lra_matmul_i8_workspace_bytes(m: int, n: int, k: int, dtype: torch.dtype = torch.bfloat16) -> int:
@@ -668,10 +757,6 @@ def lra_matmul_i8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_sca
                   workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """y [m][n] (bf16 or fp32) = x_scale[i] w_scale[j] (x w^T)[i][j] for codes x int8 [m][k] and weights w int8 [n][k].
     `workspace` (optional, lra_matmul_i8_workspace_bytes bytes) lets few tokens divide k over the chip."""
-    _check_codes("x", x, x_scale)
-    _check_codes("w", w, w_scale)
-    if x.size(1) != w.size(1) or tuple(y.shape) != (x.size(0), w.size(0)) or y.stride(1) != 1:
-        raise LraError(2, "x [m][k], w [n][k] and y [m][n] must agree, y with unit stride on the features")
-    ops = LraI8Operands(_ptr(x), _ptr(w), _ptr(x_scale), _ptr(w_scale), _row_stride(x), _row_stride(w), x.size(0), w.size(0), x.size(1))
-    _check(load_library().lra_matmul_i8(ctypes.byref(ops), _ptr(y), _dtype_code(y), _row_stride(y), *_workspace_args(workspace),
-                                        _stream_ptr(stream)))
+    status = (_calls8 or _entry_points8()).matmul(x, x_scale, w, w_scale, y, workspace, stream)
+    if status:
+        _check8(status, _check_matmul, x, x_scale, w, w_scale, y)
