@@ -1,9 +1,8 @@
-// Attention over 8-bit codes for sequences with few query rows (bf16, gfx950): 64 at most per kv head, a decode step of some
+// Attention over 8-bit codes for sequences with few query rows (bf16, gfx950): 16 at most per kv head, a decode step of some
 // agents or a few tokens, through a window and sinks or not.
 //
-// One workgroup streams a share of one (sequence, kv head)'s visible keys for all its rows: 16 rows to a wave, the four waves (or pairs
-// of them with up to 32 rows, or with more one of them) taking 64-key tiles in turn, four blocks each.  They are on their own from the
-// first tile to the last:
+// One workgroup streams a share of one (sequence, kv head)'s visible keys for all its rows; its four waves take 64-key tiles in turn,
+// four blocks each, and are on their own from the first tile to the last:
 //   S^T = K Q^T + L Qt^T,   online softmax along keys,   O^T += V^T P^T,   Olr^T += L^T P^T      (v_mfma_f32_16x16x32_bf16)
 // Nothing passes through LDS on the way: the layout of the cache is that of the operands.  Which key stands in which row of a product
 // is free, as long as the next product agrees, and so is the order of the dimension that a product sums over:
@@ -66,18 +65,16 @@ __device__ __forceinline__ uint4 codes_to_values(uint32_t lo, uint32_t hi, float
 
 __device__ __forceinline__ uint4 masked(uint4 v, uint4 m) { return make_uint4(v.x & m.x, v.y & m.y, v.z & m.z, v.w & m.w); }
 
-// RT: row tiles of a workgroup (1, 2 or 4).
-template <int D, int RT, int RP, bool HAS_BK, int CODE>
+template <int D, int RP, bool HAS_BK, int CODE>
 __global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
-  constexpr int NS = 4 / RT;   // waves that divide the tiles of one row tile
+  constexpr int NS = 4;        // waves that divide the tiles
   constexpr int KS = D / 32;   // k-steps of S^T over the head dimension
   constexpr int DB = D / 16;   // 16-row blocks of O^T
   constexpr int RB = RP / 16;  // 16-row blocks of Olr^T
   constexpr int KW = D / 64;   // 16-byte pieces of a lane's quarter of a K row
   constexpr int SLOT = ((DB + RB) * 4 + 1) * 64 * 4;  // a wave's state, lane by lane
-  constexpr int QT_BYTES = HAS_BK ? RT * RB * 64 * 8 : 0;
-  constexpr int SMEM = 2 * SLOT > QT_BYTES ? 2 * SLOT : QT_BYTES;
-  __shared__ __align__(16) unsigned char smem[SMEM];
+  static_assert(RB * 64 * 8 <= 2 * SLOT);
+  __shared__ __align__(16) unsigned char smem[2 * SLOT];
   __shared__ float m_s[4][16];
   const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -86,15 +83,13 @@ __global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
   const int n_t = min(p.seq_lens[t], p.max_seq_len);
   const int c0 = t > 0 ? min(max(p.seq_query_start[t], 0), p.n_queries) : 0;
   const int c1 = t + 1 < p.n_seqs ? min(max(p.seq_query_start[t + 1], c0), p.n_queries) : p.n_queries;
-  const int n_rows = min((c1 - c0) * G, 16 * RT);
+  const int n_rows = min((c1 - c0) * G, 16);
   if (n_rows == 0) return;
   const int first_pos = p.causal ? n_t - (c1 - c0) : n_t - 1, pos_last = n_t - 1;
-  const int rt = wave % RT, stream = wave / RT;
   // this lane's row (the last one again past the end)
-  const int at_row = min(16 * rt + l16, n_rows - 1), tok = at_row / G;
+  const int at_row = min(l16, n_rows - 1), tok = at_row / G;
   const int row = (c0 + tok) * Hq + h * G + (at_row - tok * G), pos = first_pos + (p.causal ? tok : 0);
-  const bool live = 16 * rt + l16 < n_rows;
-  const bool has_rows = 16 * rt < n_rows;  // (uniform)
+  const bool live = l16 < n_rows;
   const int lo = p.window > 0 ? max(0, first_pos - p.window + 1) : 0, sinks = min(p.sinks, lo);
   const int sink_tiles = (sinks + 63) / 64, gap = max(0, lo / 64 - sink_tiles);
   const int n_tiles = n_t <= 0 ? 0 : (n_t - 1) / 64 + 1 - gap;
@@ -105,7 +100,7 @@ __global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
   auto adapter_of_row = [&]() __attribute__((always_inline)) -> int { return p.causal ? a_first : p.query_adapter[c0 + tok]; };
   if (t0 >= t1) {
     // an empty state, all the merge kernel looks at; for a row that sees nothing at all share 0 leaves one that gives zeros
-    if (stream == 0 && live) {
+    if (wave == 0 && live) {
       const bool nothing = split == 0 && pos < 0;
       if (g == 0) {
         p.part_ml[slot * 2 + 0] = nothing ? 0.f : -INFINITY;
@@ -160,7 +155,7 @@ __global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
     for (int b = 0; b < DB; ++b) vc[b] = *reinterpret_cast<const uint4*>(src + b * 256);
     vs_raw = p.v_scale[id * p.scale_block_stride + h];
   };
-  const int first = has_rows ? t0 + stream : t1;
+  const int first = t0 + wave;
   int id_next = 0;
   if (first < t1) {
     const int id = look_up(key_of(first));
@@ -178,14 +173,14 @@ __global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
     for (int ks = 0; ks < KS; ++ks) qb[ks] = as_bf16x8(*reinterpret_cast<const uint4*>(qr + ks * 8));
   }
   // Qt^T, ranks by rows: register e of block b is rank 16b + 4g + e, the operand that L Qt^T takes (k = 16: four ranks a lane group).
-  // The waves of a row tile divide its queries (each with its adapter, or the chunk's one) and hand the operands round in LDS.
+  // The waves divide the queries (each with its adapter, or the chunk's one) and hand the operands round in LDS.
   s16x4v qtb[HAS_BK ? RB : 1];
   if constexpr (HAS_BK) {
     const int64_t ldb = static_cast<int64_t>(Hkv) * D;
-    const int it0 = p.causal ? 0 : 16 * rt / G, it1 = !has_rows ? it0 : (p.causal ? 1 : (min(16 * rt + 16, n_rows) - 1) / G + 1);
-    uint2* const qt_s = reinterpret_cast<uint2*>(smem) + rt * RB * 64;
+    const int n_it = p.causal ? 1 : (n_rows - 1) / G + 1;
+    uint2* const qt_s = reinterpret_cast<uint2*>(smem);
 #pragma unroll 1
-    for (int it = it0 + stream; it < it1; it += NS) {
+    for (int it = wave; it < n_it; it += NS) {
       const int a = p.causal ? a_first : min(max(p.query_adapter[c0 + it], 0), p.n_adapters - 1);
       const bf16_t* src = static_cast<const bf16_t*>(p.b_k) + static_cast<int64_t>(a) * r * ldb + h * D + g * (D / 4);
 #pragma unroll
@@ -343,14 +338,14 @@ __global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
     __builtin_amdgcn_sched_barrier(0);
   }
 
-  // ---------------- the states of a row tile's waves: two by two through LDS, the first of them stores ----------------
+  // ---------------- the waves' states: two by two through LDS, wave 0 stores ----------------
   l_run = sum_over_lane_groups(l_run);
   float m_all = m_run;
-  if constexpr (NS > 1) {
+  {
     if (g == 0) m_s[wave][l16] = m_run;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < NS; ++i) m_all = fmaxf(m_all, m_s[i * RT + rt][l16]);
+    for (int i = 0; i < NS; ++i) m_all = fmaxf(m_all, m_s[i][l16]);
     const float wgt = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_all);
     l_run = m_run == -INFINITY ? l_run : l_run * wgt;  // (a sum of NaN stays one)
 #pragma unroll
@@ -359,8 +354,8 @@ __global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
     for (int b = 0; b < RB; ++b) lr_acc[b] *= wgt;
 #pragma unroll
     for (int stride = NS / 2; stride >= 1; stride >>= 1) {
-      if (stream >= stride && stream < 2 * stride) {
-        float* dst = reinterpret_cast<float*>(smem + (wave - stride * RT) * SLOT) + lane;
+      if (wave >= stride && wave < 2 * stride) {
+        float* dst = reinterpret_cast<float*>(smem + (wave - stride) * SLOT) + lane;
 #pragma unroll
         for (int b = 0; b < DB; ++b)
 #pragma unroll
@@ -372,7 +367,7 @@ __global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
         dst[(DB + RB) * 4 * 64] = l_run;
       }
       __syncthreads();
-      if (stream < stride) {
+      if (wave < stride) {
         const float* src = reinterpret_cast<const float*>(smem + wave * SLOT) + lane;
 #pragma unroll
         for (int b = 0; b < DB; ++b)
@@ -387,7 +382,7 @@ __global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
       __syncthreads();
     }
   }
-  if (stream != 0 || !live) return;
+  if (wave != 0 || !live) return;
   if (g == 0) {
     const bool nothing = split == 0 && pos < 0;  // (such a row's O and O_lr are zeros)
     p.part_ml[slot * 2 + 0] = nothing ? 0.f : m_all * 0.69314718055994530942f;  // natural-log units
@@ -399,25 +394,6 @@ __global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
 #pragma unroll
   for (int b = 0; b < RB; ++b)
     if (16 * b + 4 * g < r) *reinterpret_cast<f32x4*>(p.part_lr + slot * r + 16 * b + 4 * g) = lr_acc[b];  // (the rank is a multiple of 8)
-}
-
-template <int D, int CODE>
-static hipError_t launch_attn8_rows(const Batch8Params& p, int row_tiles, hipStream_t s) {
-  const dim3 grid(p.n_kv_heads * p.n_splits, p.n_seqs);
-  auto launch = [&](auto rt_c, auto rp_c) {
-    constexpr int RT = decltype(rt_c)::value, RP = decltype(rp_c)::value;
-    if (p.b_k != nullptr) hipLaunchKernelGGL((attn8_rows_kernel<D, RT, RP, true, CODE>), grid, dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((attn8_rows_kernel<D, RT, RP, false, CODE>), grid, dim3(256), 0, s, p);
-  };
-  auto by_rank = [&](auto rt_c) {
-    if (p.rank <= 16) launch(rt_c, std::integral_constant<int, 16>{});
-    else if (p.rank <= 32) launch(rt_c, std::integral_constant<int, 32>{});
-    else launch(rt_c, std::integral_constant<int, 64>{});
-  };
-  if (row_tiles <= 1) by_rank(std::integral_constant<int, 1>{});
-  else if (row_tiles <= 2) by_rank(std::integral_constant<int, 2>{});
-  else by_rank(std::integral_constant<int, 4>{});
-  return hipGetLastError();
 }
 
 }  // namespace lra

@@ -1,5 +1,5 @@
-// Instantiations of the few-rows kernel over LRA_E4M3 codes (a file each: they compile side by side).
-#include "lra_attn8_rows.h"
+// Instantiations of the few-rows kernels over LRA_E4M3 codes (a file each: they compile side by side).
+#include "lra_attn8_rows32.h"
 
 namespace lra {
 
