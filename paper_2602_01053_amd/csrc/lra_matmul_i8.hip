@@ -88,12 +88,12 @@ __device__ __forceinline__ void store_scaled(const I8Params& p, int i, int j, in
 
 // The sums' order does not matter (integers), the scaling is the same everywhere: all kernels below give the same bits.
 
-// Few tokens (64 at most): the weights are read once and nothing else counts.  A workgroup of eight waves takes 16 features and all
+// Few tokens (32 at most): the weights are read once and nothing else counts.  A workgroup of eight waves takes 16 features and all
 // tokens, a wave every eighth 64-wide piece of k, eight pieces of its weights requested at a time; operands straight from memory
 // (v_mfma_i32_16x16x64_i8: a lane's 16 bytes of a row are its operand), the waves' sums meet in LDS.  RT: token tiles of 16.
 template <typename T, int RT>
 __global__ __launch_bounds__(512) void matmul_i8_stream_kernel(I8Params p) {
-  constexpr int U = RT == 4 ? 4 : 8;
+  constexpr int U = 8;
   __shared__ int sums[8][RT][4][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, g = lane >> 4;
@@ -173,30 +173,31 @@ __device__ __forceinline__ bool tile_of(int n_tt, int n_ct, int& tt, int& ct) {
   return true;
 }
 
-// 64 features x 64 tokens by eight waves, two of which divide k of each of the four 32 x 32 blocks.  Steps of 256 bytes of k, four
-// stages in LDS (a step's 32 KB are asked for three steps ahead: a tile is a chain of k / 256 steps with nothing else to hide their
-// latency).  A row of a stage is 256 bytes, its 16-byte chunks exchanged by row (xor), so that sixteen rows' reads spread over the banks.
-template <typename T>
-__global__ __launch_bounds__(512, 2) void matmul_i8_quarter_kernel(I8Params p) {
-  constexpr int BK = 256, NS = 4, TILE = 64 * BK, STAGE = 2 * TILE;
+// 64 B features x 64 B tokens by eight waves, two of which divide k of each of the four blocks of 32 B x 32 B.  Steps of 256 / B bytes of
+// k, four stages in LDS (a step's 32 KB are asked for three steps ahead: a tile is a chain of steps with nothing else to hide their
+// latency).  The rows of a stage are 256 / B bytes, their 16-byte chunks exchanged by row (xor), so that sixteen rows' reads spread over
+// the banks.
+template <typename T, int B>
+__global__ __launch_bounds__(512, 2) void matmul_i8_chain_kernel(I8Params p) {
+  constexpr int ROWS = 64 * B, BK = 256 / B, CH = BK / 16, NS = 4, TILE = ROWS * BK, STAGE = 2 * TILE;
   __shared__ __align__(16) unsigned char smem[NS * STAGE];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l32 = lane & 31, g2 = lane >> 5;
   int tt, ct;
-  if (!tile_of((p.m + 63) / 64, (p.n + 63) / 64, tt, ct)) return;
-  const int tok0 = tt * 64, feat0 = ct * 64;
+  if (!tile_of((p.m + ROWS - 1) / ROWS, (p.n + ROWS - 1) / ROWS, tt, ct)) return;
+  const int tok0 = tt * ROWS, feat0 = ct * ROWS;
   const uint32_t ldw = static_cast<uint32_t>(p.w_stride), ldx = static_cast<uint32_t>(p.x_stride);  // (at most 2^22)
-  const pf_u32x4 rs_w = pf_rsrc(p.w + feat0 * p.w_stride, (min(64, p.n - feat0) - 1u) * ldw + p.k);
-  const pf_u32x4 rs_x = pf_rsrc(p.x + tok0 * p.x_stride, (min(64, p.m - tok0) - 1u) * ldx + p.k);
+  const pf_u32x4 rs_w = pf_rsrc(p.w + feat0 * p.w_stride, (min(ROWS, p.n - feat0) - 1u) * ldw + p.k);
+  const pf_u32x4 rs_x = pf_rsrc(p.x + tok0 * p.x_stride, (min(ROWS, p.m - tok0) - 1u) * ldx + p.k);
   const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(PF_LDS_AS(unsigned char, smem)));
-  // request i of sixteen per tile fills rows 4i .. 4i + 3; wave w has i = w and w + 8 (the same rows mod 16: 4w .. 4w + 3)
-  const int row = lane >> 4, chunk = (lane & 15) ^ ((4 * wave + row) & 15);
+  // request i of sixteen per tile fills rows 4 B i .. 4 B i + 4 B - 1; wave w has i = w and w + 8; row r's chunk c is at c ^ (r / B) % CH
+  const int row = lane / CH, chunk = (lane & (CH - 1)) ^ ((4 * wave + row / B) & (CH - 1));
   const int n_steps = (p.k + BK - 1) / BK;
   auto issue = [&](int step) __attribute__((always_inline)) {
     const bool in = step * BK + chunk * 16 < p.k;  // (behind the last column: zeros)
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      const int r = 4 * (wave + 8 * q) + row;
+      const int r = 4 * B * (wave + 8 * q) + row;
       const uint32_t dst = lds0 + (step % NS) * STAGE + (wave + 8 * q) * 1024;
       pf_load16_to_lds(rs_w, dst, in ? r * ldw + chunk * 16 : kPfOob, step * BK);
       pf_load16_to_lds(rs_x, dst + TILE, in ? r * ldx + chunk * 16 : kPfOob, step * BK);
@@ -205,10 +206,14 @@ __global__ __launch_bounds__(512, 2) void matmul_i8_quarter_kernel(I8Params p) {
   for (int s = 0; s < NS - 1; ++s)
     if (s < n_steps) issue(s);
   const int kh = wave >> 2, fb = wave & 1, tb = (wave >> 1) & 1;
-  const int a_row = (32 * fb + l32) * BK, b_row = TILE + (32 * tb + l32) * BK, x15 = (l32 & 15);
-  i32x16 acc;
+  const int a_row = (32 * B * fb + l32) * BK, b_row = TILE + (32 * B * tb + l32) * BK, swap = (l32 / B) & (CH - 1);
+  i32x16 acc[B][B];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) acc[i] = 0;
+  for (int a = 0; a < B; ++a)
+#pragma unroll
+    for (int b = 0; b < B; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[a][b][i] = 0;
   for (int s = 0; s < n_steps; ++s) {
     // this step's four requests of the wave are here, those of the two behind it may be on their way
     if (s + 2 < n_steps) asm volatile("s_waitcnt vmcnt(8)");
@@ -218,23 +223,48 @@ __global__ __launch_bounds__(512, 2) void matmul_i8_quarter_kernel(I8Params p) {
     if (s + NS - 1 < n_steps) issue(s + NS - 1);
     const unsigned char* st = smem + (s % NS) * STAGE;
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) {
-      const int c = ((8 * kh + 2 * ks + g2) ^ x15) << 4;
-      const i32x4 a = *reinterpret_cast<const i32x4*>(st + a_row + c), b = *reinterpret_cast<const i32x4*>(st + b_row + c);
-      acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, acc, 0, 0, 0);
+    for (int ks = 0; ks < BK / 64; ++ks) {
+      const int c = ((CH / 2 * kh + 2 * ks + g2) ^ swap) << 4;
+      i32x4 a[B], b[B];
+#pragma unroll
+      for (int i = 0; i < B; ++i) {
+        a[i] = *reinterpret_cast<const i32x4*>(st + a_row + i * 32 * BK + c);
+        b[i] = *reinterpret_cast<const i32x4*>(st + b_row + i * 32 * BK + c);
+      }
+#pragma unroll
+      for (int i = 0; i < B; ++i)
+#pragma unroll
+        for (int j = 0; j < B; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(a[i], b[j], acc[i][j], 0, 0, 0);
     }
   }
+  // the second half of k is added to the first; of several blocks each half stores those of one token column
   __syncthreads();
-  int* other = reinterpret_cast<int*>(smem) + (wave & 3) * 1024 + lane;
-  if (kh == 1) {
+  int* other = reinterpret_cast<int*>(smem) + (wave & 3) * (B * B * 1024) + lane;
+  if constexpr (B == 1) {
+    if (kh == 1) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) other[i * 64] = acc[i];
+      for (int i = 0; i < 16; ++i) other[i * 64] = acc[0][0][i];
+    }
+    __syncthreads();
+    if (kh == 1) return;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[0][0][i] += other[i * 64];
+    store_block<T>(p, acc[0][0], tok0 + 32 * tb + l32, feat0 + 32 * fb, g2);
+  } else {
+#pragma unroll
+    for (int a = 0; a < B; ++a)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) other[((kh ^ 1) * B + a) * 1024 + i * 64] = kh ? acc[a][0][i] : acc[a][1][i];
+    __syncthreads();
+#pragma unroll
+    for (int a = 0; a < B; ++a) {
+      i32x16 sum;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sum[i] = (kh ? acc[a][1][i] : acc[a][0][i]) + other[(kh * B + a) * 1024 + i * 64];
+      const int f0 = feat0 + 32 * (B * fb + a);
+      if (f0 < p.n) store_block<T>(p, sum, tok0 + 32 * (B * tb + kh) + l32, f0, g2);
+    }
   }
-  __syncthreads();
-  if (kh == 1) return;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) acc[i] += other[i * 64];
-  store_block<T>(p, acc, tok0 + 32 * tb + l32, feat0 + 32 * fb, g2);
 }
 
 // 256 features x 256 tokens by eight waves of 128 x 64 (eight 32 x 32 accumulators): six operand reads for eight products, 64 KB into
@@ -350,23 +380,53 @@ __global__ __launch_bounds__(256) void matmul_i8_far_kernel(I8Params p) {
   }
 }
 
+// Tiles of 64, 128 or 256 a side, a compute unit holding one at a time: a round of the chip takes 10, 21 and 50 to 57 us at k = 4096, so
+// that the fewest rounds by these weights are taken.  A few features behind whole tiles may get the smallest tiles in a launch of their own:
+// 8192 tokens x 6160 features are 800 tiles of 256 in four rounds, 218 us, or 768 in three and 128 small ones.
+struct I8Split {
+  int side, features;
+};
+static int64_t tiles_of(int64_t m, int64_t n, int64_t side) { return (m + side - 1) / side * ((n + side - 1) / side); }
+static I8Split split_features(int64_t m, int64_t n) {
+  auto cost = [&](int64_t features, int side) { return (tiles_of(m, features, side) + 255) / 256 * (side == 256 ? 55 : (side == 128 ? 21 : 10)); };
+  I8Split best{64, static_cast<int>(n)};
+  int64_t least = cost(n, 64);
+  for (const int side : {128, 256}) {
+    const int64_t whole = n / side * side;
+    if (cost(n, side) < least) least = cost(n, side), best = {side, static_cast<int>(n)};
+    if (whole > 0 && whole < n && cost(whole, side) + cost(n - whole, 64) + 3 < least)
+      least = cost(whole, side) + cost(n - whole, 64) + 3, best = {side, static_cast<int>(whole)};
+  }
+  return best;
+}
+
 template <typename T>
 static void launch_matmul(const I8Params& p, hipStream_t s) {
   constexpr int64_t kNear = int64_t{1} << 22;  // 256 rows within 32-bit offsets below the one that stands for "outside"
-  if (p.m <= 64) {
+  // (up to 32 tokens while the chip holds all workgroups at once, 16 at any width: 32 tokens x 4640 features of 3584 take 15.3 us in two
+  // rounds, and 8.4 us in tiles of 64; 4096 of 4096 8.4 and 9.5 us)
+  if (p.m <= 16 || (p.m <= 32 && p.n <= 16 * 256)) {
     const dim3 grid((p.n + 15) / 16);
     if (p.m <= 16) hipLaunchKernelGGL((matmul_i8_stream_kernel<T, 1>), grid, dim3(512), 0, s, p);
-    else if (p.m <= 32) hipLaunchKernelGGL((matmul_i8_stream_kernel<T, 2>), grid, dim3(512), 0, s, p);
-    else hipLaunchKernelGGL((matmul_i8_stream_kernel<T, 4>), grid, dim3(512), 0, s, p);
+    else hipLaunchKernelGGL((matmul_i8_stream_kernel<T, 2>), grid, dim3(512), 0, s, p);
     return;
   }
   if (p.x_stride > kNear || p.w_stride > kNear) {
     hipLaunchKernelGGL((matmul_i8_far_kernel<T>), dim3((p.n + 63) / 64, min((p.m + 15) / 16, 65535)), dim3(256), 0, s, p);
     return;
   }
-  const int64_t wide = static_cast<int64_t>((p.m + 255) / 256) * ((p.n + 255) / 256), quarter = static_cast<int64_t>((p.m + 63) / 64) * ((p.n + 63) / 64);
-  if (wide >= 128) hipLaunchKernelGGL((matmul_i8_wide_kernel<T>), dim3(static_cast<unsigned>((wide + 7) / 8 * 8)), dim3(512), 0, s, p);
-  else hipLaunchKernelGGL((matmul_i8_quarter_kernel<T>), dim3(static_cast<unsigned>((quarter + 7) / 8 * 8)), dim3(512), 0, s, p);
+  const I8Split sp = split_features(p.m, p.n);
+  I8Params first = p, rest = p;
+  first.n = sp.features;
+  rest.n = p.n - sp.features;
+  rest.w += sp.features * p.w_stride;
+  rest.w_scale += sp.features;
+  rest.y = static_cast<T*>(p.y) + sp.features;
+  auto grid = [](const I8Params& q, int side) { return dim3(static_cast<unsigned>((tiles_of(q.m, q.n, side) + 7) / 8 * 8)); };
+  if (sp.side == 256) hipLaunchKernelGGL((matmul_i8_wide_kernel<T>), grid(first, 256), dim3(512), 0, s, first);
+  else if (sp.side == 128) hipLaunchKernelGGL((matmul_i8_chain_kernel<T, 2>), grid(first, 128), dim3(512), 0, s, first);
+  else hipLaunchKernelGGL((matmul_i8_chain_kernel<T, 1>), grid(first, 64), dim3(512), 0, s, first);
+  if (rest.n > 0) hipLaunchKernelGGL((matmul_i8_chain_kernel<T, 1>), grid(rest, 64), dim3(512), 0, s, rest);
 }
 
 }  // namespace lra
