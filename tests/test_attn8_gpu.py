@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import paper_2602_01053_amd as lra
-from tests.attn8_reference import Case8, Device8, attention_with_bound, close_enough, make8
+from tests.attn8_reference import Case8, Device8, attention_with_bound, close_enough, make8, values_of
 
 pytestmark = pytest.mark.gpu
 F32, BF16 = torch.float32, torch.bfloat16
@@ -55,6 +55,66 @@ def test_against_float64(c):
     assert torch.equal(got, dev.attend())          # equal arguments, equal bits
 
 
+ROWS = [(heads, counts) for heads, per in (((16, 1, 64), (1, 2, 3, 4, 5)), ((7, 1, 128), (2, 3, 4, 5, 9, 10)), ((2, 2, 128), (16, 17, 32, 33, 64, 65)))
+        for n in per for counts in ([n, 1, 0, max(n - 1, 1)],)]
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("code,rank", [("e4m3", 16), ("int8", 40), ("e4m3", 64), ("int8", 32)])
+@pytest.mark.parametrize("heads,counts", ROWS, ids=str)
+def test_rows_at_the_ends_of_tiles(heads, counts, code, rank, causal):
+    """Either side of 16, 32 and 64 rows per kv head, beside sequences with a few rows or none; lengths at the ends of key tiles."""
+    for window, sinks in ((0, 0), (70, 3)):
+        c = Case8([321, 64, 7, 129], counts, causal=causal, heads=heads, rank=rank, code=code, window=window, sinks=sinks, seed=len(counts) + rank)
+        x = make8(c)
+        want, bound = attention_with_bound(x)
+        close_enough(Device8(x, lra).attend(), want, bound, c.label())
+
+
+@pytest.mark.parametrize("c", [Case8([200, 90], [2, 2], heads=(8, 2, 128), rank=16), Case8([200, 90], [6, 3], heads=(8, 2, 64), rank=24, code="int8"),
+                               Case8([200, 90], [90, 20], heads=(4, 2, 64), rank=16), Case8([200, 90], [90, 20], causal=True, heads=(4, 2, 64)),
+                               Case8([200, 90], [2, 2], dtype=F32, rank=5)], ids=lambda c: c.label())
+def test_adapter_ids_out_of_range(c):
+    """Clamped into [0, n_adapters)."""
+    x = make8(c)
+    x.adapter = torch.tensor([-5, 900, 1 << 30, 1], dtype=torch.int32).repeat(len(x.adapter) // 4 + 1)[:len(x.adapter)].contiguous()
+    want, bound = attention_with_bound(x)
+    close_enough(Device8(x, lra).attend(), want, bound, c.label())
+
+
+@pytest.mark.parametrize("n_seqs", [300, 70000])
+@pytest.mark.parametrize("causal", [False, True])
+def test_many_short_sequences(n_seqs, causal):
+    """A block each (70000: more than a grid's second dimension holds), one query each, some of no tokens."""
+    g = torch.Generator().manual_seed(n_seqs)
+    codes = torch.randint(-127, 128, (2, n_seqs, 16, 64), generator=g, dtype=torch.int8)
+    scale = torch.randint(118, 124, (2, n_seqs, 1), generator=g, dtype=torch.uint8)
+    lens = torch.randint(0, 17, (n_seqs,), generator=g, dtype=torch.int32)
+    q = torch.randn(n_seqs, 1, 64, generator=g).to(BF16)
+    k, v = (values_of(z, s[..., None]) for z, s in zip(codes, scale))
+    size = torch.einsum("td,tnd->tn", q[:, 0].double().abs(), k.abs()).amax(1) / 8
+    s = (torch.einsum("td,tnd->tn", q[:, 0].double(), k) / 8).masked_fill(torch.arange(16) >= lens[:, None], -float("inf"))
+    pr = torch.softmax(s, 1).nan_to_num(0.0)
+    want, mass = torch.einsum("tn,tnd->td", pr, v), torch.einsum("tn,tnd->td", pr, v.abs())
+    # scores: sums of 64 products in fp32; weights move by twice a score's slip, probabilities round to bf16, and so does the output
+    rel = 2 * size * 72 * 2.0 ** -24 + 2.0 ** -8 + 2.0 ** -16
+    bound = mass * rel[:, None] + want.abs() * 2.0 ** -8 * (1 + 2.0 ** -6) + 1e-30
+    dev = [z.cuda() for z in (codes[0][:, None].contiguous(), codes[1].transpose(1, 2)[:, None].contiguous(), scale[0], scale[1], q)]
+    l = torch.full((n_seqs, 16, 8), float("nan"), dtype=BF16)
+    l[torch.arange(16) < lens[:, None]] = 1.0
+    l, lens_dev = l.cuda(), lens.cuda()
+    shape = lra.make_shape(dev[4], 1, 8)
+    table = torch.arange(n_seqs, dtype=torch.int32, device="cuda")[:, None].contiguous()
+    cache = lra.make_cache8(*dev[:4], l, lens_dev, 16, table)
+    start, adapter = torch.arange(n_seqs + 1, dtype=torch.int32, device="cuda"), torch.zeros(n_seqs, dtype=torch.int32, device="cuda")
+    batch = lra.make_batch(start, adapter, 1, causal=causal)
+    out = torch.full_like(dev[4], float("nan"))
+    ws = torch.empty(max(lra.lra_batch8_workspace_bytes(shape, cache, batch), 256), dtype=torch.uint8, device="cuda")
+    lra.lra_attn_batch8(shape, cache, None, None, 1, batch, dev[4], out, ws)
+    torch.cuda.synchronize()
+    close_enough(out[:, 0], want, bound, f"{n_seqs}")
+
+
 @pytest.mark.parametrize("variant", [1, 2])
 @pytest.mark.parametrize("c", [Case8([700, 33], [4, 2], heads=(8, 2, 128), rank=16),
                                Case8([400, 129, 9], [150, 1, 12], causal=True, window=90, sinks=3, heads=(8, 2, 64), rank=24, code="int8")],
@@ -94,7 +154,6 @@ def test_scales_at_their_ends():
     kc, ks, vc, vs = x.codes
     vs[0, 0], vs[0, 1], vs[0, 2] = 1, 190, 120
     ks[0, 3] = 1
-    from tests.attn8_reference import values_of
     x.v = values_of(vc, vs[..., None, None]).transpose(2, 3).reshape(1, -1, 2, 64)
     x.k = values_of(kc, ks[..., None, None]).transpose(2, 3).reshape(1, -1, 2, 64)
     want, bound = attention_with_bound(x)
