@@ -143,8 +143,7 @@ typedef struct {
 /*
  * y[i][j] = x_scale[i] * w_scale[j] * sum_c x[i][c] w[j][c]: the sum exact in 32-bit integers, scaled in fp32, rounded once.
  *   y          DEVICE [m][n] of dtype (lra_dtype), rows y_stride elements apart, 16-byte aligned; any n and y_stride >= n
- *   workspace  DEVICE, 256-byte aligned, optional (NULL, 0): with lra_matmul_i8_workspace_bytes(...) bytes products of few
- *              tokens divide k among more workgroups; the result is the same bit for bit
+ *   workspace  as many bytes as lra_matmul_i8_workspace_bytes says: none for any size so far, NULL and 0 will do
  */
 lra_status lra_matmul_i8(const lra_i8_operands* ops, void* y, int32_t dtype, int64_t y_stride, void* workspace,
                          size_t workspace_bytes, void* stream);

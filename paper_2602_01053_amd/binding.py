@@ -756,7 +756,7 @@ def lra_matmul_i8_workspace_bytes(m: int, n: int, k: int, dtype: torch.dtype = t
 def lra_matmul_i8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, y: torch.Tensor,
                   workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """y [m][n] (bf16 or fp32) = x_scale[i] w_scale[j] (x w^T)[i][j] for codes x int8 [m][k] and weights w int8 [n][k].
-    `workspace` (optional, lra_matmul_i8_workspace_bytes bytes) lets few tokens divide k over the chip."""
+    `workspace`: as many bytes as lra_matmul_i8_workspace_bytes says, none for any size so far."""
     status = (_calls8 or _entry_points8()).matmul(x, x_scale, w, w_scale, y, workspace, stream)
     if status:
         _check8(status, _check_matmul, x, x_scale, w, w_scale, y)
