@@ -65,6 +65,20 @@ __device__ __forceinline__ uint4 codes_to_values(uint32_t lo, uint32_t hi, float
 
 __device__ __forceinline__ uint4 masked(uint4 v, uint4 m) { return make_uint4(v.x & m.x, v.y & m.y, v.z & m.z, v.w & m.w); }
 
+// Workgroup x -> key share and kv head.  Consecutive workgroups go to consecutive XCDs; the kv heads of a share read the same low-rank
+// rows, so where the shares divide by eight those go to one XCD, one after the other, and meet in its L2.
+__device__ __forceinline__ void attn8_share(const Batch8Params& p, int& split, int& h) {
+  const int x = blockIdx.x, Hkv = p.n_kv_heads;
+  if ((p.n_splits & 7) == 0) {
+    const int eight = (x >> 3) / Hkv;
+    h = (x >> 3) - eight * Hkv;
+    split = 8 * eight + (x & 7);
+  } else {
+    split = x / Hkv;
+    h = x - split * Hkv;
+  }
+}
+
 template <int D, int RP, bool HAS_BK, int CODE>
 __global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
   constexpr int NS = 4;        // waves that divide the tiles
@@ -79,7 +93,9 @@ __global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
   const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int Hq = p.n_q_heads, Hkv = p.n_kv_heads, G = p.group, r = p.rank;
-  const int split = blockIdx.x / Hkv, h = blockIdx.x - split * Hkv, t = blockIdx.y;
+  const int t = blockIdx.y;
+  int split, h;
+  attn8_share(p, split, h);
   const int n_t = min(p.seq_lens[t], p.max_seq_len);
   const int c0 = t > 0 ? min(max(p.seq_query_start[t], 0), p.n_queries) : 0;
   const int c1 = t + 1 < p.n_seqs ? min(max(p.seq_query_start[t + 1], c0), p.n_queries) : p.n_queries;

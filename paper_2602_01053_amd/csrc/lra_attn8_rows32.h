@@ -33,7 +33,9 @@ __global__ __launch_bounds__(256, attn8_rows32_waves(RP)) void attn8_rows32_kern
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int rt = wave % RT, stream = wave / RT;
   const int Hq = p.n_q_heads, Hkv = p.n_kv_heads, G = p.group, r = p.rank;
-  const int split = blockIdx.x / Hkv, h = blockIdx.x - split * Hkv, t = blockIdx.y;
+  const int t = blockIdx.y;
+  int split, h;
+  attn8_share(p, split, h);
   const int n_t = min(p.seq_lens[t], p.max_seq_len);
   const int c0 = t > 0 ? min(max(p.seq_query_start[t], 0), p.n_queries) : 0;
   const int c1 = t + 1 < p.n_seqs ? min(max(p.seq_query_start[t + 1], c0), p.n_queries) : p.n_queries;
