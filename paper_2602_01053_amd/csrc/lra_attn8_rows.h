@@ -6,8 +6,8 @@
 //   S^T = K Q^T + L Qt^T,   online softmax along keys,   O^T += V^T P^T,   Olr^T += L^T P^T      (v_mfma_f32_16x16x32_bf16)
 // Nothing passes through LDS on the way: the layout of the cache is that of the operands.  Which key stands in which row of a product
 // is free, as long as the next product agrees, and so is the order of the dimension that a product sums over:
-//   row rho of key tile t (of four) is token 4t + rho % 4 of block rho / 4.  A lane of the A operand then takes a quarter of one
-//     token's K row, 32 bytes in a piece, with Q's dimensions in the same order;
+//   row rho of key tile t (of four) is token 4t + rho % 4 of block rho / 4.  A lane of the A operand then takes 16 bytes
+//     of every 64 of one token's K row, with Q's dimensions in the same order: a load's four lanes of a row have 64 bytes in a piece;
 //   lane group g of the result S^T holds all sixteen tokens of block g, which is what the B operand of V^T P^T wants of it: its A
 //     operand is sixteen tokens of one dimension, the 16 bytes that the cache holds together;
 //   L is transposed by a product with the identity: the result layout of L I is the operand layout of L^T.
@@ -138,7 +138,7 @@ __global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
 
   // ---------------- a tile's requests ----------------
   const int my_block = l16 >> 2, my_token = l16 & 3;  // of the A operands of S^T: row l16
-  const uint8_t* const kh = static_cast<const uint8_t*>(p.k_base) + h * p.kv_head_stride + my_token * D + g * (D / 4);
+  const uint8_t* const kh = static_cast<const uint8_t*>(p.k_base) + h * p.kv_head_stride + my_token * D + g * 16;
   const uint8_t* const vh = static_cast<const uint8_t*>(p.v_base) + h * p.kv_head_stride + l16 * 16;
   const bf16_t* const lh = static_cast<const bf16_t*>(p.l) + my_token * p.l_row_stride + 4 * g;
   // id of block g of the tile; a block that nobody sees may have any: the one of the last token stands in, weighted zero
@@ -155,7 +155,7 @@ __global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int w = 0; w < KW; ++w) kc[i][w] = *reinterpret_cast<const uint4*>(src + i * 4 * D + w * 16);
+      for (int w = 0; w < KW; ++w) kc[i][w] = *reinterpret_cast<const uint4*>(src + i * 4 * D + w * 64);
     ks_raw = p.k_scale[id * p.scale_block_stride + h];
   };
   auto issue_l = [&](int id) __attribute__((always_inline)) {
@@ -168,7 +168,7 @@ __global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
   auto issue_v = [&](int id) __attribute__((always_inline)) {
     const uint8_t* src = vh + id * p.kv_block_stride;
 #pragma unroll
-    for (int b = 0; b < DB; ++b) vc[b] = *reinterpret_cast<const uint4*>(src + b * 256);
+    for (int b = 0; b < DB; ++b) vc[b] = load_once(src + b * 256);
     vs_raw = p.v_scale[id * p.scale_block_stride + h];
   };
   const int first = t0 + wave;
@@ -184,9 +184,9 @@ __global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
   // ---------------- prologue: Q operands, Qt = Q B_K^T ----------------
   bf16x8 qb[KS];
   {
-    const bf16_t* qr = static_cast<const bf16_t*>(p.q) + static_cast<int64_t>(row) * D + g * (D / 4);
+    const bf16_t* qr = static_cast<const bf16_t*>(p.q) + static_cast<int64_t>(row) * D + g * 16;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qb[ks] = as_bf16x8(*reinterpret_cast<const uint4*>(qr + ks * 8));
+    for (int ks = 0; ks < KS; ++ks) qb[ks] = as_bf16x8(*reinterpret_cast<const uint4*>(qr + (ks >> 1) * 64 + (ks & 1) * 8));
   }
   // Qt^T, ranks by rows: register e of block b is rank 16b + 4g + e, the operand that L Qt^T takes (k = 16: four ranks a lane group).
   // The waves divide the queries (each with its adapter, or the chunk's one) and hand the operands round in LDS.
@@ -198,13 +198,13 @@ __global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
 #pragma unroll 1
     for (int it = wave; it < n_it; it += NS) {
       const int a = p.causal ? a_first : min(max(p.query_adapter[c0 + it], 0), p.n_adapters - 1);
-      const bf16_t* src = static_cast<const bf16_t*>(p.b_k) + static_cast<int64_t>(a) * r * ldb + h * D + g * (D / 4);
+      const bf16_t* src = static_cast<const bf16_t*>(p.b_k) + static_cast<int64_t>(a) * r * ldb + h * D + g * 16;
 #pragma unroll
       for (int b = 0; b < RB; ++b) {
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-          const uint4 bk = 16 * b + l16 < r ? *reinterpret_cast<const uint4*>(src + (16 * b + l16) * ldb + ks * 8) : make_uint4(0u, 0u, 0u, 0u);
+          const uint4 bk = 16 * b + l16 < r ? *reinterpret_cast<const uint4*>(src + (16 * b + l16) * ldb + (ks >> 1) * 64 + (ks & 1) * 8) : make_uint4(0u, 0u, 0u, 0u);
           acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(bk), qb[ks], acc, 0, 0, 0);
         }
         if (p.causal || tok == it) qt_s[b * 64 + lane] = make_uint2(pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3]));

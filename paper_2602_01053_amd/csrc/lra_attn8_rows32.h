@@ -20,7 +20,7 @@ template <int D, int RT, int RP, bool HAS_BK, int CODE>
 __global__ __launch_bounds__(256, attn8_rows32_waves(RP)) void attn8_rows32_kernel(Batch8Params p) {
   constexpr int NS = 4 / RT;          // waves that divide the tiles of one row tile
   constexpr int KS = D / 16;          // k-steps of S^T over the head dimension
-  constexpr int KW = D / 32;          // 16-byte pieces of a lane's half of a K row
+  constexpr int KW = D / 32;          // 16-byte pieces of a K row per lane: one of every two
   constexpr int DB = D / 32;          // 32-row blocks of O^T
   constexpr int RKS = RP / 16;        // k-steps over the padded rank
   constexpr int RB = (RP + 31) / 32;  // 32-row blocks of Olr^T
@@ -78,7 +78,7 @@ __global__ __launch_bounds__(256, attn8_rows32_waves(RP)) void attn8_rows32_kern
   // ---------------- a tile's requests ----------------
   const int my_odd = (l32 >> 2) & 1;                                         // of the A operands of S^T: the tile's second block
   const int my_token = 8 * (l32 >> 4) + 4 * ((l32 >> 3) & 1) + (l32 & 3);
-  const uint8_t* const kh = static_cast<const uint8_t*>(p.k_base) + h * p.kv_head_stride + my_token * D + g2 * (D / 2);
+  const uint8_t* const kh = static_cast<const uint8_t*>(p.k_base) + h * p.kv_head_stride + my_token * D + g2 * 16;
   const uint8_t* const vh = static_cast<const uint8_t*>(p.v_base) + h * p.kv_head_stride + l32 * 16;
   const bf16_t* const lh = static_cast<const bf16_t*>(p.l) + my_token * p.l_row_stride + 8 * g2;
   // lane l: id of block l % 4 of the tile; a block that nobody sees may have any: the one of the last token stands in, weighted zero
@@ -95,7 +95,7 @@ __global__ __launch_bounds__(256, attn8_rows32_waves(RP)) void attn8_rows32_kern
     for (int kt = 0; kt < 2; ++kt) {
       const uint8_t* src = kh + (my_odd ? block(id, 2 * kt + 1) : block(id, 2 * kt)) * p.kv_block_stride;
 #pragma unroll
-      for (int w = 0; w < KW; ++w) kc[kt][w] = *reinterpret_cast<const uint4*>(src + w * 16);
+      for (int w = 0; w < KW; ++w) kc[kt][w] = *reinterpret_cast<const uint4*>(src + w * 32);
     }
     ks_raw = p.k_scale[id * p.scale_block_stride + h];
   };
@@ -112,7 +112,7 @@ __global__ __launch_bounds__(256, attn8_rows32_waves(RP)) void attn8_rows32_kern
     for (int kt = 0; kt < 2; ++kt) {
       const uint8_t* src = vh + (g2 ? block(id, 2 * kt + 1) : block(id, 2 * kt)) * p.kv_block_stride;
 #pragma unroll
-      for (int b = 0; b < DB; ++b) vc[kt][b] = *reinterpret_cast<const uint4*>(src + b * 512);
+      for (int b = 0; b < DB; ++b) vc[kt][b] = load_once(src + b * 512);
     }
     vs_raw = p.v_scale[id * p.scale_block_stride + h];
   };
@@ -127,11 +127,11 @@ __global__ __launch_bounds__(256, attn8_rows32_waves(RP)) void attn8_rows32_kern
   }
 
   // ---------------- prologue: Q operands, Qt = Q B_K^T ----------------
-  // lane (row l32, half g2) of k-step ks: dimensions D/2 g2 + 8 ks + 0..7, the order of a lane's codes of K
+  // lane (row l32, half g2) of k-step ks: dimensions 32 (ks / 2) + 16 g2 + 8 (ks % 2) + 0..7, the order of a lane's codes of K
   {
-    const bf16_t* qr = static_cast<const bf16_t*>(p.q) + static_cast<int64_t>(row) * D + g2 * (D / 2);
+    const bf16_t* qr = static_cast<const bf16_t*>(p.q) + static_cast<int64_t>(row) * D + g2 * 16;
 #pragma unroll
-    for (int i = 0; i < KS / NS; ++i) q_s[rt][stream + NS * i][lane] = *reinterpret_cast<const pf_u32x4*>(qr + (stream + NS * i) * 8);
+    for (int i = 0; i < KS / NS; ++i) q_s[rt][stream + NS * i][lane] = *reinterpret_cast<const pf_u32x4*>(qr + ((stream + NS * i) >> 1) * 32 + ((stream + NS * i) & 1) * 8);
   }
   __syncthreads();
   auto q_of = [&](int ks) __attribute__((always_inline)) -> bf16x8 { return __builtin_bit_cast(bf16x8, q_s[rt][ks][lane]); };
@@ -144,7 +144,7 @@ __global__ __launch_bounds__(256, attn8_rows32_waves(RP)) void attn8_rows32_kern
 #pragma unroll 1
     for (int it = it0 + stream; it < it1; it += NS) {
       const int a = p.causal ? a_first : min(max(p.query_adapter[c0 + it], 0), p.n_adapters - 1);
-      const bf16_t* src = static_cast<const bf16_t*>(p.b_k) + static_cast<int64_t>(a) * r * ldb + h * D + g2 * (D / 2);
+      const bf16_t* src = static_cast<const bf16_t*>(p.b_k) + static_cast<int64_t>(a) * r * ldb + h * D + g2 * 16;
 #pragma unroll 1
       for (int b = 0; b < RB; ++b) {
         pf_f32x16 acc;
@@ -152,7 +152,7 @@ __global__ __launch_bounds__(256, attn8_rows32_waves(RP)) void attn8_rows32_kern
         for (int i = 0; i < 16; ++i) acc[i] = 0.f;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-          const uint4 bk = 32 * b + l32 < r ? *reinterpret_cast<const uint4*>(src + (32 * b + l32) * ldb + ks * 8) : make_uint4(0u, 0u, 0u, 0u);
+          const uint4 bk = 32 * b + l32 < r ? *reinterpret_cast<const uint4*>(src + (32 * b + l32) * ldb + (ks >> 1) * 32 + (ks & 1) * 8) : make_uint4(0u, 0u, 0u, 0u);
           acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(bk), q_of(ks), acc, 0, 0, 0);
         }
 #pragma unroll
