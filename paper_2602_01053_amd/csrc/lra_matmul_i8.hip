@@ -286,13 +286,18 @@ __global__ __launch_bounds__(512, 2) void matmul_i8_wide_kernel(I8Params p) {
   const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(PF_LDS_AS(unsigned char, smem)));
   // request i of thirty-two per tile fills rows 8i .. 8i + 7, wave w has i = w + 8 part; chunk c of row r at c ^ (r / 2) % 8
   const int chunk = (lane & 7) ^ ((4 * wave + (lane >> 4)) & 7);
-  const uint32_t w_off = static_cast<uint32_t>(lane >> 3) * ldw + chunk * 16, x_off = static_cast<uint32_t>(lane >> 3) * ldx + chunk * 16;
+  // (rows by the lanes' offsets: what a resource's size cuts does not hang on how it counts the scalar one)
+  uint32_t w_off[4], x_off[4];
+#pragma unroll
+  for (int part = 0; part < 4; ++part) {
+    const uint32_t row = 8u * (wave + 8 * part) + (lane >> 3);
+    w_off[part] = row * ldw + chunk * 16, x_off[part] = row * ldx + chunk * 16;
+  }
   auto issue = [&](int step, int st, int part) __attribute__((always_inline)) {
-    const int i = wave + 8 * part;
-    const uint32_t dst = lds0 + st * STAGE + i * 1024;
+    const uint32_t dst = lds0 + st * STAGE + (wave + 8 * part) * 1024;
     const bool in = step * BK + chunk * 16 < p.k;  // (behind the last column: zeros)
-    pf_load16_to_lds(rs_w, dst, in ? w_off : kPfOob, 8u * i * ldw + step * BK);
-    pf_load16_to_lds(rs_x, dst + TILE, in ? x_off : kPfOob, 8u * i * ldx + step * BK);
+    pf_load16_to_lds(rs_w, dst, in ? w_off[part] : kPfOob, step * BK);
+    pf_load16_to_lds(rs_x, dst + TILE, in ? x_off[part] : kPfOob, step * BK);
   };
   const int n_steps = (p.k + BK - 1) / BK;
 #pragma unroll
