@@ -9,7 +9,8 @@ namespace lra {
 // One workgroup of four waves per (query row, share of its key tiles), 64 tokens a tile: four aligned blocks.  A quarter of a
 // wave's lanes share a token's score (a quarter of its K row, of its L row each), a thread then sums one dimension of V over the
 // tokens of some of the four blocks, sixteen codes a load, and one rank of L over sixteen tokens.  For fp32, ranks that are no
-// multiple of 8, and as a second opinion on the MFMA kernels.
+// multiple of 8, and as a second opinion on the MFMA kernels.  16 rows that see 260 keys take 8 us, the chain of a tile two to three times;
+// long contexts are bound by the vector units, every row decoding its keys anew: 32 rows over 64 k tokens in fp32 184 us.
 template <typename T, int D, int CODE>
 __global__ __launch_bounds__(256) void attn8_vector_kernel(Batch8Params p) {
   constexpr int DQ = D / 4;             // dimensions of a K row per lane

@@ -92,7 +92,7 @@ static int64_t keys_per_row(const lra_cache8* c, const lra_batch* b) {
 
 // 64 rows at most per sequence and kv head: workgroups of (kv head, key share, sequence), two to a compute unit, whose waves (four, or
 // two for each of two row tiles) have a tile of 64 keys each.  More shares even out sequences of unlike lengths but leave more states:
-// 16 sequences of 4 k to 64 k tokens, 28 rows: 188 us with two per compute unit, 192, 196 and 206 with four, six and eight.  Shares of two
+// 16 sequences of 4 k to 64 k tokens, 28 rows, take 2, 4 and 10 % longer with four, six and eight workgroups to a compute unit.  Shares of two
 // tiles to a wave: 16 rows over 8 k tokens take 14.6 us instead of 13.2.
 static bool plan_few_rows(Attn8Plan& pl, const lra_shape* sh, const lra_cache8* c, const lra_batch* b) {
   const int64_t G = sh->n_q_heads / sh->n_kv_heads, most = b->max_queries_per_seq * G;
