@@ -240,6 +240,8 @@ lra_status lra_attn_batch8(const lra_shape* shape, const lra_cache8* cache, cons
   Batch8Params p = batch8_params(shape, cache, adapters, batch, q);
   p.out = out;
   p.n_splits = pl.n_splits;
+  p.head_shares = pl.head_shares;
+  p.share_least = pl.share_least;
   if (pl.states) {
     char* ws = static_cast<char*>(workspace);
     p.part_ml = reinterpret_cast<float*>(ws + pl.off_ml);

@@ -10,10 +10,14 @@ lra_status check_cache8(const lra_shape* sh, const lra_cache8* c);
 lra_status check_batch8(const lra_shape* sh, const lra_cache8* c, const lra_batch* b);
 lra_status check_new_rows(const lra_shape* sh, const lra_cache8* c, const lra_new_rows* n);
 
+// The most sequences whose key shares the kernels for few rows form by their lengths.
+constexpr int kShareSeqs = 128;
+
 struct Attn8Plan {
   bool launchable;
   bool few_rows, tiles, states;
   int rows, n_splits, row_tiles, tile_places;
+  int head_shares, share_least;  // few rows: shares of a kv head over all sequences (0: n_splits of each), tiles of the shortest
   size_t off_ml, off_o, off_lr, off_adapter, bytes;
 };
 Attn8Plan plan_attn8(const lra_shape* sh, const lra_cache8* c, const lra_batch* b, const Tuning& tune);

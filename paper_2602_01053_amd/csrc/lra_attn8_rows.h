@@ -15,10 +15,11 @@
 // the scales instead, exactly): the codes of a tile cost a wave some 500 cycles, the 16 KB that they stand for 2000 of the memory's.
 // K of a wave's next tile is requested as soon as its scores are taken, V and L as soon as the products are: with eight waves to a
 // compute unit some hundred KB are on their way.
-// Bound by HBM where the shares are long: 14 rows over 16 sequences of 4 k to 64 k tokens 163 us with the merge, 4.8 TB/s of the bytes
-// needed (a large copy reaches 5.2); 16 rows over 32 k tokens of 8 kv heads 17.5 us (68 MB), of which the start, two dependent round trips and Q B_K^T, is 5.
+// Bound by HBM where the shares are long: 14 rows over 16 sequences of 4 k to 64 k tokens 144 us with the merge, 5.4 TB/s of the bytes
+// needed (a large copy reaches 5.2, both directions counted); 16 rows over 32 k tokens of 8 kv heads 17.5 us (68 MB), of which the start, two dependent round trips and Q B_K^T, is 5.
 #pragma once
 
+#include "lra_attn8_plan.h"
 #include "lra_codes.h"
 #include "lra_decode_util.h"
 
@@ -67,17 +68,105 @@ __device__ __forceinline__ uint4 codes_to_values(uint32_t lo, uint32_t hi, float
 
 __device__ __forceinline__ uint4 masked(uint4 v, uint4 m) { return make_uint4(v.x & m.x, v.y & m.y, v.z & m.z, v.w & m.w); }
 
-// Workgroup x -> key share and kv head.  Consecutive workgroups go to consecutive XCDs; the kv heads of a share read the same low-rank
-// rows, so where the shares divide by eight those go to one XCD, one after the other, and meet in its L2.
-__device__ __forceinline__ void attn8_share(const Batch8Params& p, int& split, int& h) {
+// Sequence t: its queries, and the tiles of 64 keys that they see: n_tiles in all, those from sink_tiles on `gap` further.
+struct Attn8Sequence {
+  int n_t, c0, c1, first_pos, lo, sinks, sink_tiles, gap, n_tiles;
+};
+__device__ __forceinline__ Attn8Sequence attn8_sequence(const Batch8Params& p, int t) {
+  Attn8Sequence s;
+  s.n_t = min(p.seq_lens[t], p.max_seq_len);
+  s.c0 = t > 0 ? min(max(p.seq_query_start[t], 0), p.n_queries) : 0;
+  s.c1 = t + 1 < p.n_seqs ? min(max(p.seq_query_start[t + 1], s.c0), p.n_queries) : p.n_queries;
+  s.first_pos = p.causal ? s.n_t - (s.c1 - s.c0) : s.n_t - 1;
+  s.lo = p.window > 0 ? max(0, s.first_pos - p.window + 1) : 0;
+  s.sinks = min(p.sinks, s.lo);
+  s.sink_tiles = (s.sinks + 63) / 64;
+  s.gap = max(0, s.lo / 64 - s.sink_tiles);
+  s.n_tiles = s.n_t <= 0 ? 0 : (s.n_t - 1) / 64 + 1 - s.gap;
+  return s;
+}
+
+// Workgroup -> sequence, kv head, and which of the sequence's `shares` of the keys; false: none.  Consecutive workgroups go to
+// consecutive XCDs; the kv heads of a share read the same low-rank rows, so where the shares divide by eight those go to one XCD, one
+// after the other, and meet in its L2.
+// Of several sequences (kShareSeqs at most) every wave forms the shares by itself: about as long as they are for head_shares of them in all, so
+// that a batch of unlike lengths ends together.  With as many shares for
+// every sequence 16 of 1 k to 64 k tokens (8 kv heads, 16 rows) take 234 us instead of 190, 5.6 TB/s.
+__device__ __forceinline__ bool attn8_share(const Batch8Params& p, int lane, int& t, int& split, int& shares, int& h) {
   const int x = blockIdx.x, Hkv = p.n_kv_heads;
-  if ((p.n_splits & 7) == 0) {
-    const int eight = (x >> 3) / Hkv;
-    h = (x >> 3) - eight * Hkv;
-    split = 8 * eight + (x & 7);
-  } else {
-    split = x / Hkv;
-    h = x - split * Hkv;
+  const int eight = (x >> 3) / Hkv;
+  if (p.head_shares == 0) {
+    t = blockIdx.y;
+    shares = p.n_splits;
+    if ((p.n_splits & 7) == 0) {
+      h = (x >> 3) - eight * Hkv;
+      split = 8 * eight + (x & 7);
+    } else {
+      split = x / Hkv;
+      h = x - split * Hkv;
+    }
+    return true;
+  }
+  h = (x >> 3) - eight * Hkv;
+  int at = 8 * eight + (x & 7);
+  constexpr int N = kShareSeqs / 64;
+  int tiles[N], mine[N];
+  bool queries[N];
+  auto sum = [&](const int (&v)[N]) __attribute__((always_inline)) -> uint32_t {  // (fewer than 2^32: 128 times 2^24)
+    uint32_t s = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) s += static_cast<uint32_t>(v[i]);
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) s += static_cast<uint32_t>(__shfl_xor(static_cast<int>(s), off, kWave));
+    return __builtin_amdgcn_readfirstlane(s);
+  };
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const Attn8Sequence s = attn8_sequence(p, min(64 * i + lane, p.n_seqs - 1));
+    queries[i] = 64 * i + lane < p.n_seqs && s.c1 > s.c0;
+    tiles[i] = queries[i] ? s.n_tiles : 0;
+  }
+  const uint32_t total = sum(tiles);
+  // each sequence rounds its shares up: room for none, half or all of them
+#pragma unroll 1
+  for (int half = 0; half < 3; ++half) {
+    const uint32_t room = max(p.head_shares - half * p.n_seqs / 2, (p.head_shares + 1) / 2);
+    const uint32_t per = max((total + room - 1) / room, static_cast<uint32_t>(p.share_least));
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint32_t n = tiles[i], long_ = max(per, (n + p.n_splits - 1) / p.n_splits);
+      mine[i] = queries[i] ? max(1, static_cast<int>((n + long_ - 1) / long_)) : 0;
+    }
+    if (sum(mine) <= static_cast<uint32_t>(p.head_shares)) break;
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    int upto = mine[i];
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int below = __shfl_up(upto, off, kWave);
+      upto += lane >= off ? below : 0;
+    }
+    const uint64_t beyond = __builtin_amdgcn_ballot_w64(at < upto);
+    if (beyond != 0) {
+      const int k = __builtin_ctzll(beyond);
+      t = 64 * i + k;
+      shares = __builtin_amdgcn_readlane(mine[i], k);
+      split = at - (__builtin_amdgcn_readlane(upto, k) - shares);
+      return true;
+    }
+    at -= __builtin_amdgcn_readlane(upto, 63);
+  }
+  return false;
+}
+
+// The states of shares that a sequence does not have: empty, left by its first.
+__device__ __forceinline__ void attn8_missing_shares(const Batch8Params& p, const Attn8Sequence& s, int n_rows, int h, int shares) {
+  const int missing = p.n_splits - shares;
+  for (int i = threadIdx.x; i < n_rows * missing; i += 256) {
+    const int at = i / missing, tok = at / p.group;
+    const int64_t row = static_cast<int64_t>(s.c0 + tok) * p.n_q_heads + h * p.group + (at - tok * p.group);
+    *reinterpret_cast<float2*>(p.part_ml + (row * p.n_splits + shares + (i - at * missing)) * 2) = make_float2(-INFINITY, 0.f);
   }
 }
 
@@ -95,24 +184,20 @@ __global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
   const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int Hq = p.n_q_heads, Hkv = p.n_kv_heads, G = p.group, r = p.rank;
-  const int t = blockIdx.y;
-  int split, h;
-  attn8_share(p, split, h);
-  const int n_t = min(p.seq_lens[t], p.max_seq_len);
-  const int c0 = t > 0 ? min(max(p.seq_query_start[t], 0), p.n_queries) : 0;
-  const int c1 = t + 1 < p.n_seqs ? min(max(p.seq_query_start[t + 1], c0), p.n_queries) : p.n_queries;
+  int t, split, shares, h;
+  if (!attn8_share(p, lane, t, split, shares, h)) return;
+  const Attn8Sequence seq = attn8_sequence(p, t);
+  const int n_t = seq.n_t, c0 = seq.c0, c1 = seq.c1, first_pos = seq.first_pos, lo = seq.lo, sinks = seq.sinks;
+  const int sink_tiles = seq.sink_tiles, gap = seq.gap, n_tiles = seq.n_tiles, pos_last = n_t - 1;
   const int n_rows = min((c1 - c0) * G, 16);
   if (n_rows == 0) return;
-  const int first_pos = p.causal ? n_t - (c1 - c0) : n_t - 1, pos_last = n_t - 1;
+  if (split == 0 && shares < p.n_splits) attn8_missing_shares(p, seq, n_rows, h, shares);
   // this lane's row (the last one again past the end)
   const int at_row = min(l16, n_rows - 1), tok = at_row / G;
   const int row = (c0 + tok) * Hq + h * G + (at_row - tok * G), pos = first_pos + (p.causal ? tok : 0);
   const bool live = l16 < n_rows;
-  const int lo = p.window > 0 ? max(0, first_pos - p.window + 1) : 0, sinks = min(p.sinks, lo);
-  const int sink_tiles = (sinks + 63) / 64, gap = max(0, lo / 64 - sink_tiles);
-  const int n_tiles = n_t <= 0 ? 0 : (n_t - 1) / 64 + 1 - gap;
-  const int t0 = static_cast<int>(static_cast<int64_t>(n_tiles) * split / p.n_splits);
-  const int t1 = static_cast<int>(static_cast<int64_t>(n_tiles) * (split + 1) / p.n_splits);
+  const int t0 = static_cast<int>(static_cast<int64_t>(n_tiles) * split / shares);
+  const int t1 = static_cast<int>(static_cast<int64_t>(n_tiles) * (split + 1) / shares);
   const int a_first = min(max(p.query_adapter[c0], 0), p.n_adapters - 1);
   const int64_t slot = static_cast<int64_t>(row) * p.n_splits + split;
   auto adapter_of_row = [&]() __attribute__((always_inline)) -> int { return p.causal ? a_first : p.query_adapter[c0 + tok]; };

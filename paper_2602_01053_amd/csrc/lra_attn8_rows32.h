@@ -1,6 +1,6 @@
 // Attention over 8-bit codes for sequences with 17 to 64 query rows per kv head: attn8_rows_kernel with 32 rows to a wave
 // (v_mfma_f32_32x32x16_bf16).  Waves of 16 rows each read every key once per row tile: 16 sequences of 4 k to 64 k tokens with 28 rows took
-// 244 us so (e4m3; integers 258) and take 178 (192), 4.4 TB/s of the bytes needed; 64 rows over 32 k tokens take 40 us, as much by their
+// 244 us so (e4m3; integers 258) and take 156 (168), 5.0 TB/s of the bytes needed; 64 rows over 32 k tokens take 40 us, as much by their
 // states and products as by the reading.
 //
 // Operands straight from the cache, as there: row rho of key tile t (of two) is token 8 (rho / 16) + 4 (rho / 8 % 2) + rho % 4 of block
@@ -8,6 +8,8 @@
 // bytes of a dimension of V as two operands.  Q and Qt wait in LDS, where all waves read the same operands: with them in registers there
 // are too few for two waves per SIMD.
 #pragma once
+
+#include <algorithm>
 
 #include "lra_attn8_rows.h"
 
@@ -34,29 +36,31 @@ __global__ __launch_bounds__(256, attn8_rows32_waves(RP)) void attn8_rows32_kern
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int rt = wave % RT, stream = wave / RT;
   const int Hq = p.n_q_heads, Hkv = p.n_kv_heads, G = p.group, r = p.rank;
-  const int t = blockIdx.y;
-  int split, h;
-  attn8_share(p, split, h);
-  const int n_t = min(p.seq_lens[t], p.max_seq_len);
-  const int c0 = t > 0 ? min(max(p.seq_query_start[t], 0), p.n_queries) : 0;
-  const int c1 = t + 1 < p.n_seqs ? min(max(p.seq_query_start[t + 1], c0), p.n_queries) : p.n_queries;
+  int t, split, shares, h;
+  if (!attn8_share(p, lane, t, split, shares, h)) return;
+  const Attn8Sequence seq = attn8_sequence(p, t);
+  const int n_t = seq.n_t, c0 = seq.c0, c1 = seq.c1, first_pos = seq.first_pos, lo = seq.lo, sinks = seq.sinks;
+  const int sink_tiles = seq.sink_tiles, gap = seq.gap, n_tiles = seq.n_tiles, pos_last = n_t - 1;
   const int n_rows = min((c1 - c0) * G, 32 * RT);
   if (n_rows == 0) return;
-  const int first_pos = p.causal ? n_t - (c1 - c0) : n_t - 1, pos_last = n_t - 1;
+  if (split == 0 && shares < p.n_splits) attn8_missing_shares(p, seq, n_rows, h, shares);
   // this lane's row (the last one again past the end)
   const int at_row = min(32 * rt + l32, n_rows - 1), tok = at_row / G;
   const int row = (c0 + tok) * Hq + h * G + (at_row - tok * G), pos = first_pos + (p.causal ? tok : 0);
   const bool live = 32 * rt + l32 < n_rows;
   const bool has_rows = 32 * rt < n_rows;  // (uniform)
-  const int lo = p.window > 0 ? max(0, first_pos - p.window + 1) : 0, sinks = min(p.sinks, lo);
-  const int sink_tiles = (sinks + 63) / 64, gap = max(0, lo / 64 - sink_tiles);
-  const int n_tiles = n_t <= 0 ? 0 : (n_t - 1) / 64 + 1 - gap;
-  const int t0 = static_cast<int>(static_cast<int64_t>(n_tiles) * split / p.n_splits);
-  const int t1 = static_cast<int>(static_cast<int64_t>(n_tiles) * (split + 1) / p.n_splits);
+  const int t0 = static_cast<int>(static_cast<int64_t>(n_tiles) * split / shares);
+  const int t1 = static_cast<int>(static_cast<int64_t>(n_tiles) * (split + 1) / shares);
   const int a_first = min(max(p.query_adapter[c0], 0), p.n_adapters - 1);
-  const int64_t slot = static_cast<int64_t>(row) * p.n_splits + split;
   auto adapter_of_row = [&]() __attribute__((always_inline)) -> int { return p.causal ? a_first : p.query_adapter[c0 + tok]; };
+  // (formed where it is used: held over the loop, it went to scratch memory)
+  auto slot_of_row = [&]() __attribute__((always_inline)) -> int64_t {
+    int at = row;
+    asm volatile("" : "+v"(at));
+    return static_cast<int64_t>(at) * p.n_splits + split;
+  };
   if (t0 >= t1) {
+    const int64_t slot = slot_of_row();
     // an empty state, all the merge kernel looks at; for a row that sees nothing at all share 0 leaves one that gives zeros
     if (stream == 0 && live) {
       const bool nothing = split == 0 && pos < 0;
@@ -376,6 +380,7 @@ __global__ __launch_bounds__(256, attn8_rows32_waves(RP)) void attn8_rows32_kern
     __syncthreads();
   }
   if (stream != 0 || !live) return;
+  const int64_t slot = slot_of_row();
   if (g2 == 0) {
     const bool nothing = split == 0 && pos < 0;  // (such a row's O and O_lr are zeros)
     p.part_ml[slot * 2 + 0] = nothing ? 0.f : m_all * 0.69314718055994530942f;  // natural-log units
@@ -400,7 +405,9 @@ __global__ __launch_bounds__(256, attn8_rows32_waves(RP)) void attn8_rows32_kern
 // row_tiles: of sixteen rows, 1 (attn8_rows_kernel), 2 or 4
 template <int D, int CODE>
 static hipError_t launch_attn8_rows(const Batch8Params& p, int row_tiles, hipStream_t s) {
-  const dim3 grid(p.n_kv_heads * p.n_splits, p.n_seqs);
+  // (with head_shares: as many as all sequences' rounding up can make of them, by eights)
+  const int most = std::max(p.head_shares, (p.head_shares + 1) / 2 + p.n_seqs);
+  const dim3 grid = p.head_shares > 0 ? dim3(p.n_kv_heads * ((most + 7) / 8 * 8)) : dim3(p.n_kv_heads * p.n_splits, p.n_seqs);
   auto launch = [&](auto rp_c, auto bk_c) {
     constexpr int RP = decltype(rp_c)::value;
     constexpr bool BK = decltype(bk_c)::value;

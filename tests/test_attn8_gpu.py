@@ -82,6 +82,32 @@ def test_adapter_ids_out_of_range(c):
     close_enough(Device8(x, lra).attend(), want, bound, c.label())
 
 
+@pytest.mark.parametrize("code,heads,rank", [("e4m3", (8, 2, 64), 16), ("int8", (14, 2, 128), 32), ("e4m3", (4, 4, 64), 8)])
+@pytest.mark.parametrize("causal,window", [(False, 0), (True, 0), (True, 5000)])
+def test_sequences_of_unlike_lengths(code, heads, rank, causal, window):
+    """A bound beyond which the shares go by the lengths: among them sequences of no tokens, of one, without queries, and of fewer
+    tokens than queries; several sets of lengths under one bound, as a graph meets them."""
+    bound_len = 150000
+    lens = [9000, 1, 0, 64, 700, 4097, 130, 20, 12, 3000, 65, 5, 8192]
+    counts = [2, 1, 1, 0, 2, 1, 2, 1, 0, 2, 1, 2, 1]
+    for order in (lens, lens[::-1], [17] * 13, [0] * 12 + [2500], [6000] + [1] * 12):
+        c = Case8(order, counts, causal=causal, window=window, sinks=3, heads=heads, rank=rank, code=code, seed=len(order))
+        x = make8(c)
+        want, bound = attention_with_bound(x)
+        dev = Device8(x, lra, max_seq_len=bound_len)
+        got = dev.attend()
+        close_enough(got, want, bound, c.label())
+        assert torch.equal(got, dev.attend())
+
+
+def test_shares_of_more_than_64_sequences():
+    for n in (65, 128, 129):
+        c = Case8([700 * (t % 7) + t for t in range(n)], [1 + t % 2 for t in range(n)], heads=(4, 1, 64), rank=8, code="int8", seed=n)
+        x = make8(c)
+        want, bound = attention_with_bound(x)
+        close_enough(Device8(x, lra, max_seq_len=70000).attend(), want, bound, c.label())
+
+
 @pytest.mark.parametrize("n_seqs", [300, 70000])
 @pytest.mark.parametrize("causal", [False, True])
 def test_many_short_sequences(n_seqs, causal):
