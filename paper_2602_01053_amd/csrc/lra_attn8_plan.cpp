@@ -92,7 +92,7 @@ static int64_t keys_per_row(const lra_cache8* c, const lra_batch* b) {
 
 // 64 rows at most per sequence and kv head: workgroups of (kv head, key share, sequence), two to a compute unit, whose waves (four, or
 // two for each of two row tiles) have a tile of 64 keys each.  More shares even out sequences of unlike lengths but leave more states:
-// 16 sequences of 4 k to 64 k tokens, 28 rows, take 2, 4 and 10 % longer with four, six and eight workgroups to a compute unit.  Shares of two
+// 16 sequences of 4 k to 64 k tokens, 28 rows, took 2, 4 and 10 % longer with four, six and eight workgroups to a compute unit.  Shares of two
 // tiles to a wave: 16 rows over 8 k tokens take 14.6 us instead of 13.2.
 // Of several sequences the device forms the shares by their lengths (attn8_share) where equal numbers would have 128 tiles and more, some 25 us:
 // that takes 1.5 us, and rounds up a sequence's shares, so that 32 sequences of 0.5 k to 8 k tokens, two shares each, take 96 us instead of 85;
