@@ -220,7 +220,7 @@ __device__ __forceinline__ bool tile_of(int n_tt, int n_ct, int& tt, int& ct) {
 // k, four stages in LDS (a step's 32 KB are asked for three steps ahead: a tile is a chain of steps with nothing else to hide their
 // latency).  The rows of a stage are 256 / B bytes, their 16-byte chunks exchanged by row (xor), so that sixteen rows' reads spread over
 // the banks.  Bound by the way of a step's 32 KB from L2 into LDS: 0.37 us a step of B = 1 and 0.5 of B = 2, whatever the tokens: 333 tokens x
-// 1056 features of 3584 9.1 us, 1024 x 4096 of 4096 25 us.  (Operands read under the products of the step before changed nothing.)
+// 1056 features of 3584 9.1 us, 1024 x 4096 of 4096 24 us.  (Operands read under the products of the step before changed nothing.)
 template <typename T, int B>
 __global__ __launch_bounds__(512, 2) void matmul_i8_chain_kernel(I8Params p) {
   constexpr int ROWS = 64 * B, BK = 256 / B, CH = BK / 16, NS = 4, TILE = ROWS * BK, STAGE = 2 * TILE;
@@ -321,8 +321,8 @@ __global__ __launch_bounds__(512, 2) void matmul_i8_chain_kernel(I8Params p) {
 // 256 features x 256 tokens by eight waves of 128 x 64 (eight 32 x 32 accumulators): six operand reads for eight products, 64 KB into
 // LDS for 16.8 M multiply-adds.  Steps of 128 bytes of k, two stages, one workgroup per compute unit; the two waves of a SIMD cover each
 // other's reads and requests.  Bound by the matrix cores at the clock that they leave (busy 54 %) and the steps' 64 KB from L2: 4096 tokens x
-// 4096 features of 4096 65 us, 2.1 POP/s; a round of 256 tiles takes 57.  (Steps of 64 bytes in four stages: 76 us, rows in pieces of
-// half a line.)
+// 4096 features of 4096 63 us, 2.2 POP/s; 8192 x 14336 407, 2.4; a round of 256 tiles takes 47 to 54.  (Steps of 64 bytes in four stages: a
+// sixth longer, rows in pieces of half a line.)
 template <typename T>
 __global__ __launch_bounds__(512, 2) void matmul_i8_wide_kernel(I8Params p) {
   constexpr int BK = 128, TILE = 256 * BK, STAGE = 2 * TILE;
@@ -445,22 +445,28 @@ __global__ __launch_bounds__(256) void matmul_i8_far_kernel(I8Params p) {
   }
 }
 
-// Tiles of 64, 128 or 256 a side, a compute unit holding one at a time: a round of the chip takes 10, 21 and 50 to 57 us at k = 4096, so
-// that the fewest rounds by these weights are taken.  A few features behind whole tiles may get the smallest tiles in a launch of their own:
-// 8192 tokens x 6160 features are 800 tiles of 256 in four rounds, 218 us, or 768 in three and 128 small ones.
+// Tiles of 64, 128 or 256 a side, a compute unit holding one at a time: a round of the chip takes 10, 21 and 47 to 54 us at k = 4096, so
+// that the fewest rounds by these weights are taken.  Features behind whole tiles, or behind whole rounds, may get smaller tiles in a launch of
+// their own: 8192 tokens x 6160 features are 800 tiles of 256 in four rounds, 218 us, or 768 in three and 128 of 64, 188; 4096 x 4640 (of 3584)
+// 304 tiles in two rounds, 96 us, or 256 in one and 160 of 128, 76.
 struct I8Split {
-  int side, features;
+  int side, features, rest;  // of the first launch, and the tiles' side of the other
 };
 static int64_t tiles_of(int64_t m, int64_t n, int64_t side) { return (m + side - 1) / side * ((n + side - 1) / side); }
 static I8Split split_features(int64_t m, int64_t n) {
-  auto cost = [&](int64_t features, int side) { return (tiles_of(m, features, side) + 255) / 256 * (side == 256 ? 55 : (side == 128 ? 21 : 10)); };
-  I8Split best{64, static_cast<int>(n)};
+  auto cost = [&](int64_t features, int side) { return (tiles_of(m, features, side) + 255) / 256 * (side == 256 ? 54 : (side == 128 ? 21 : 10)); };
+  I8Split best{64, static_cast<int>(n), 64};
   int64_t least = cost(n, 64);
   for (const int side : {128, 256}) {
-    const int64_t whole = n / side * side;
-    if (cost(n, side) < least) least = cost(n, side), best = {side, static_cast<int>(n)};
-    if (whole > 0 && whole < n && cost(whole, side) + cost(n - whole, 64) + 3 < least)
-      least = cost(whole, side) + cost(n - whole, 64) + 3, best = {side, static_cast<int>(whole)};
+    if (cost(n, side) < least) least = cost(n, side), best = {side, static_cast<int>(n), 64};
+    const int64_t rows = (m + side - 1) / side;
+    for (const int64_t columns : {n / side, tiles_of(m, n, side) / 256 * 256 / rows})
+      for (const int rest : {64, 128}) {
+        const int64_t first = columns * side;
+        if (first <= 0 || first >= n || rest >= side) continue;
+        const int64_t both = cost(first, side) + cost(n - first, rest) + 3;
+        if (both < least) least = both, best = {side, static_cast<int>(first), rest};
+      }
   }
   return best;
 }
@@ -491,7 +497,9 @@ static void launch_matmul(const I8Params& p, hipStream_t s) {
   if (sp.side == 256) hipLaunchKernelGGL((matmul_i8_wide_kernel<T>), grid(first, 256), dim3(512), 0, s, first);
   else if (sp.side == 128) hipLaunchKernelGGL((matmul_i8_chain_kernel<T, 2>), grid(first, 128), dim3(512), 0, s, first);
   else hipLaunchKernelGGL((matmul_i8_chain_kernel<T, 1>), grid(first, 64), dim3(512), 0, s, first);
-  if (rest.n > 0) hipLaunchKernelGGL((matmul_i8_chain_kernel<T, 1>), grid(rest, 64), dim3(512), 0, s, rest);
+  if (rest.n <= 0) return;
+  if (sp.rest == 128) hipLaunchKernelGGL((matmul_i8_chain_kernel<T, 2>), grid(rest, 128), dim3(512), 0, s, rest);
+  else hipLaunchKernelGGL((matmul_i8_chain_kernel<T, 1>), grid(rest, 64), dim3(512), 0, s, rest);
 }
 
 }  // namespace lra
