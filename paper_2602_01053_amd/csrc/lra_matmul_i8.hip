@@ -89,53 +89,42 @@ __device__ __forceinline__ void store_scaled(const I8Params& p, int i, int j, in
 
 // The sums' order does not matter (integers), the scaling is the same everywhere: all kernels below give the same bits.
 
-// Few tokens (32 at most): the weights are read once and nothing else counts.  A workgroup of eight waves takes 16 features and all
+// Few tokens (eight at most): the weights are read once and nothing else counts.  A workgroup of eight waves takes 16 features and all
 // tokens, a wave every eighth 64-wide piece of k, eight pieces of its weights requested at a time; operands straight from memory
-// (v_mfma_i32_16x16x64_i8: a lane's 16 bytes of a row are its operand), the waves' sums meet in LDS.  RT: token tiles of 16.  4 tokens x
-// 2064 features of 4096 (8.5 MB) take 5.0 us, a chain of the launch, one round trip, the exchange and the store.
-template <typename T, int RT>
+// (v_mfma_i32_16x16x64_i8: a lane's 16 bytes of a row are its operand), the waves' sums meet in LDS.  4 tokens x 2064 features of 4096
+// (8.5 MB) take 4.9 us, a chain of the launch, one round trip, the exchange and the store; in tiles of 32 5.9.
+template <typename T>
 __global__ __launch_bounds__(512) void matmul_i8_stream_kernel(I8Params p) {
   constexpr int U = 8;
-  __shared__ int sums[8][RT][4][64];
+  __shared__ int sums[8][4][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, g = lane >> 4;
   const int j0 = static_cast<int>(blockIdx.x) * 16;
   const int8_t* wr = p.w + min(j0 + l16, p.n - 1) * p.w_stride + 16 * g;
-  const int8_t* xr[RT];
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) xr[rt] = p.x + min(16 * rt + l16, p.m - 1) * p.x_stride + 16 * g;
-  i32x4 acc[RT];
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) acc[rt] = i32x4{0, 0, 0, 0};
+  const int8_t* xr = p.x + min(l16, p.m - 1) * p.x_stride + 16 * g;
+  i32x4 acc = {0, 0, 0, 0};
   for (int c0 = wave * 64; c0 < p.k; c0 += 8 * 64 * U) {
-    i32x4 a[U], b[U][RT];
+    i32x4 a[U], b[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int c = c0 + u * 512;
       const bool in = c + 16 * g < p.k;
       a[u] = in ? *reinterpret_cast<const i32x4*>(wr + c) : i32x4{0, 0, 0, 0};
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) b[u][rt] = in ? *reinterpret_cast<const i32x4*>(xr[rt] + c) : i32x4{0, 0, 0, 0};
+      b[u] = in ? *reinterpret_cast<const i32x4*>(xr + c) : i32x4{0, 0, 0, 0};
     }
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) acc[rt] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[u], b[u][rt], acc[rt], 0, 0, 0);
+    for (int u = 0; u < U; ++u) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[u], b[u], acc, 0, 0, 0);
   }
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) sums[wave][rt][e][lane] = acc[rt][e];
+  for (int e = 0; e < 4; ++e) sums[wave][e][lane] = acc[e];
   __syncthreads();
-  // register e: feature j0 + 4g + e of token 16 rt + l16; neighbouring threads take neighbouring features
-  for (int i = threadIdx.x; i < RT * 256; i += 512) {
-    const int f = i & 15, tok = i >> 4;
-    if (tok >= p.m || j0 + f >= p.n) continue;
-    int sum = 0;
+  // register e: feature j0 + 4g + e of token l16; neighbouring threads take neighbouring features
+  const int f = threadIdx.x & 15, tok = threadIdx.x >> 4;
+  if (tok >= min(p.m, 16) || j0 + f >= p.n) return;
+  int sum = 0;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) sum += sums[w][tok >> 4][f & 3][(f >> 2) * 16 + (tok & 15)];
-    store_scaled<T>(p, tok, j0 + f, sum);
-  }
+  for (int w = 0; w < 8; ++w) sum += sums[w][f & 3][(f >> 2) * 16 + tok];
+  store_scaled<T>(p, tok, j0 + f, sum);
 }
 
 // The scaled sums of a 32 x 32 block: register i of a lane is feature f0 + 8 (i / 4) + 4 g2 + i % 4 of token `tok`.
@@ -216,14 +205,102 @@ __device__ __forceinline__ bool tile_of(int n_tt, int n_ct, int& tt, int& ct) {
   return true;
 }
 
-// 64 B features x 64 B tokens by eight waves, two of which divide k of each of the four blocks of 32 B x 32 B.  Steps of 256 / B bytes of
-// k, four stages in LDS (a step's 32 KB are asked for three steps ahead: a tile is a chain of steps with nothing else to hide their
-// latency).  The rows of a stage are 256 / B bytes, their 16-byte chunks exchanged by row (xor), so that sixteen rows' reads spread over
-// the banks.  Bound by the way of a step's 32 KB from L2 into LDS: 0.37 us a step of B = 1 and 0.5 of B = 2, whatever the tokens: 333 tokens x
-// 1056 features of 3584 9.1 us, 1024 x 4096 of 4096 24 us.  (Operands read under the products of the step before changed nothing.)
-template <typename T, int B>
+// 32 FB features x 32 TB tokens by eight waves, 8 / (FB TB) of which divide k of each of the 32 x 32 blocks.  Steps of 256 bytes of k, four
+// stages in LDS (a step's tiles are asked for three steps ahead: a workgroup is a chain of steps with nothing else to hide their latency).
+// A row of a stage is 256 bytes, its 16-byte chunks exchanged by row (xor), so that sixteen rows' reads spread over the banks.  Bound by
+// the way of a step's 8 (FB + TB) KB from L2 into LDS, whatever the tokens (five stages changed nothing), so the smaller the tiles the shorter the chain, as long as
+// the chip holds them: 64 tokens x 4096 features of 4096 take 6.0 us in tiles of 32, 7.4 of 64 x 32 and 9.5 of 64; 128 tokens 8.7, 7.8 and 9.5;
+// 256 tokens 15.9, 14 and 10.4.
+template <typename T, int FB, int TB>
+__global__ __launch_bounds__(512, 2) void matmul_i8_small_kernel(I8Params p) {
+  constexpr int BK = 256, NS = 4, W_TILE = 32 * FB * BK, STAGE = W_TILE + 32 * TB * BK, NB = FB * TB, KG = 8 / NB, KS = 8 / KG;
+  constexpr int SUMS = 8 * 1024 * 4;
+  __shared__ __align__(16) unsigned char smem[NS * STAGE > SUMS ? NS * STAGE : SUMS];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l32 = lane & 31, g2 = lane >> 5;
+  int tt, ct;
+  if (!tile_of((p.m + 32 * TB - 1) / (32 * TB), (p.n + 32 * FB - 1) / (32 * FB), tt, ct)) return;
+  const int tok0 = tt * 32 * TB, feat0 = ct * 32 * FB;
+  const uint32_t ldw = static_cast<uint32_t>(p.w_stride), ldx = static_cast<uint32_t>(p.x_stride);  // (at most 2^22)
+  const pf_u32x4 rs_w = pf_rsrc(p.w + feat0 * p.w_stride, (min(32 * FB, p.n - feat0) - 1u) * ldw + p.k);
+  const pf_u32x4 rs_x = pf_rsrc(p.x + tok0 * p.x_stride, (min(32 * TB, p.m - tok0) - 1u) * ldx + p.k);
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(PF_LDS_AS(unsigned char, smem)));
+  // request i of eight per 32 rows fills rows 4i .. 4i + 3; wave w has i = w of each 32
+  const int row = 4 * wave + (lane >> 4), chunk = (lane & 15) ^ (row & 15);
+  const int n_steps = (p.k + BK - 1) / BK;
+  auto issue = [&](int step) __attribute__((always_inline)) {
+    const bool in = step * BK + chunk * 16 < p.k;  // (behind the last column: zeros)
+    const uint32_t dst = lds0 + (step % NS) * STAGE + wave * 1024;
+#pragma unroll
+    for (int q = 0; q < FB; ++q) pf_load16_to_lds(rs_w, dst + q * 32 * BK, in ? (row + 32u * q) * ldw + chunk * 16 : kPfOob, step * BK);
+#pragma unroll
+    for (int q = 0; q < TB; ++q) pf_load16_to_lds(rs_x, dst + W_TILE + q * 32 * BK, in ? (row + 32u * q) * ldx + chunk * 16 : kPfOob, step * BK);
+  };
+  for (int s = 0; s < NS - 1; ++s)
+    if (s < n_steps) issue(s);
+  const int blk = wave % NB, kg = wave / NB, fb = blk % FB, tb = blk / FB;
+  const int a_row = (32 * fb + l32) * BK, b_row = W_TILE + (32 * tb + l32) * BK, swap = l32 & 15;
+  i32x16 acc;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) acc[i] = 0;
+  for (int s = 0; s < n_steps; ++s) {
+    // this step's requests of the wave are here, those of the two behind it may be on their way
+    if (s + 2 < n_steps) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * (FB + TB)));
+    else if (s + 1 < n_steps) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(FB + TB));
+    else pf_wait_vm0();
+    __syncthreads();  // ... and everybody's; and everybody has read the stage that is filled next
+    if (s + NS - 1 < n_steps) issue(s + NS - 1);
+    const unsigned char* st = smem + (s % NS) * STAGE;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const int c = ((2 * (KS * kg + ks) + g2) ^ swap) << 4;
+      const i32x4 a = *reinterpret_cast<const i32x4*>(st + a_row + c), b = *reinterpret_cast<const i32x4*>(st + b_row + c);
+      acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, acc, 0, 0, 0);
+    }
+  }
+  // the waves of a block meet in LDS, each of them adds up and stores its part of the registers: register i of a lane is feature
+  // 8 (i / 4) + 4 g2 + i % 4 of its token
+  constexpr int R = 16 / KG, V = R < 4 ? R : 4;
+  __syncthreads();
+  int* const sums = reinterpret_cast<int*>(smem) + blk * 1024 + lane;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) sums[kg * NB * 1024 + i * 64] = acc[i];
+  __syncthreads();
+  const int tok = tok0 + 32 * tb + l32;
+  if (tok >= p.m) return;
+  const float xs = p.x_scale[tok];
+  T* const out = static_cast<T*>(p.y) + tok * p.y_stride;
+  const bool whole = p.y_stride % V == 0;  // (V features lie together and aligned)
+#pragma unroll
+  for (int o = 0; o < R; o += V) {
+    const int i0 = R * kg + o, f = feat0 + 32 * fb + 8 * (i0 >> 2) + 4 * g2 + (i0 & 3);
+    float v[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      int sum = 0;
+#pragma unroll
+      for (int g = 0; g < KG; ++g) sum += sums[g * NB * 1024 + (i0 + e) * 64];
+      v[e] = static_cast<float>(sum) * xs * p.w_scale[min(f + e, p.n - 1)];
+    }
+    if (whole && f + V <= p.n) {
+      if constexpr (V == 4 && sizeof(T) == 2) *reinterpret_cast<uint2*>(out + f) = make_uint2(pf_pack2(v[0], v[1]), pf_pack2(v[2], v[3]));
+      else if constexpr (V == 4) *reinterpret_cast<float4*>(out + f) = make_float4(v[0], v[1], v[2], v[3]);
+      else if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t*>(out + f) = pf_pack2(v[0], v[1]);
+      else *reinterpret_cast<float2*>(out + f) = make_float2(v[0], v[1]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        if (f + e < p.n) out[f + e] = from_f32<T>(v[e]);
+    }
+  }
+}
+
+// 128 features x 128 tokens by eight waves, two of which divide k of each of the four blocks of 64 x 64.  As above, in steps of 128 bytes and
+// with the same bound, 0.5 us a step: 1024 tokens x 4096 features of 4096 24 us.  (Operands read under the products of the step before
+// changed nothing.)
+template <typename T>
 __global__ __launch_bounds__(512, 2) void matmul_i8_chain_kernel(I8Params p) {
-  constexpr int ROWS = 64 * B, BK = 256 / B, CH = BK / 16, NS = 4, TILE = ROWS * BK, STAGE = 2 * TILE;
+  constexpr int B = 2, ROWS = 64 * B, BK = 256 / B, CH = BK / 16, NS = 4, TILE = ROWS * BK, STAGE = 2 * TILE;
   __shared__ __align__(16) unsigned char smem[NS * STAGE];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l32 = lane & 31, g2 = lane >> 5;
@@ -281,41 +358,29 @@ __global__ __launch_bounds__(512, 2) void matmul_i8_chain_kernel(I8Params p) {
         for (int j = 0; j < B; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(a[i], b[j], acc[i][j], 0, 0, 0);
     }
   }
-  // the second half of k is added to the first; of several blocks each half stores those of one token column
+  // each half of k has the sums of one token column of its blocks from the other
   __syncthreads();
   int* other = reinterpret_cast<int*>(smem) + (wave & 3) * (B * B * 1024) + lane;
-  if constexpr (B == 1) {
-    if (kh == 1) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) other[i * 64] = acc[0][0][i];
+  for (int a = 0; a < B; ++a)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) other[((kh ^ 1) * B + a) * 1024 + i * 64] = kh ? acc[a][0][i] : acc[a][1][i];
+  __syncthreads();
+  i32x16 sum[B];
+#pragma unroll
+  for (int a = 0; a < B; ++a)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum[a][i] = (kh ? acc[a][1][i] : acc[a][0][i]) + other[(kh * B + a) * 1024 + i * 64];
+  const int tok = tok0 + 32 * (B * tb + kh), f0 = feat0 + 32 * B * fb;
+  if constexpr (sizeof(T) == 2) {
+    if ((p.y_stride & 7) == 0) {
+      store_by_rows<B, 1>(p, smem + 4 * B * B * 4096 + wave * B * 2048, tok, f0, lane, [&](int a, int) -> const i32x16& { return sum[a]; });
+      return;
     }
-    __syncthreads();
-    if (kh == 1) return;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) acc[0][0][i] += other[i * 64];
-    store_block<T>(p, acc[0][0], tok0 + 32 * tb + l32, feat0 + 32 * fb, g2);
-  } else {
-#pragma unroll
-    for (int a = 0; a < B; ++a)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) other[((kh ^ 1) * B + a) * 1024 + i * 64] = kh ? acc[a][0][i] : acc[a][1][i];
-    __syncthreads();
-    i32x16 sum[B];
-#pragma unroll
-    for (int a = 0; a < B; ++a)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sum[a][i] = (kh ? acc[a][1][i] : acc[a][0][i]) + other[(kh * B + a) * 1024 + i * 64];
-    const int tok = tok0 + 32 * (B * tb + kh), f0 = feat0 + 32 * B * fb;
-    if constexpr (sizeof(T) == 2) {
-      if ((p.y_stride & 7) == 0) {
-        store_by_rows<B, 1>(p, smem + 4 * B * B * 4096 + wave * B * 2048, tok, f0, lane, [&](int a, int) -> const i32x16& { return sum[a]; });
-        return;
-      }
-    }
-#pragma unroll
-    for (int a = 0; a < B; ++a)
-      if (f0 + 32 * a < p.n) store_block<T>(p, sum[a], tok + l32, f0 + 32 * a, g2);
   }
+#pragma unroll
+  for (int a = 0; a < B; ++a)
+    if (f0 + 32 * a < p.n) store_block<T>(p, sum[a], tok + l32, f0 + 32 * a, g2);
 }
 
 // 256 features x 256 tokens by eight waves of 128 x 64 (eight 32 x 32 accumulators): six operand reads for eight products, 64 KB into
@@ -445,41 +510,61 @@ __global__ __launch_bounds__(256) void matmul_i8_far_kernel(I8Params p) {
   }
 }
 
-// Tiles of 64, 128 or 256 a side, a compute unit holding one at a time: a round of the chip takes 10, 21 and 47 to 54 us at k = 4096, so
-// that the fewest rounds by these weights are taken.  Features behind whole tiles, or behind whole rounds, may get smaller tiles in a launch of
-// their own: 8192 tokens x 6160 features are 800 tiles of 256 in four rounds, 218 us, or 768 in three and 128 of 64, 188; 4096 x 4640 (of 3584)
-// 304 tiles in two rounds, 96 us, or 256 in one and 160 of 128, 76.
-struct I8Split {
-  int side, features, rest;  // of the first launch, and the tiles' side of the other
+// Tiles of 32 to 256 a side by what they cost: a launch and the rounds of the chip that it takes, a compute unit holding one tile at a
+// time (two of 32, which the figures count as two rounds of half the length).  Features behind whole tiles, or behind whole rounds,
+// may get smaller tiles in a launch of their own: 8192 tokens x 6160 features are 800 tiles of 256 in four rounds, 218 us, or 768 in
+// three and a few small ones, 188; 4096 x 4640 (of 3584) 304 tiles in two rounds, 96 us, or 256 in one and 160 of 128, 76.
+enum I8Tile { kTile32, kTile64x32, kTile32x64, kTile64, kTile128, kTile256 };  // features x tokens
+struct I8Shape {
+  int features, tokens, start, round;  // time of a launch and of each round of the chip, in 0.1 us at k = 4096
 };
-static int64_t tiles_of(int64_t m, int64_t n, int64_t side) { return (m + side - 1) / side * ((n + side - 1) / side); }
+constexpr I8Shape kI8Shapes[] = {{32, 32, 24, 32}, {64, 32, 8, 64}, {32, 64, 8, 64}, {64, 64, 5, 88}, {128, 128, 0, 210}, {256, 256, 0, 540}};
+struct I8Split {
+  int tile, features, rest;  // of the first launch, and the tile of the other
+};
+static int64_t tiles_of(int64_t m, int64_t n, int tile) {
+  const I8Shape& s = kI8Shapes[tile];
+  return (m + s.tokens - 1) / s.tokens * ((n + s.features - 1) / s.features);
+}
 static I8Split split_features(int64_t m, int64_t n) {
-  auto cost = [&](int64_t features, int side) { return (tiles_of(m, features, side) + 255) / 256 * (side == 256 ? 54 : (side == 128 ? 21 : 10)); };
-  I8Split best{64, static_cast<int>(n), 64};
-  int64_t least = cost(n, 64);
-  for (const int side : {128, 256}) {
-    if (cost(n, side) < least) least = cost(n, side), best = {side, static_cast<int>(n), 64};
-    const int64_t rows = (m + side - 1) / side;
-    for (const int64_t columns : {n / side, tiles_of(m, n, side) / 256 * 256 / rows})
-      for (const int rest : {64, 128}) {
+  auto cost = [&](int64_t features, int tile) { return kI8Shapes[tile].start + (tiles_of(m, features, tile) + 255) / 256 * kI8Shapes[tile].round; };
+  I8Split best{kTile64, static_cast<int>(n), kTile64};
+  int64_t least = cost(n, kTile64);
+  for (int tile = kTile32; tile <= kTile256; ++tile) {
+    if (cost(n, tile) < least) least = cost(n, tile), best = {tile, static_cast<int>(n), kTile64};
+    if (tile < kTile128) continue;
+    const int64_t side = kI8Shapes[tile].features, rows = (m + side - 1) / side;
+    for (const int64_t columns : {n / side, tiles_of(m, n, tile) / 256 * 256 / rows})
+      for (int rest = kTile32; rest < tile; ++rest) {
         const int64_t first = columns * side;
-        if (first <= 0 || first >= n || rest >= side) continue;
-        const int64_t both = cost(first, side) + cost(n - first, rest) + 3;
-        if (both < least) least = both, best = {side, static_cast<int>(first), rest};
+        if (first <= 0 || first >= n) continue;
+        const int64_t both = cost(first, tile) + cost(n - first, rest) + 30;
+        if (both < least) least = both, best = {tile, static_cast<int>(first), rest};
       }
   }
   return best;
 }
 
 template <typename T>
+static void launch_tiles(const I8Params& p, int tile, hipStream_t s) {
+  const dim3 grid(static_cast<unsigned>((tiles_of(p.m, p.n, tile) + 7) / 8 * 8));
+  switch (tile) {
+    case kTile32: hipLaunchKernelGGL((matmul_i8_small_kernel<T, 1, 1>), grid, dim3(512), 0, s, p); break;
+    case kTile64x32: hipLaunchKernelGGL((matmul_i8_small_kernel<T, 2, 1>), grid, dim3(512), 0, s, p); break;
+    case kTile32x64: hipLaunchKernelGGL((matmul_i8_small_kernel<T, 1, 2>), grid, dim3(512), 0, s, p); break;
+    case kTile64: hipLaunchKernelGGL((matmul_i8_small_kernel<T, 2, 2>), grid, dim3(512), 0, s, p); break;
+    case kTile128: hipLaunchKernelGGL((matmul_i8_chain_kernel<T>), grid, dim3(512), 0, s, p); break;
+    default: hipLaunchKernelGGL((matmul_i8_wide_kernel<T>), grid, dim3(512), 0, s, p);
+  }
+}
+
+template <typename T>
 static void launch_matmul(const I8Params& p, hipStream_t s) {
   constexpr int64_t kNear = int64_t{1} << 22;  // 256 rows within 32-bit offsets below the one that stands for "outside"
-  // (up to 32 tokens while the chip holds all workgroups at once, 16 at any width: 32 tokens x 4640 features of 3584 take 15.3 us in two
-  // rounds, and 8.4 us in tiles of 64; 4096 of 4096 8.4 and 9.5 us)
-  if (p.m <= 16 || (p.m <= 32 && p.n <= 16 * 256)) {
-    const dim3 grid((p.n + 15) / 16);
-    if (p.m <= 16) hipLaunchKernelGGL((matmul_i8_stream_kernel<T, 1>), grid, dim3(512), 0, s, p);
-    else hipLaunchKernelGGL((matmul_i8_stream_kernel<T, 2>), grid, dim3(512), 0, s, p);
+  // (while the chip holds all workgroups at once: 4 tokens x 6160 features of 4096 take 8.1 us in two rounds, in tiles of 32 6.6; of 4096
+  // features 5.6 and 6.0; 16 tokens x 4096 6.4 and 6.0)
+  if (p.m <= 8 && p.n <= 16 * 256) {
+    hipLaunchKernelGGL((matmul_i8_stream_kernel<T>), dim3((p.n + 15) / 16), dim3(512), 0, s, p);
     return;
   }
   if (p.x_stride > kNear || p.w_stride > kNear) {
@@ -493,13 +578,8 @@ static void launch_matmul(const I8Params& p, hipStream_t s) {
   rest.w += sp.features * p.w_stride;
   rest.w_scale += sp.features;
   rest.y = static_cast<T*>(p.y) + sp.features;
-  auto grid = [](const I8Params& q, int side) { return dim3(static_cast<unsigned>((tiles_of(q.m, q.n, side) + 7) / 8 * 8)); };
-  if (sp.side == 256) hipLaunchKernelGGL((matmul_i8_wide_kernel<T>), grid(first, 256), dim3(512), 0, s, first);
-  else if (sp.side == 128) hipLaunchKernelGGL((matmul_i8_chain_kernel<T, 2>), grid(first, 128), dim3(512), 0, s, first);
-  else hipLaunchKernelGGL((matmul_i8_chain_kernel<T, 1>), grid(first, 64), dim3(512), 0, s, first);
-  if (rest.n <= 0) return;
-  if (sp.rest == 128) hipLaunchKernelGGL((matmul_i8_chain_kernel<T, 2>), grid(rest, 128), dim3(512), 0, s, rest);
-  else hipLaunchKernelGGL((matmul_i8_chain_kernel<T, 1>), grid(rest, 64), dim3(512), 0, s, rest);
+  launch_tiles<T>(first, sp.tile, s);
+  if (rest.n > 0) launch_tiles<T>(rest, sp.rest, s);
 }
 
 }  // namespace lra

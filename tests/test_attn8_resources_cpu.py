@@ -23,10 +23,11 @@ def test_tile_walking_kernels_two_workgroups_per_compute_unit(table):  # noqa: F
 
 
 def test_products_of_integers(table):  # noqa: F811
-    """A workgroup of eight waves per compute unit with its stages in LDS, two of the kernel for few tokens."""
-    for kernel in ("matmul_i8_chain_kernel", "matmul_i8_wide_kernel"):
+    """A workgroup of eight waves per compute unit with its stages in LDS, two of the kernel for few tokens and of tiles of 32."""
+    for kernel in ("matmul_i8_small_kernel", "matmul_i8_chain_kernel", "matmul_i8_wide_kernel"):
         for name, row in rows_of(table, kernel).items():
             assert row[SCRATCH] == 0 and row[OCC] >= 2 and row[LDS] <= 128 * 1024, (name, row)
+    assert sum(row[OCC] >= 4 and row[LDS] <= 80 * 1024 for row in rows_of(table, "matmul_i8_small_kernel").values()) == 2
     for name, row in rows_of(table, "matmul_i8_stream_kernel").items():
         assert row[SCRATCH] == 0 and row[OCC] >= 2 and row[LDS] <= 80 * 1024, (name, row)
 

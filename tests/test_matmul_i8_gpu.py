@@ -66,7 +66,8 @@ SIZES = [(1, 1, 16), (1, 2064, 4096), (4, 100, 48), (3, 17, 80), (16, 64, 64), (
          (100, 2064, 4096), (128, 128, 128), (129, 300, 2000), (333, 1056, 3584), (600, 520, 272), (1025, 2064, 1040), (2048, 700, 64), (5, 5000, 96),
          (300, 33, 16384), (7, 9, (1 << 17) - 16),
          # either side of the rules: few tokens, few enough features, tiles of 128 and 256, features left over for the smallest tiles
-         (16, 4112, 64), (32, 4096, 80), (32, 4097, 80), (33, 4096, 48), (2048, 2048, 400), (2047, 2065, 1040), (1900, 2100, 16), (4096, 4112, 48),
+         (8, 4096, 64), (9, 4096, 80), (8, 4097, 80), (33, 4096, 48), (1, 4100, 272), (64, 4095, 272), (100, 4098, 528), (130, 2100, 1040),
+         (16, 4112, 64), (32, 4096, 80), (32, 4097, 80), (200, 1062, 3600), (333, 1057, 64), (40, 14336, 48), (70, 14337, 16), (2048, 2048, 400), (2047, 2065, 1040), (1900, 2100, 16), (4096, 4112, 48),
          (4096, 4640, 32), (2990, 6152, 16), (1024, 4643, 48)]
 
 
