@@ -9,13 +9,14 @@ namespace lra {
 // One workgroup of four waves per (query row, share of its key tiles), 64 tokens a tile: four aligned blocks.  A quarter of a
 // wave's lanes share a token's score (a quarter of its K row, of its L row each), a thread then sums one dimension of V over the
 // tokens of some of the four blocks, sixteen codes a load, and one rank of L over sixteen tokens.  For fp32, ranks that are no
-// multiple of 8, and as a second opinion on the MFMA kernels.  16 rows that see 260 keys take 8 us, the chain of a tile two to three times;
-// long contexts are bound by the vector units, every row decoding its keys anew: 32 rows over 64 k tokens in fp32 184 us.
+// multiple of 8, and as a second opinion on the MFMA kernels.  16 rows that see 260 keys take 7.5 us, the chain of a tile two to three times;
+// long contexts are bound by the vector units, every row decoding its keys anew: 32 rows over 64 k tokens in fp32 167 us.
 template <typename T, int D, int CODE>
 __global__ __launch_bounds__(256) void attn8_vector_kernel(Batch8Params p) {
   constexpr int DQ = D / 4;             // dimensions of a K row per lane
   constexpr int VB = 4 * D / 256;       // blocks of a tile per thread (2 or 1)
   __shared__ float q_s[D], qt_s[64], s_s[64], ks_s[4], vs_s[4], o_s[256], lr_s[256];
+  __shared__ __align__(16) float p_s[4][64];  // the tile's weights, of each wave for itself
   __shared__ int id_s[4];
   const int tid = threadIdx.x, lane = tid & 63;
   const int Hq = p.n_q_heads, Hkv = p.n_kv_heads, r = p.rank;
@@ -107,7 +108,9 @@ __global__ __launch_bounds__(256) void attn8_vector_kernel(Batch8Params p) {
     const float alpha = m == -INFINITY ? 0.f : expf(m - m_new);
     const float pj = s == -INFINITY || m_new == -INFINITY ? 0.f : expf(s - m_new);
     m = m_new;
-    ell = ell * alpha + wave_sum(pj);
+    ell = ell * alpha + pj;  // (of this lane's tokens)
+    p_s[piece][lane] = pj;  // (by lanes' exchange instead, sixteen at a time, 200 rows over 2 k tokens took 733 us instead of 565)
+    __builtin_amdgcn_wave_barrier();
     o *= alpha;
     olr *= alpha;
 #pragma unroll
@@ -121,25 +124,29 @@ __global__ __launch_bounds__(256) void attn8_vector_kernel(Batch8Params p) {
       for (int c = 0; c < 4; ++c) {
         float x[4];
         decode4<CODE>(w[c], x);
+        const float4 p4 = *reinterpret_cast<const float4*>(&p_s[piece][16 * blk + 4 * c]);
+        const float pk[4] = {p4.x, p4.y, p4.z, p4.w};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float pk = __shfl(pj, 16 * blk + 4 * c + e, kWave);
-          acc = pk == 0.f ? acc : fmaf(pk, x[e], acc);  // (a token that is not seen adds nothing, whatever its code)
-        }
+        for (int e = 0; e < 4; ++e) acc = pk[e] == 0.f ? acc : fmaf(pk[e], x[e], acc);  // (a token that is not seen adds nothing, whatever its code)
       }
       o = fmaf(acc, vs_s[blk], o);
     }
     {
       const int id = id_s[piece];
       const T* src = static_cast<const T*>(p.l) + static_cast<int64_t>(id) * 16 * p.l_row_stride + min(rho_of, r - 1);
+      T x[16];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float pk = __shfl(pj, 16 * piece + e, kWave);
-        const float x = to_f32<T>(src[e * p.l_row_stride]);
-        olr = pk == 0.f ? olr : fmaf(pk, x, olr);
+      for (int e = 0; e < 16; ++e) x[e] = src[e * p.l_row_stride];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const float4 p4 = *reinterpret_cast<const float4*>(&p_s[piece][16 * piece + 4 * c]);
+        const float pk[4] = {p4.x, p4.y, p4.z, p4.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) olr = pk[e] == 0.f ? olr : fmaf(pk[e], to_f32<T>(x[4 * c + e]), olr);
       }
     }
   }
+  ell = wave_sum(ell);
   o_s[tid] = o;
   lr_s[tid] = olr;
   __syncthreads();

@@ -149,7 +149,7 @@ Attn8Plan plan_attn8(const lra_shape* sh, const lra_cache8* c, const lra_batch* 
     if (plan_tiles(pl, sh, c, b)) return pl;
   }
   // vector-ALU kernel: one workgroup per row and share, three to a compute unit; a share of 128 keys at least (a window of 256 keys
-  // and 16 rows take 10.7 us, 12.7 in shares of 256)
+  // and 16 rows take 10.2 us, 2 more in shares of 256)
   pl.n_splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({3 * kCUs / rows, (keys + 127) / 128, 64})));
   pl.launchable = rows < (int64_t{1} << 24);  // (a grid dimension holds fewer than 2^32 threads)
   if (pl.launchable) place_states(pl, sh);
