@@ -119,9 +119,10 @@ static bool plan_few_rows(Attn8Plan& pl, const lra_shape* sh, const lra_cache8* 
 }
 
 // A workgroup of attn8_tiles_kernel takes 128 rows of one sequence.  The key tiles of a q tile are shared where there are fewer q tiles
-// than the chip has places, two per compute unit, and then so that they fill the places once; a share walks two tiles at least.  Twice
-// as many where there are several sequences, whose lengths and chunks may be unlike: 12 chunks of 1 to 256 tokens over 1 k to 8 k tokens
-// take 184 us instead of 206, over 0.5 k to 32 k 474 instead of 657; one of 256 over 8 k takes 63 us, and 80 with twice as many.
+// than the chip has places, two per compute unit, and then so that they fill the places once; a share walks two tiles at least.  Those of
+// several sequences are shared out by their lengths, on the device (attn8_tiles_per_share), into some three and a half to a unit: 12 chunks of 1 to 256
+// tokens over 1 k to 8 k tokens take 179 us, 184 in twice as many equal shares for each q tile as fill the places and 206 in as many; over 0.5 k to
+// 32 k 405, 474 and 657; 4 of 256 over 16 k 171 and 189.  In 2.7, 4.7 and 7 to a unit the first take 194, 193 and 197.
 static bool plan_tiles(Attn8Plan& pl, const lra_shape* sh, const lra_cache8* c, const lra_batch* b) {
   const int64_t G = sh->n_q_heads / sh->n_kv_heads;
   const int64_t places = b->n_queries * G / 128 + c->n_seqs;
@@ -133,6 +134,10 @@ static bool plan_tiles(Attn8Plan& pl, const lra_shape* sh, const lra_cache8* c, 
   pl.tiles = true;
   pl.tile_places = static_cast<int>(places);
   pl.n_splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({places_per_cu * kCUs / (q_tiles * sh->n_kv_heads), (key_tiles + 1) / 2, 64})));
+  if (pl.n_splits > 1 && c->n_seqs > 1 && c->n_seqs <= kShareSeqs) {
+    pl.head_shares = std::max(1, 7 * kCUs / 2 / sh->n_kv_heads);
+    pl.n_splits = static_cast<int>(std::min<int64_t>({2 * pl.n_splits, (key_tiles + 1) / 2, 64}));
+  }
   // states also where the rows of a tile have adapters of their own (the merge kernel applies B_V row by row), and at d = 128 and ranks
   // above 32 (with the product by B_V behind its loop the kernel goes to scratch memory)
   if (pl.n_splits > 1 || !b->causal || (sh->head_dim == 128 && sh->rank > 32)) place_states(pl, sh);

@@ -17,6 +17,20 @@
 
 namespace lra {
 
+// Key tiles of a share, where the q tiles of several sequences (kShareSeqs at most) are shared out by their lengths: about head_shares
+// shares of a kv head in all.
+__device__ __forceinline__ int attn8_tiles_per_share(const Batch8Params& p, int lane) {
+  float steps = 0.f;
+#pragma unroll
+  for (int i = 0; i < kShareSeqs / 64; ++i) {
+    const Attn8Sequence s = attn8_sequence(p, min(64 * i + lane, p.n_seqs - 1));
+    const int q_tiles = ((s.c1 - s.c0) * p.group + 127) >> 7;
+    steps += 64 * i + lane < p.n_seqs ? static_cast<float>(s.n_tiles) * static_cast<float>(q_tiles) : 0.f;
+  }
+  steps = wave_sum(steps);
+  return __builtin_amdgcn_readfirstlane(max(2, static_cast<int>(ceilf(steps / static_cast<float>(p.head_shares)))));
+}
+
 // A thread's codes and low-rank elements of one tile.
 template <int D, int RP>
 struct Attn8Pieces {
@@ -234,8 +248,13 @@ __global__ __launch_bounds__(256, 2) void attn8_tiles_kernel(Batch8Params p) {
   const int n_tiles = wg_last < 0 ? 0 : wg_last / BN + 1 - gap_tiles;
   // this workgroup's share of the q tile's key tiles: [tile_begin, tile_end)
   const int split = SPLIT ? blockIdx.y : 0;
-  const int tile_begin = SPLIT ? static_cast<int>(static_cast<int64_t>(n_tiles) * split / p.n_splits) : 0;
-  const int tile_end = SPLIT ? static_cast<int>(static_cast<int64_t>(n_tiles) * (split + 1) / p.n_splits) : n_tiles;
+  int shares = p.n_splits;
+  if (SPLIT && p.head_shares > 0) {
+    const int per = max(attn8_tiles_per_share(p, lane), (n_tiles + p.n_splits - 1) / p.n_splits);
+    shares = __builtin_amdgcn_readfirstlane(max(1, (n_tiles + per - 1) / per));
+  }
+  const int tile_begin = SPLIT ? (split < shares ? static_cast<int>(static_cast<int64_t>(n_tiles) * split / shares) : n_tiles) : 0;
+  const int tile_end = SPLIT ? (split < shares ? static_cast<int>(static_cast<int64_t>(n_tiles) * (split + 1) / shares) : n_tiles) : n_tiles;
   if constexpr (!SPLIT) {
     if (n_tiles == 0) {  // nothing is seen: zeros
       const int out_row = global_row(false);
