@@ -233,6 +233,30 @@ def test_graph_replays_with_other_lengths_and_inputs():
         assert bool(torch.isfinite(out).all())
 
 
+@pytest.mark.parametrize("counts", [[2, 1, 2], [70, 1, 20]])
+def test_graph_replays_where_shares_go_by_length(counts):
+    """A bound far above the lengths; the shares of a replay are those of its own lengths, an eager call's the same."""
+    c = Case8([5000, 900, 70], counts, causal=len(set(counts)) == 3, heads=(8, 2, 128), rank=16, poison=False)
+    dev = Device8(make8(c), lra, max_seq_len=150000)
+    ws, out = dev.workspace(), torch.empty_like(dev.q)
+    dev.call(out, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        dev.call(out, ws)
+    for lens in ([5000, 900, 70], [70, 900, 70], [0, 0, 1], [4097, 0, 64], [1, 1, 1], [5000, 900, 70]):
+        dev.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        dev.q.add_(0.125)
+        out.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = torch.empty_like(out)
+        dev.call(want, dev.workspace())
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), lens
+        assert bool(torch.isfinite(out).all())
+
+
 def test_two_calls_at_once_on_two_streams():
     a, b = (Device8(make8(Case8([900, 300], [4, 4], heads=(8, 2, 128), rank=16, seed=s)), lra) for s in (1, 2))
     alone = [a.attend(), b.attend()]
