@@ -306,3 +306,49 @@ def test_append_in_a_graph():
         torch.cuda.synchronize()
         twin.append([1 + step, 31 + step], [1, 1], k, v, l)
         assert all(torch.equal(a, b) for a, b in zip(pool.bytes(), twin.bytes())), step
+
+
+def test_gather_in_a_graph():
+    """Other kept rows, lengths and cache contents between the replays."""
+    pool = Pool([120, 60], 2, 128, 16, "e4m3", BF16, seed=5)
+    _, gpu = rows_of(3, 180, 2, 128, 16, BF16)
+    pool.append([120, 60], [120, 60], *gpu)
+    dst, twin = ([torch.zeros(8, 2, BLOCK, 128, dtype=BF16, device="cuda") for _ in range(2)] + [torch.zeros(8, BLOCK, 16, dtype=BF16, device="cuda")] for _ in range(2))
+    table = torch.arange(8, dtype=torch.int32, device="cuda").view(2, 4).contiguous()
+    lens = torch.tensor([64, 10], dtype=torch.int32, device="cuda")
+    kept = torch.arange(64, dtype=torch.int32, device="cuda").repeat(2, 1).contiguous()
+    caches = [lra.make_cache(*z, lens, 64, table) for z in (dst, twin)]
+    lra.lra_cache8_gather(pool.shape, pool.cache, caches[0], kept)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    cache = pool.cache
+    with torch.cuda.graph(graph):
+        lra.lra_cache8_gather(pool.shape, cache, caches[0], kept)
+    for step, m in enumerate(([64, 10], [1, 60], [0, 0], [33, 17])):
+        lens.copy_(torch.tensor(m, dtype=torch.int32))
+        kept.copy_((kept * 7 + step) % 60)
+        pool.k_scale.add_(1)
+        for z in dst + twin:
+            z.fill_(step)
+        graph.replay()
+        lra.lra_cache8_gather(pool.shape, pool.cache, caches[1], kept)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(dst, twin)), step
+
+
+def test_appends_and_gathers_on_two_streams():
+    pools = [Pool([90, 40], 2, 64, 8, "int8", BF16, seed=s) for s in (1, 2, 1, 2)]
+    rows = [rows_of(s, 130, 2, 64, 8, BF16)[1] for s in (1, 2)]
+    for pool, (k, v, l) in zip(pools[2:], rows):
+        pool.append([90, 40], [90, 40], k, v, l)
+    start = torch.tensor([0, 90, 130], dtype=torch.int32, device="cuda")
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for pool in pools[:2]:
+        pool.lens.copy_(torch.tensor([90, 40], dtype=torch.int32))
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for pool, (k, v, l), stream in zip(pools, rows, streams):
+            lra.lra_cache8_append(pool.shape, pool.cache, start, 90, k, v, l, THETA, stream=stream)
+    torch.cuda.synchronize()
+    for pool, twin in zip(pools[:2], pools[2:]):
+        assert all(torch.equal(a, b) for a, b in zip(pool.bytes(), twin.bytes()))
