@@ -136,7 +136,7 @@ static bool plan_tiles(Attn8Plan& pl, const lra_shape* sh, const lra_cache8* c, 
   pl.n_splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({places_per_cu * kCUs / (q_tiles * sh->n_kv_heads), (key_tiles + 1) / 2, 64})));
   if (pl.n_splits > 1 && c->n_seqs > 1 && c->n_seqs <= kShareSeqs) {
     pl.head_shares = std::max(1, 7 * kCUs / 2 / sh->n_kv_heads);
-    pl.n_splits = static_cast<int>(std::min<int64_t>({2 * pl.n_splits, (key_tiles + 1) / 2, 64}));
+    pl.n_splits = static_cast<int>(std::min<int64_t>({(3 * pl.n_splits + 1) / 2, (key_tiles + 1) / 2, 64}));
   }
   // states also where the rows of a tile have adapters of their own (the merge kernel applies B_V row by row), and at d = 128 and ranks
   // above 32 (with the product by B_V behind its loop the kernel goes to scratch memory)
