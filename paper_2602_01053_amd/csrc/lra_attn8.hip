@@ -263,6 +263,7 @@ lra_status lra_attn_batch8(const lra_shape* shape, const lra_cache8* cache, cons
   } else if (pl.tiles) {
     p.row_mul = (65535 + p.group) / p.group;
     p.tile_places = pl.tile_places;
+    p.longest_first = pl.longest_first;
     if ((p.code == LRA_E4M3 ? launch_attn8_tiles_e4m3 : launch_attn8_tiles_int8)(p, s) != hipSuccess) return LRA_ERR_HIP;
   } else if (launch_attn8_vector(p, bf16, pl.rows, s) != hipSuccess) {
     return LRA_ERR_HIP;

@@ -15,7 +15,7 @@ constexpr int kShareSeqs = 128;
 
 struct Attn8Plan {
   bool launchable;
-  bool few_rows, tiles, states;
+  bool few_rows, tiles, states, longest_first;
   int rows, n_splits, row_tiles, tile_places;
   int head_shares, share_least;  // few rows: shares of a kv head over all sequences (0: n_splits of each), tiles of the shortest
   size_t off_ml, off_o, off_lr, off_adapter, bytes;

@@ -17,6 +17,69 @@
 
 namespace lra {
 
+// Workgroup `at` -> q tile, those that see the most tokens first (in classes of 256 of them), so that none of those begins when the others are
+// done: 32 chunks of unlike contexts take a fifth less.  Every workgroup finds its tile by itself: a class by bisection over the number of tiles from a class on, which
+// for a sequence's tiles, each seeing more than the one before, is a quotient; then the sequence by a running sum over its class.
+__device__ __forceinline__ bool attn8_longest_first(const Batch8Params& p, int at, int lane, BatchTiles& item) {
+  constexpr int N = kShareSeqs / 64;
+  int tiles[N], first_pos[N], new_tokens[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const Attn8Sequence s = attn8_sequence(p, min(64 * i + lane, p.n_seqs - 1));
+    new_tokens[i] = 64 * i + lane < p.n_seqs ? s.c1 - s.c0 : 0;  // (none, and no tiles of any class, behind the last)
+    tiles[i] = (new_tokens[i] * p.group + 127) >> 7;
+    first_pos[i] = s.first_pos;
+  }
+  // the first of sequence i's tiles of class `cls` and above
+  auto first_of = [&](int i, int cls) __attribute__((always_inline)) -> int {
+    if (cls <= 0) return 0;
+    if (p.window > 0 && cls * 256 > p.window + p.sinks) return tiles[i];  // (that many tokens nobody sees)
+    const int x = cls * 256 - 1 - first_pos[i];
+    return x <= 0 ? 0 : (!p.causal || x >= new_tokens[i] ? tiles[i] : (x * p.group) >> 7);
+  };
+  auto count = [&](int cls) __attribute__((always_inline)) -> int {
+    int c = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) c += tiles[i] - first_of(i, cls);
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) c += __shfl_xor(c, off, kWave);
+    return __builtin_amdgcn_readfirstlane(c);
+  };
+  if (at >= count(0)) return false;
+  int cls = 0, beyond = (p.max_seq_len >> 8) + 1;  // count(cls) > at >= count(beyond) = 0
+  while (beyond - cls > 1) {
+    const int mid = (cls + beyond) >> 1;
+    if (count(mid) > at) cls = mid;
+    else beyond = mid;
+  }
+  at -= count(cls + 1);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int end = first_of(i, cls + 1), mine = end - first_of(i, cls);
+    int upto = mine;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int below = __shfl_up(upto, off, kWave);
+      upto += lane >= off ? below : 0;
+    }
+    const uint64_t there = __builtin_amdgcn_ballot_w64(at < upto);
+    if (there != 0) {
+      const int k = __builtin_ctzll(there);
+      item.t = 64 * i + k;
+      item.tile = __builtin_amdgcn_readlane(end, k) - 1 - (at - (__builtin_amdgcn_readlane(upto, k) - __builtin_amdgcn_readlane(mine, k)));
+      const Attn8Sequence s = attn8_sequence(p, item.t);
+      item.n_t = __builtin_amdgcn_readfirstlane(s.n_t);
+      item.first_query = __builtin_amdgcn_readfirstlane(s.c0);
+      item.n_queries = __builtin_amdgcn_readfirstlane(s.c1 - s.c0);
+      item.first_pos = __builtin_amdgcn_readfirstlane(s.first_pos);
+      item.adapter = __builtin_amdgcn_readfirstlane(min(max(p.query_adapter[s.c0], 0), p.n_adapters - 1));
+      return true;
+    }
+    at -= __builtin_amdgcn_readlane(upto, 63);
+  }
+  return false;
+}
+
 // Key tiles of a share, where the q tiles of several sequences (kShareSeqs at most) are shared out by their lengths: about head_shares
 // shares of a kv head in all.
 __device__ __forceinline__ int attn8_tiles_per_share(const Batch8Params& p, int lane) {
@@ -187,8 +250,13 @@ __global__ __launch_bounds__(256, 2) void attn8_tiles_kernel(Batch8Params p) {
   const int lin = blockIdx.x;
   const int rest = lin / Hkv, hk = lin - rest * Hkv;
   const int head_first = hk * G;
-  // (the last tiles of a chunk see the most keys: they go first)
-  const BatchTiles item = batch_tiles(p, static_cast<int>(gridDim.x) / Hkv - 1 - rest, lane);
+  // (the last tiles of a chunk see the most keys: they go first, of several chunks the longest of all)
+  BatchTiles item;
+  if (p.longest_first) {
+    if (!attn8_longest_first(p, rest, lane, item)) return;
+  } else {
+    item = batch_tiles(p, static_cast<int>(gridDim.x) / Hkv - 1 - rest, lane);
+  }
   const int n_rows = item.n_queries * G;           // query rows of these heads: (new token, q head), the q head fastest
   const int t = item.t, a_idx = item.adapter, n_t = item.n_t;
   if (static_cast<int64_t>(item.tile) * BM >= n_rows) return;

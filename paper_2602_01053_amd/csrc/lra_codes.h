@@ -12,6 +12,7 @@ struct Batch8Params : BatchParams {
   const uint8_t *k_scale, *v_scale;
   int64_t scale_block_stride;
   int32_t code;
+  int32_t longest_first;            // tiles kernel: q tiles in the order of what they see
   int32_t head_shares, share_least;  // rows kernels: key shares of a kv head (0: n_splits of every sequence), tiles of the shortest
 };
 

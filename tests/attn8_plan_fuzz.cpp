@@ -32,7 +32,7 @@ int main(int argc, char** argv) {
   const int cases = argc > 1 ? std::atoi(argv[1]) : 200000;
   alignas(16) static char dummy[64];
   const int32_t* ints = reinterpret_cast<const int32_t*>(dummy);
-  int accepted = 0, few[5] = {}, tiles = 0, whole = 0, vector = 0, refused = 0, rows_taken = 0, by_length = 0;
+  int accepted = 0, few[5] = {}, tiles = 0, whole = 0, vector = 0, refused = 0, rows_taken = 0, by_length = 0, ordered = 0, shared = 0;
   for (int it = 0; it < cases; ++it) {
     lra_shape sh{};
     sh.n_kv_heads = static_cast<int32_t>(pick({1, 2, 4, 8, 3, 256}));
@@ -103,6 +103,10 @@ int main(int argc, char** argv) {
       }
     } else if (pl.tiles) {
       ++tiles;
+      CHECK(pl.head_shares == 0 || (pl.n_splits > 1 && c.n_seqs > 1 && c.n_seqs <= kShareSeqs));
+      CHECK(!pl.longest_first || (pl.n_splits == 1 && c.n_seqs > 1 && c.n_seqs <= kShareSeqs));
+      ordered += pl.longest_first;
+      shared += pl.head_shares > 0;
       CHECK(mfma && pl.tile_places >= (b.n_queries * group + 127) / 128 && pl.tile_places >= c.n_seqs);
       CHECK(static_cast<int64_t>(pl.tile_places) * sh.n_kv_heads * 256 < (int64_t{1} << 32));
     } else {
@@ -110,9 +114,9 @@ int main(int argc, char** argv) {
       CHECK(pl.states && rows * 256 < (int64_t{1} << 32));
     }
   }
-  if (!few[1] || !few[2] || !few[4] || !tiles || !whole || !vector || !refused || !rows_taken || !by_length) {
-    std::fprintf(stderr, "attn8_plan_fuzz: a kind of plan never came up (%d %d %d %d %d %d %d %d %d)\n", few[1], few[2], few[4], tiles, whole, vector,
-                 refused, rows_taken, by_length);
+  if (!few[1] || !few[2] || !few[4] || !tiles || !whole || !vector || !refused || !rows_taken || !by_length || !ordered || !shared) {
+    std::fprintf(stderr, "attn8_plan_fuzz: a kind of plan never came up (%d %d %d %d %d %d %d %d %d %d %d)\n", few[1], few[2], few[4], tiles, whole, vector,
+                 refused, rows_taken, by_length, ordered, shared);
     return 1;
   }
   std::printf("%d accepted, all plans consistent\n", accepted);

@@ -100,6 +100,32 @@ def test_sequences_of_unlike_lengths(code, heads, rank, causal, window):
         assert torch.equal(got, dev.attend())
 
 
+@pytest.mark.parametrize("heads,code", [((4, 1, 64), "e4m3"), ((7, 1, 64), "int8"), ((2, 2, 128), "e4m3")])
+@pytest.mark.parametrize("window", [0, 300])
+def test_chunks_of_many_tiles(heads, code, window):
+    """Several q tiles in every class of lengths, the longest sequence first, last and between; more tokens than their sequence has."""
+    for lens, counts in (([700, 1500, 40, 600], [300, 1200, 40, 3]), ([1500, 40, 0, 700], [1100, 90, 2, 700]), ([257, 1300], [257, 900]), ([1300, 1024], [1000, 1024]),
+                         ([700, 1500, 40, 600, 0, 257, 900, 130, 1], [300, 800, 40, 3, 2, 257, 130, 1, 1]),
+                         ([64] * 7 + [1400, 3], [64, 0, 1, 2, 50, 64, 3, 1200, 3])):
+        c = Case8(lens, counts, causal=True, window=window, sinks=5, heads=heads, rank=8, code=code, seed=len(lens))
+        x = make8(c)
+        want, bound = attention_with_bound(x)
+        close_enough(Device8(x, lra).attend(), want, bound, c.label())
+        close_enough(Device8(x, lra, max_seq_len=4096).attend(), want, bound, c.label())
+
+
+@pytest.mark.parametrize("window,causal", [(0, True), (700, True), (0, False)])
+def test_chunks_in_the_order_of_what_they_see(window, causal):
+    """So many kv heads that nothing is shared out: the q tiles of eight sequences and more, longest first."""
+    for code, lens, counts in (("e4m3", [300, 800, 40, 257, 0, 130, 560, 1, 20], [10, 200, 40, 3, 2, 129, 130, 1, 20]),
+                               ("int8", [64] * 7 + [800, 3], [64, 0, 1, 2, 5, 6, 3, 260, 3])):
+        c = Case8(lens, counts, causal=causal, window=window, sinks=5, heads=(64, 64, 64), rank=8, code=code, seed=len(lens))
+        x = make8(c)
+        want, bound = attention_with_bound(x)
+        close_enough(Device8(x, lra).attend(), want, bound, c.label())
+        close_enough(Device8(x, lra, max_seq_len=9000).attend(), want, bound, c.label())
+
+
 def test_shares_of_more_than_64_sequences():
     for n in (65, 128, 129):
         c = Case8([700 * (t % 7) + t for t in range(n)], [1 + t % 2 for t in range(n)], heads=(4, 1, 64), rank=8, code="int8", seed=n)
