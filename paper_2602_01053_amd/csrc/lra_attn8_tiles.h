@@ -91,7 +91,7 @@ __device__ __forceinline__ int attn8_tiles_per_share(const Batch8Params& p, int 
     steps += 64 * i + lane < p.n_seqs ? static_cast<float>(s.n_tiles) * static_cast<float>(q_tiles) : 0.f;
   }
   steps = wave_sum(steps);
-  return __builtin_amdgcn_readfirstlane(max(2, static_cast<int>(ceilf(steps / static_cast<float>(p.head_shares)))));
+  return __builtin_amdgcn_readfirstlane(max(2, static_cast<int>(fminf(ceilf(steps / static_cast<float>(p.head_shares)), 1e9f))));
 }
 
 // A thread's codes and low-rank elements of one tile.
