@@ -9,7 +9,7 @@
 //      that eight lanes holding the chunks of one row do not meet in a bank;
 //   V: the cache holds sixteen tokens of a dimension together, which are two lanes' operands of O^T += V^T P^T: tokens 0-3 and 8-11,
 //      4-7 and 12-15, as the score registers have them.  No transposed reads (batch_tiles_kernel takes two per operand).
-// Bound by what a step of 64 keys issues: chunks of 2048 and 1376 tokens over 18 k and 13 k take 1083 us, 0.90 PFLOP/s (matrix cores busy
+// Bound by what a step of 64 keys issues: chunks of 2048 and 1376 tokens over 18 k and 13 k take 1055 us, 0.93 PFLOP/s (matrix cores busy
 // 41 %, vector units and LDS 38 % each; two workgroups to a compute unit); the same call on 16-bit rows takes 1016, without the conversion.
 #pragma once
 
@@ -498,8 +498,9 @@ __global__ __launch_bounds__(256, 2) void attn8_tiles_kernel(Batch8Params p) {
 
     // S^T for the two 32-key halves of the tile.  The halves alternate, so consecutive
     // matrix instructions never wait for each other's result, and the LDS reads run
-    // kReadAheadS operands ahead of the products that consume them.  The wave goes ahead of the SIMD's other one meanwhile:
-    // chunks of 2048 and 1376 tokens over 18 k and 13 k take 1083 us instead of 1111 (over V's products as well 1090).
+    // kReadAheadS operands ahead of the products that consume them.  The wave goes ahead of the SIMD's other one meanwhile
+    // and, before all, while it converts the next tile, which three other waves wait for; softmax and V's products are what goes on beside:
+    // chunks of 2048 and 1376 tokens over 18 k and 13 k take 1055 us, 1105 without, 1090 with the scores alone or V's products too.
     __builtin_amdgcn_s_setprio(1);
     pf_f32x16 s[2];
 #pragma unroll
@@ -664,6 +665,7 @@ __global__ __launch_bounds__(256, 2) void attn8_tiles_kernel(Batch8Params p) {
         __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
       }
     }
+    __builtin_amdgcn_s_setprio(2);
     if (more) {
       if (!K_EARLY) loader.convert_kl((ST ^ 1) * STAGE, raw);
       loader.convert_v(j_next, (ST ^ 1) * STAGE, raw);
