@@ -321,6 +321,9 @@ __global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
     const bool more = tile + NS < t1;
     const bool all = whole(j);
     // S^T: element (i, e) of this lane is token 4i + e of block g
+    // (from here to the next tile's requests the wave goes ahead of the SIMD's other one: 14 rows over 16 sequences take 141 us
+    // instead of 143)
+    __builtin_amdgcn_s_setprio(1);
     f32x4 s[4];
     {
       const float ks_mine = scale8(ks_raw), ks_row = __shfl(ks_mine, my_block * 16, kWave);
@@ -342,6 +345,7 @@ __global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
       id_next = look_up(key_of(min(tile + 2 * NS, t1 - 1)));
     }
     __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(0);
     // L: rows that nobody sees are zeros
     if (!all) {
 #pragma unroll

@@ -204,6 +204,9 @@ __global__ __launch_bounds__(256, attn8_rows32_waves(RP)) void attn8_rows32_kern
     const bool more = tile + NS < t1;
     const bool all = whole(j);
     // S^T: register i of tile kt is token i of block 2 kt + g2
+    // (from here to the next tile's requests the wave goes ahead of the SIMD's other one: 28 rows over 16 sequences 156 us instead of 159, integers 166
+    // instead of 172)
+    __builtin_amdgcn_s_setprio(1);
     pf_f32x16 s[2];
     {
       float ks_row[2], ks_mine[2];
@@ -235,6 +238,7 @@ __global__ __launch_bounds__(256, attn8_rows32_waves(RP)) void attn8_rows32_kern
       id_next = look_up(key_of(min(tile + 2 * NS, t1 - 1)));
     }
     __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(0);
     // L: rows that nobody sees are zeros
     if (!all) {
 #pragma unroll
