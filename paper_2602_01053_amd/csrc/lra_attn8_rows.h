@@ -15,7 +15,7 @@
 // the scales instead, exactly): the codes of a tile cost a wave some 500 cycles, the 16 KB that they stand for 2000 of the memory's.
 // K of a wave's next tile is requested as soon as its scores are taken, V and L as soon as the products are: with eight waves to a
 // compute unit some hundred KB are on their way.
-// Bound by HBM where the shares are long: 14 rows over 16 sequences of 4 k to 64 k tokens 144 us with the merge, 5.4 TB/s of the bytes
+// Bound by HBM where the shares are long: 14 rows over 16 sequences of 4 k to 64 k tokens 141 us with the merge, 5.5 TB/s of the bytes
 // needed (a large copy reaches 5.2, both directions counted); 16 rows over 32 k tokens of 8 kv heads 17.5 us (68 MB), of which the start, two dependent round trips and Q B_K^T, is 5.
 #pragma once
 

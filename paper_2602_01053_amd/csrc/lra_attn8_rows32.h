@@ -1,6 +1,6 @@
 // Attention over 8-bit codes for sequences with 17 to 64 query rows per kv head: attn8_rows_kernel with 32 rows to a wave
 // (v_mfma_f32_32x32x16_bf16).  Waves of 16 rows each read every key once per row tile: 16 sequences of 4 k to 64 k tokens with 28 rows took
-// 244 us so (e4m3; integers 258) and take 156 (168), 5.0 TB/s of the bytes needed; 64 rows over 32 k tokens take 40 us, as much by their
+// 244 us so (e4m3; integers 258) and take 152 to 156 (165), 5.0 TB/s of the bytes needed; 64 rows over 32 k tokens take 38 us, as much by their
 // states and products as by the reading.
 //
 // Operands straight from the cache, as there: row rho of key tile t (of two) is token 8 (rho / 16) + 4 (rho / 8 % 2) + rho % 4 of block
