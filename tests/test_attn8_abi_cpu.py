@@ -215,3 +215,31 @@ def test_binding_refuses_mismatched_calls():
                 (codes, s, w, s, torch.zeros(3, 7))):
         with pytest.raises(lra.LraError):
             lra.lra_matmul_i8(*bad)
+
+
+def test_header_is_c_and_the_structs_are_the_bindings(tmp_path):
+    """lra_attn8.h in a C program: sizes and the last fields' places of its structs."""
+    import os
+    import shutil
+    import subprocess
+
+    gcc = shutil.which("gcc")
+    if gcc is None:
+        pytest.skip("no host C compiler")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    source, exe = tmp_path / "sizes.c", tmp_path / "sizes"
+    source.write_text('''#include <stddef.h>
+#include <stdio.h>
+#include "lra_attn8.h"
+int main(void) {
+  printf("%zu %zu %zu %zu %zu %zu\\n", sizeof(lra_cache8), offsetof(lra_cache8, max_seq_len), sizeof(lra_new_rows), offsetof(lra_new_rows, rope_theta),
+         sizeof(lra_i8_operands), offsetof(lra_i8_operands, k));
+  return 0;
+}
+''')
+    build = subprocess.run([gcc, "-std=c99", "-Wall", "-Wextra", "-Werror", "-pedantic", "-I", os.path.join(root, "include"), str(source), "-o", str(exe)],
+                           capture_output=True, text=True)
+    assert build.returncode == 0, build.stderr
+    got = [int(v) for v in subprocess.run([str(exe)], capture_output=True, text=True, check=True, env=dict(os.environ, LD_PRELOAD="")).stdout.split()]
+    assert got == [ctypes.sizeof(LraCache8), LraCache8.max_seq_len.offset, ctypes.sizeof(LraNewRows), LraNewRows.rope_theta.offset,
+                   ctypes.sizeof(LraI8Operands), LraI8Operands.k.offset]
