@@ -110,7 +110,7 @@ __global__ __launch_bounds__(256) void attn8_vector_kernel(Batch8Params p) {
     m = m_new;
     ell = ell * alpha + pj;  // (of this lane's tokens)
     p_s[piece][lane] = pj;  // (by lanes' exchange instead, sixteen at a time, 200 rows over 2 k tokens took 733 us instead of 565)
-    __builtin_amdgcn_wave_barrier();
+    wave_fence();
     o *= alpha;
     olr *= alpha;
 #pragma unroll

@@ -37,6 +37,13 @@ __device__ __forceinline__ int least_scale8(uint32_t bits) {
   return max(e, 1);
 }
 
+// What a wave's lanes have written to LDS, its other lanes read behind this (in order anyhow: for the compiler).
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // Codes that the launch reads once, past the caches' replacement: 64 k tokens of 8 kv heads take 31 us so instead of 36 (14 rows over a
 // batch of 780 MB 4 % less); what the memory-side cache still holds comes a little later, 32 k tokens in 21.8 instead of 20.8 us.
 __device__ __forceinline__ uint4 load_once(const uint8_t* src) {

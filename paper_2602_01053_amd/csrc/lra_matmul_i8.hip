@@ -1,5 +1,6 @@
 // Products of 8-bit integers with a scale per token and feature, and the quantization of their operands (contracts in lra_attn8.h).
 #include "lra_attn8.h"
+#include "lra_codes.h"
 #include "lra_common.h"
 #include "lra_prefill_util.h"
 
@@ -200,6 +201,7 @@ __device__ __forceinline__ void store_by_rows(const I8Params& p, unsigned char* 
         *reinterpret_cast<uint2*>(mine + place(tok, 4 * a + q) + 8 * g2) = make_uint2(pf_pack2(v[0], v[1]), pf_pack2(v[2], v[3]));
       }
   }
+  wave_fence();
   const int c = lane % CH, f = feat0 + 8 * c;
 #pragma unroll
   for (int i = 0; i < 32 * B * CH / 64; ++i) {
