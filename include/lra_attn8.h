@@ -120,7 +120,8 @@ size_t lra_batch8_workspace_bytes(const lra_shape* shape, const lra_cache8* cach
 /*
  * Rows as 8-bit integers with a scale each: scales[i] = max_j |x[i][j]| / 127, codes[i][j] = x[i][j] * (127 / max) rounded to
  * nearest, ties to even, in fp32.  A row of zeros has scale 0 and codes 0; a row that is not finite gets the scale NaN, which
- * makes its row of a product NaN.  For activations (a row is a token) and for weights alike (a row is a feature).
+ * makes its row of a product NaN.  (Of rows whose largest value is below 127 * 2^-126, 1.5e-36, the scale is a denormal number: right to
+ * 2^-150, and so with fewer bits.)  For activations (a row is a token) and for weights alike (a row is a feature).
  *   x      DEVICE [rows][cols] of dtype (lra_dtype), rows x_stride elements apart; x and the stride multiples of 16 bytes
  *   codes  DEVICE int8 [rows][cols], rows codes_stride bytes apart; both multiples of 16 bytes
  *   scales DEVICE float [rows]

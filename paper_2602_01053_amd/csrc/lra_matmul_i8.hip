@@ -74,8 +74,10 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantParams p) {
   most = max(max(most_s[0], most_s[1]), max(most_s[2], most_s[3]));
   const float top = __uint_as_float(most);
   const bool finite = most < 0x7f800000u;
-  // (a row below 2^-119 or so: 127 / max is beyond fp32, and the largest finite factor leaves its codes smaller than they could be)
-  const float inv = most == 0 || !finite ? 0.f : fminf(127.f / top, 3.402823466e38f);
+  // (for a largest value below 127 / (2^128 - 2^104), 3.7e-37, the factor 127 / max is beyond fp32: rows below 2^-100 are taken 2^64 times as
+  // large, which rounds nothing)
+  const float up = top < 0x1p-100f ? 0x1p64f : 1.f;
+  const float inv = most == 0 || !finite ? 0.f : 127.f / (top * up);
   if (tid == 0) p.scales[row] = finite ? top / 127.f : __uint_as_float(0x7fc00000u);
   int8_t* dst = p.codes + row * p.codes_stride;
   auto store = [&](const Sixteen<T>& v, int c) __attribute__((always_inline)) {
@@ -86,7 +88,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantParams p) {
     for (int i = 0; i < 4; ++i) {
       w[i] = 0;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) w[i] |= (finite ? static_cast<uint32_t>(static_cast<int>(rintf(x[4 * i + e] * inv))) & 255u : 0u) << (8 * e);
+      for (int e = 0; e < 4; ++e) w[i] |= (finite ? static_cast<uint32_t>(static_cast<int>(rintf(x[4 * i + e] * up * inv))) & 255u : 0u) << (8 * e);
     }
     *reinterpret_cast<uint4*>(dst + c) = make_uint4(w[0], w[1], w[2], w[3]);
   };

@@ -129,3 +129,30 @@ def test_matmul_i8_in_a_graph_and_on_two_streams():
         lra.lra_matmul_i8(x, sx, w, sw, y2, ws2, stream=b)
     torch.cuda.synchronize()
     assert torch.equal(y, first) and torch.equal(y2, first)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("cols", [64, 4096, 20000])
+def test_quantize_rows_of_the_smallest_values(dtype, cols):
+    """Largest values about 127 / the largest fp32 number (3.7e-37), below which 127 / max is beyond fp32, down to denormal ones."""
+    tops = [1e-30, 1e-35, 1e-36, 3.8e-37, 3.7e-37, 3.6e-37, 1e-37, 2e-38, 1.2e-38, 1e-39, 1e-40] + ([1e-42, 3e-44] if dtype == F32 else [])
+    g = torch.Generator().manual_seed(cols)
+    x = torch.rand(len(tops), cols, generator=g, dtype=torch.float64) * 2 - 1
+    x[:, cols // 3] = 1
+    x = (x * torch.tensor(tops, dtype=torch.float64)[:, None]).to(dtype)
+    codes, scales = torch.full((len(tops), cols), 77, dtype=torch.int8, device="cuda"), torch.empty(len(tops), device="cuda")
+    lra.lra_quantize_rows(x.cuda(), codes, scales)
+    torch.cuda.synchronize()
+    got, s = codes.cpu().double(), scales.cpu().double()
+    top = x.double().abs().amax(1)
+    # a division's rounding: half a step of fp32, of its denormal numbers half of 2^-149
+    assert bool(((s - top / 127).abs() <= 2.0 ** -24 * top / 127 + 2.0 ** -150).all())
+    # as for larger values: a quotient and a product rounded in fp32, 2^-23 of at most 127, before the code's own half step
+    assert bool(((got - x.double() * 127 / top[:, None]).abs() <= 0.5 + 127 * 2.0 ** -23).all())
+    assert bool((got.abs().amax(1) == 127).all())
+    if cols == 64:
+        y = torch.empty(len(tops), 64, device="cuda")
+        lra.lra_matmul_i8(codes, scales, torch.eye(64, dtype=torch.int8, device="cuda"), torch.ones(64, device="cuda"), y)
+        torch.cuda.synchronize()
+        # two products in fp32
+        assert bool(((y.cpu().double() - got * s[:, None]).abs() <= (got * s[:, None]).abs() * 2.0 ** -23 + 2.0 ** -149).all())
