@@ -106,7 +106,8 @@ __global__ __launch_bounds__(256) void attn8_vector_kernel(Batch8Params p) {
     const float top = wave_max(s);
     const float m_new = fmaxf(m, top < -7e8f ? -INFINITY : top);
     const float alpha = m == -INFINITY ? 0.f : expf(m - m_new);
-    const float pj = s == -INFINITY || m_new == -INFINITY ? 0.f : expf(s - m_new);
+    // (no weight where the score is minus infinity, nor where no number is above -7e8 so far; a score of NaN makes the sum one)
+    const float pj = s == -INFINITY || (m_new == -INFINITY && s == s) ? 0.f : expf(s - m_new);
     m = m_new;
     ell = ell * alpha + pj;  // (of this lane's tokens)
     p_s[piece][lane] = pj;  // (by lanes' exchange instead, sixteen at a time, 200 rows over 2 k tokens took 733 us instead of 565)

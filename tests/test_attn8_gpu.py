@@ -308,3 +308,30 @@ def test_output_and_workspace_ends_are_respected():
     torch.cuda.synchronize()
     assert torch.equal(out, want)
     assert bool((buf[:256] == -7).all()) and bool((buf[256 + dev.q.numel():] == -7).all()) and bool((ws[n:] == 0xA5).all())
+
+
+KERNELS = [dict(heads=(8, 2, 64), counts=[2]), dict(heads=(14, 2, 128), counts=[2]), dict(heads=(8, 1, 64), counts=[3]), dict(heads=(8, 1, 128), counts=[6]),
+           dict(heads=(2, 2, 64), counts=[90]), dict(heads=(2, 1, 128), counts=[90], causal=True), dict(heads=(2, 2, 64), counts=[3], dtype=F32)]
+# (16 query rows per kv head and fewer, up to 32, up to 64, tiles of 128 with states and without, vector ALU)
+
+
+@pytest.mark.parametrize("kernel", KERNELS + [dict(heads=(4, 2, 64), counts=[2], rank=5), dict(heads=(4, 2, 128), counts=[40], rank=13, causal=True)], ids=str)
+@pytest.mark.parametrize("blocks", [range(0, 4), range(8, 12), range(36, 37), range(18, 20)], ids=str)
+@pytest.mark.parametrize("side", ["k", "v"])
+def test_no_number_in_one_share(kernel, blocks, side):
+    """Blocks of the last kv head whose scale is no number, a whole tile of 64 keys, the tile of a single key, or some of a tile: they reach
+    every row of that head that sees them, whatever the other tiles and shares hold, and no other head."""
+    c = Case8([577], **dict(dict(rank=8), key_side=False, poison=False, **kernel))
+    x = make8(c)
+    want, bound = attention_with_bound(x)
+    dev = Device8(x, lra)
+    scale = dev.k_scale if side == "k" else dev.v_scale
+    for b in blocks:
+        scale[dev.table[0, b].long(), -1] = 255
+    got = dev.attend().cpu()
+    hq, hkv, _ = c.heads
+    g = hq // hkv
+    sees = torch.tensor([(577 - c.counts[0] + i if c.causal else 576) >= 16 * blocks[0] for i in range(c.counts[0])])
+    assert bool(torch.isnan(got[sees][:, hq - g:]).all())
+    if hkv > 1:
+        close_enough(got[:, :hq - g], want[:, :hq - g], bound[:, :hq - g], c.label())
