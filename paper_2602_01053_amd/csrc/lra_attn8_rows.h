@@ -66,6 +66,13 @@ __device__ __forceinline__ uint4 codes_to_values(uint32_t lo, uint32_t hi, float
   }
 }
 
+// Integer codes have their scale in the weights: over 2^(unit - 127), at least the largest scale that the wave has met, which multiplies the
+// accumulators in the end.  So the weights are within [0, 1], and rounded to bf16 as probabilities are, whatever the size of V; from 2^-127 of the unit
+// down a scale counts as zero.  (With the scale itself as factor, weights of blocks below 2^-105 or so were denormal bf16 numbers of few bits.)
+__device__ __forceinline__ float over_unit(int s, int unit) { return __uint_as_float(static_cast<uint32_t>(max(127 + s - unit, 0)) << 23); }
+// The unit for a largest scale byte `most`: some steps above, so that blocks of about the same size seldom raise it (255 stays: no number).
+__device__ __forceinline__ int unit_above(int most) { return most == 255 ? 255 : min(most + 8, 254); }
+
 __device__ __forceinline__ uint4 masked(uint4 v, uint4 m) { return make_uint4(v.x & m.x, v.y & m.y, v.z & m.z, v.w & m.w); }
 
 // Sequence t: its queries, and the tiles of 64 keys that they see: n_tiles in all, those from sink_tiles on `gap` further.
@@ -315,6 +322,7 @@ __global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
 #pragma unroll
   for (int b = 0; b < RB; ++b) lr_acc[b] = zero4;
   float m_run = -INFINITY, l_run = 0.f;
+  int unit = 0;  // integers: what o_acc is counted in, a scale byte
   const float sc = p.scale * 1.44269504088896340736f;
   for (int tile = first; tile < t1; tile += NS) {
     const int j = key_of(tile);
@@ -380,7 +388,6 @@ __global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
     }
     // (the accumulators are rescaled only where some row's maximum grows; the probabilities, at most 1, round to bf16 for the
     // matrix cores, their sum is taken in fp32 before)
-    const float vs_mine = scale8(vs_raw);
     uint32_t wl[8], wv[8];  // weights for L, and for V: with the block's scale, where that is not in V's operand
     {
       float mx = -INFINITY;
@@ -389,17 +396,27 @@ __global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[i][e]);
       mx = tile_reference(max_over_lane_groups(mx) * sc);
-      if (__builtin_amdgcn_ballot_w64(mx > m_run) != 0) {
+      if (__builtin_amdgcn_ballot_w64(mx > m_run || (CODE == LRA_INT8 && vs_raw > unit)) != 0) {
         const float m_new = fmaxf(m_run, mx);
         const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
         m_run = m_new;
         l_run *= alpha;
+        float alpha_o = alpha;
+        if constexpr (CODE == LRA_INT8) {
+          int most = 0;
 #pragma unroll
-        for (int b = 0; b < DB; ++b) o_acc[b] *= alpha;
+          for (int i = 0; i < 4; ++i) most = max(most, __builtin_amdgcn_readlane(vs_raw, 16 * i));
+          const int next = most > unit ? unit_above(most) : unit;
+          alpha_o *= over_unit(unit, next);
+          unit = next;
+        }
+#pragma unroll
+        for (int b = 0; b < DB; ++b) o_acc[b] *= alpha_o;
 #pragma unroll
         for (int b = 0; b < RB; ++b) lr_acc[b] *= alpha;
       }
       const float nm = m_run == -INFINITY ? 0.f : -m_run;
+      const float vs_part = over_unit(vs_raw, unit);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float x[4];
@@ -410,11 +427,12 @@ __global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
         }
         wl[2 * i] = pack_bf16x2(x[0], x[1]), wl[2 * i + 1] = pack_bf16x2(x[2], x[3]);
         // (a power of two: the same rounding as without it)
-        if constexpr (CODE == LRA_INT8) wv[2 * i] = pack_bf16x2(x[0] * vs_mine, x[1] * vs_mine), wv[2 * i + 1] = pack_bf16x2(x[2] * vs_mine, x[3] * vs_mine);
+        if constexpr (CODE == LRA_INT8) wv[2 * i] = pack_bf16x2(x[0] * vs_part, x[1] * vs_part), wv[2 * i + 1] = pack_bf16x2(x[2] * vs_part, x[3] * vs_part);
         else wv[2 * i] = wl[2 * i], wv[2 * i + 1] = wl[2 * i + 1];
       }
     }
     auto half = [](const uint32_t (&w)[8], int hf) __attribute__((always_inline)) { return as_bf16x8(make_uint4(w[4 * hf], w[4 * hf + 1], w[4 * hf + 2], w[4 * hf + 3])); };
+    const float vs_mine = scale8(vs_raw);
     // O^T += V^T P^T: half hf of the sixteen tokens of every block
     if (!all) {  // codes of tokens that nobody sees may be no numbers: zeros
       const uint4 mask = token_masks(j + 16 * g, n_t, sinks, lo);
@@ -456,7 +474,10 @@ __global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
     const float wgt = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_all);
     l_run = m_run == -INFINITY ? l_run : l_run * wgt;  // (a sum of NaN stays one)
 #pragma unroll
-    for (int b = 0; b < DB; ++b) o_acc[b] *= wgt;
+    for (int b = 0; b < DB; ++b) {
+      o_acc[b] *= wgt;
+      if constexpr (CODE == LRA_INT8) o_acc[b] *= scale8(unit);
+    }
 #pragma unroll
     for (int b = 0; b < RB; ++b) lr_acc[b] *= wgt;
 #pragma unroll

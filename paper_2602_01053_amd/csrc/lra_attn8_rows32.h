@@ -198,6 +198,7 @@ __global__ __launch_bounds__(256, attn8_rows32_waves(RP)) void attn8_rows32_kern
 #pragma unroll
     for (int i = 0; i < 16; ++i) lr_acc[b][i] = 0.f;
   float m_run = -INFINITY, l_run = 0.f;
+  int unit = 0;  // integers: what o_acc is counted in, a scale byte
   const float sc = p.scale * 1.44269504088896340736f;
   for (int tile = first; tile < t1; tile += NS) {
     const int j = key_of(tile);
@@ -283,13 +284,22 @@ __global__ __launch_bounds__(256, attn8_rows32_waves(RP)) void attn8_rows32_kern
 #pragma unroll
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[kt][i]);
     mx = tile_reference(fmaxf(mx, pf_partner32(mx)) * sc);
-    if (__builtin_amdgcn_ballot_w64(mx > m_run) != 0) {
+    if (__builtin_amdgcn_ballot_w64(mx > m_run || (CODE == LRA_INT8 && vs_raw > unit)) != 0) {
       const float m_new = fmaxf(m_run, mx);
       const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
       m_run = m_new;
       l_run *= alpha;
+      float alpha_o = alpha;
+      if constexpr (CODE == LRA_INT8) {
+        int most = 0;
 #pragma unroll
-      for (int b = 0; b < DB; ++b) o_acc[b] *= alpha;
+        for (int i = 0; i < 4; ++i) most = max(most, __builtin_amdgcn_readlane(vs_raw, i));
+        const int next = most > unit ? unit_above(most) : unit;
+        alpha_o *= over_unit(unit, next);
+        unit = next;
+      }
+#pragma unroll
+      for (int b = 0; b < DB; ++b) o_acc[b] *= alpha_o;
 #pragma unroll
       for (int b = 0; b < RB; ++b) lr_acc[b] *= alpha;
     }
@@ -297,7 +307,9 @@ __global__ __launch_bounds__(256, attn8_rows32_waves(RP)) void attn8_rows32_kern
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
-      const float even = scale8(__builtin_amdgcn_readlane(vs_raw, 2 * kt)), odd = scale8(__builtin_amdgcn_readlane(vs_raw, 2 * kt + 1));
+      const int vs_even = __builtin_amdgcn_readlane(vs_raw, 2 * kt), vs_odd = __builtin_amdgcn_readlane(vs_raw, 2 * kt + 1);
+      // (the scale, that of e4m3 codes goes with them, or what the weights take of it)
+      const float even = CODE == LRA_INT8 ? over_unit(vs_even, unit) : scale8(vs_even), odd = CODE == LRA_INT8 ? over_unit(vs_odd, unit) : scale8(vs_odd);
       const float vs_mine = g2 ? odd : even;
       uint32_t wl[8], wv[8];  // weights for L, and for V: with the block's scale, where that is not in V's operand
 #pragma unroll
@@ -351,7 +363,10 @@ __global__ __launch_bounds__(256, attn8_rows32_waves(RP)) void attn8_rows32_kern
   const float wgt = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_all);
   l_run = m_run == -INFINITY ? l_run : l_run * wgt;  // (a sum of NaN stays one)
 #pragma unroll
-  for (int b = 0; b < DB; ++b) o_acc[b] *= wgt;
+  for (int b = 0; b < DB; ++b) {
+    o_acc[b] *= wgt;
+    if constexpr (CODE == LRA_INT8) o_acc[b] *= scale8(unit);
+  }
 #pragma unroll
   for (int b = 0; b < RB; ++b) lr_acc[b] *= wgt;
 #pragma unroll

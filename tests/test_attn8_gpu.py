@@ -335,3 +335,23 @@ def test_no_number_in_one_share(kernel, blocks, side):
     assert bool(torch.isnan(got[sees][:, hq - g:]).all())
     if hkv > 1:
         close_enough(got[:, :hq - g], want[:, :hq - g], bound[:, :hq - g], c.label())
+
+
+# (e4m3 from 3 on: the smallest codes of the bytes below lie between bf16's denormal numbers)
+@pytest.mark.parametrize("code,byte", [("int8", 0), ("int8", 1)] + [(code, byte) for code in ("e4m3", "int8") for byte in (3, 20, 40, 63, 64, 100, 200, None)])
+@pytest.mark.parametrize("kernel", KERNELS, ids=str)
+def test_values_of_any_size(kernel, code, byte):
+    """Scale bytes of V over their range, or of all kinds beside each other: what is as small as bf16's least numbers is attended to like
+    anything else."""
+    c = Case8([333], rank=8, key_side=False, value_side=False, code=code, poison=False, seed=byte or 0, **kernel)
+    x = make8(c)
+    kc, ks, vc, vs = x.codes
+    if byte is None:
+        vs.copy_(torch.tensor([3, 40, 63, 64, 66, 118])[torch.randint(0, 6, vs.shape, generator=torch.Generator().manual_seed(1))])
+    else:
+        vs.fill_(byte)
+    x.v = values_of(vc, vs[..., None, None]).transpose(2, 3).reshape(1, -1, *c.heads[1:])[:, :333]
+    want, bound = attention_with_bound(x)
+    # no room but that of the values; of denormal outputs half a step, and of the fp32 sums' 333 and their joining's some steps
+    bound = bound - 1e-30 + 2.0 ** (-134 if c.dtype == BF16 else -150) + 400 * 2.0 ** -149
+    close_enough(Device8(x, lra).attend(), want, bound, c.label())
