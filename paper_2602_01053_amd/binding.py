@@ -43,6 +43,7 @@ class LraCache(ctypes.Structure):
                 ("l_row_stride", ctypes.c_int64), ("l_adapter_stride", ctypes.c_int64),
                 ("block_table", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p),
                 ("max_seq_len", ctypes.c_int32), ("seq_lens_host", ctypes.c_void_p)]
+    _sizes = None  # kv heads, head dimension, rank and type of the tensors, where make_cache has described some
 
 
 class LraAdapters(ctypes.Structure):
@@ -333,11 +334,12 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+_DTYPE_CODES = {torch.bfloat16: LRA_BF16, torch.float32: LRA_F32}
+
+
 def _dtype_code(t: torch.Tensor) -> int:
-    if t.dtype == torch.bfloat16:
-        return LRA_BF16
-    if t.dtype == torch.float32:
-        return LRA_F32
+    if t.dtype in _DTYPE_CODES:
+        return _DTYPE_CODES[t.dtype]
     raise LraError(3, f"unsupported torch dtype {t.dtype}")
 
 
@@ -384,6 +386,8 @@ def make_cache(k_base: torch.Tensor, v_base: torch.Tensor, l: torch.Tensor, seq_
                          int(k_base.shape[0]), int(block_table.shape[0]), l.stride(1), l_adapter_stride, _ptr(block_table),
                          _ptr(seq_lens), int(max_seq_len), mirror_ptr)
     cache._host_mirror = mirror  # the struct holds a raw pointer into it
+    alike = k_base.dtype == v_base.dtype == l.dtype and k_base.shape[1:] == v_base.shape[1:]
+    cache._sizes = (k_base.size(1), k_base.size(-1), l.size(-1), _DTYPE_CODES.get(l.dtype, -1) if alike else -1)
     return cache
 
 
@@ -675,6 +679,10 @@ def _check_new_rows(shape, cache, seq_start, k, v, l, positions) -> None:
 
 def _check_gather8(shape, cache, dst, kept) -> None:
     _check_cache8(shape, cache)
+    if dst._sizes is not None:
+        heads, d, rank, dtype = dst._sizes
+        if (heads, d, dtype) != (shape.n_kv_heads, shape.head_dim, shape.dtype) or rank < shape.rank:
+            raise LraError(2, "dst must have the shape's kv heads, head dimension and type, and room for its rank")
     if kept is not None:
         _check_kept(dst, kept, dst.max_seq_len)
 

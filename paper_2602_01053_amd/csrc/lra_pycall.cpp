@@ -258,15 +258,16 @@ struct View {
 
 PyObject* not_as_documented() { return PyLong_FromLong(-1); }
 
-// Whether the cache's kv heads, head dimension, rank and type of l (which make_cache8 left beside it) are the shape's.
-bool fits(PyObject* cache, const lra_shape* sh, bool& yes) {
+// Whether the cache's kv heads, head dimension, rank and type of l (which make_cache8 left beside it) are the shape's.  A cache that is
+// written (`dst`, of make_cache) may have room for a larger rank, and one that its caller has described by hand is taken as it is.
+bool fits(PyObject* cache, const lra_shape* sh, bool& yes, bool dst = false) {
   PyObject* v = PyObject_GetAttr(cache, s_sizes);
   if (!v) return false;
   int64_t x[4];
   int n;
-  const bool ok = ints(v, x, n);
+  const bool any = dst && v == Py_None, ok = any || ints(v, x, n);
   Py_DECREF(v);
-  yes = ok && n == 4 && x[0] == sh->n_kv_heads && x[1] == sh->head_dim && x[2] == sh->rank && x[3] == sh->dtype;
+  yes = any || (ok && n == 4 && x[0] == sh->n_kv_heads && x[1] == sh->head_dim && (dst ? x[2] >= sh->rank : x[2] == sh->rank) && x[3] == sh->dtype);
   return ok;
 }
 
@@ -351,12 +352,12 @@ PyObject* gather8(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Struct sh, c, d;
   View kept;
   void* st;
-  bool yes;
+  bool yes, room;
   if (!arity(n, 5) || !sh.open(a[0], g_shape_type) || !c.open(a[1], g_cache8_type) || !d.open(a[2], g_cache_type) || (a[3] != Py_None && !kept.open(a[3])) ||
-      !fits(a[1], sh.as<lra_shape>(), yes))
+      !fits(a[1], sh.as<lra_shape>(), yes) || !fits(a[2], sh.as<lra_shape>(), room, true))
     return nullptr;
   const lra_cache* dst = d.as<lra_cache>();
-  if (!yes || (a[3] != Py_None && (kept.dims != 2 || !kept.matrix(kI32, dst->n_seqs, kept.size[1]) || kept.size[1] < dst->max_seq_len))) return not_as_documented();
+  if (!yes || !room || (a[3] != Py_None && (kept.dims != 2 || !kept.matrix(kI32, dst->n_seqs, kept.size[1]) || kept.size[1] < dst->max_seq_len))) return not_as_documented();
   if (!stream_handle(a[4], &st)) return nullptr;
   lra_status status;
   Py_BEGIN_ALLOW_THREADS

@@ -127,3 +127,30 @@ def test_what_is_refused(noted):
         with pytest.raises((TypeError, AttributeError, ctypes.ArgumentError)):
             lra.lra_attn_batch8(**args)
     assert not noted
+
+
+def test_rows_are_read_back_into_what_has_room_for_them(noted):
+    """A cache of fewer kv heads, of another head dimension or type, or of too small a rank would be written behind its rows."""
+    c, q = cache(), torch.zeros(2, 4, 64, dtype=torch.bfloat16)
+    sh = lra.make_shape(q, 2, 8)
+    lens, table = torch.zeros(2, dtype=torch.int32), torch.zeros(2, 2, dtype=torch.int32)
+
+    def dst(heads=2, d=64, rank=8, kv=torch.bfloat16, v=None, low=torch.bfloat16):
+        return lra.make_cache(torch.zeros(4, heads, 16, d, dtype=kv), torch.zeros(4, heads, 16, d, dtype=v or kv), torch.zeros(4, 16, rank, dtype=low), lens, 32, table)
+
+    for bad in (dict(heads=1), dict(heads=3), dict(d=32), dict(d=128), dict(rank=4), dict(kv=torch.float32), dict(low=torch.float32), dict(v=torch.float16),
+                dict(kv=torch.float16, low=torch.float16), dict(kv=torch.float32, low=torch.float32)):
+        with pytest.raises(lra.LraError):
+            lra.lra_cache8_gather(sh, c, dst(**bad), stream=STREAM)
+    one = torch.zeros(1, dtype=torch.int32)
+    flat = lra.make_cache(torch.zeros(32, 1, 64).bfloat16(), torch.zeros(32, 1, 64).bfloat16(), torch.zeros(32, 8).bfloat16(), one, 32)
+    with pytest.raises(lra.LraError):
+        lra.lra_cache8_gather(sh, c, flat, stream=STREAM)
+    assert not noted
+    lra.lra_cache8_gather(sh, c, dst(), stream=STREAM)
+    lra.lra_cache8_gather(sh, c, dst(rank=16), stream=STREAM)          # the first ranks of wider rows
+    flat = lra.make_cache(torch.zeros(32, 2, 64).bfloat16(), torch.zeros(32, 2, 64).bfloat16(), torch.zeros(32, 8).bfloat16(), one, 32)
+    lra.lra_cache8_gather(sh, c, flat, stream=STREAM)
+    by_hand = B.LraCache(1 << 12, 1 << 12, 1 << 12, 64, 1024, 2048, 16, 2, 4, 2, 8, 0, 1 << 12, 1 << 12, 32)
+    lra.lra_cache8_gather(sh, c, by_hand, stream=STREAM)
+    assert [n for n, _ in noted] == ["gather"] * 4
