@@ -58,6 +58,7 @@ class LraBatch(ctypes.Structure):
     _fields_ = [("seq_query_start", ctypes.c_void_p), ("query_adapter", ctypes.c_void_p), ("n_queries", ctypes.c_int32),
                 ("max_queries_per_seq", ctypes.c_int32), ("causal", ctypes.c_int32), ("window", ctypes.c_int32),
                 ("sinks", ctypes.c_int32)]
+    _n_seqs = None  # the sequences of seq_query_start, where make_batch has described one
 
 
 class LraCache8(ctypes.Structure):
@@ -460,6 +461,7 @@ def make_batch(seq_query_start: torch.Tensor, query_adapter: torch.Tensor, max_q
     batch = LraBatch(_ptr(seq_query_start), _ptr(query_adapter), query_adapter.numel(), int(max_queries_per_seq), int(bool(causal)),
                      int(window), int(sinks))
     batch._tensors = (seq_query_start, query_adapter)  # the struct holds raw pointers into them
+    batch._n_seqs = seq_query_start.numel() - 1
     return batch
 
 
@@ -690,6 +692,8 @@ def _check_gather8(shape, cache, dst, kept) -> None:
 def _check_attend8(shape, cache, batch, q, out) -> None:
     _check_rows(batch, shape, q, out)
     _check_cache8(shape, cache)
+    if batch._n_seqs is not None and batch._n_seqs != cache.n_seqs:
+        raise LraError(2, f"seq_query_start must have {cache.n_seqs + 1} entries, one more than the cache has sequences")
 
 
 def _check_codes(name: str, codes: torch.Tensor, scales: torch.Tensor) -> None:

@@ -211,7 +211,7 @@ decltype(&lra_cache8_gather) g_gather8;
 decltype(&lra_attn_batch8) g_attend8;
 PyTypeObject *g_cache8_type, *g_batch_type;
 PyObject* g_dtypes[4];  // bfloat16, float32, int8, int32
-PyObject *s_shape, *s_stride, *s_dtype, *s_sizes;
+PyObject *s_shape, *s_stride, *s_dtype, *s_sizes, *s_n_seqs;
 enum { kBf16, kF32, kI8, kI32, kOther };
 
 bool ints(PyObject* tuple, int64_t (&x)[4], int& n) {
@@ -269,6 +269,15 @@ bool fits(PyObject* cache, const lra_shape* sh, bool& yes, bool dst = false) {
   Py_DECREF(v);
   yes = any || (ok && n == 4 && x[0] == sh->n_kv_heads && x[1] == sh->head_dim && (dst ? x[2] >= sh->rank : x[2] == sh->rank) && x[3] == sh->dtype);
   return ok;
+}
+
+// Whether the batch's seq_query_start (whose length make_batch left beside it) is that of n_seqs sequences.
+bool same_sequences(PyObject* batch, int32_t n_seqs, bool& yes) {
+  PyObject* v = PyObject_GetAttr(batch, s_n_seqs);
+  if (!v) return false;
+  yes = v == Py_None || PyLong_AsLongLong(v) == n_seqs;
+  Py_DECREF(v);
+  return !PyErr_Occurred();
 }
 
 // quantize(x, codes, scales, stream)
@@ -373,14 +382,14 @@ PyObject* attend8(PyObject*, PyObject* const* a, Py_ssize_t n) {
   View q, out;
   void *b_k, *b_v, *ws, *st;
   size_t bytes;
-  bool yes;
+  bool yes, same;
   if (!arity(n, 10) || !sh.open(a[0], g_shape_type) || !c.open(a[1], g_cache8_type) || !address(a[2], &b_k) || !address(a[3], &b_v) || !int32(a[4], &ad.n_adapters) ||
       !b.open(a[5], g_batch_type) || !q.open(a[6]) || !out.open(a[7]) || !workspace(a[8], &ws, &bytes) ||
-      !fits(a[1], sh.as<lra_shape>(), yes))
+      !fits(a[1], sh.as<lra_shape>(), yes) || !same_sequences(a[5], c.as<lra_cache8>()->n_seqs, same))
     return nullptr;
   const lra_shape* s = sh.as<lra_shape>();
   const int64_t queries = b.as<lra_batch>()->n_queries;
-  if (!yes || !q.rows(s->dtype, queries, s->n_q_heads, s->head_dim, true) || !out.rows(s->dtype, queries, s->n_q_heads, s->head_dim, true)) return not_as_documented();
+  if (!yes || !same || !q.rows(s->dtype, queries, s->n_q_heads, s->head_dim, true) || !out.rows(s->dtype, queries, s->n_q_heads, s->head_dim, true)) return not_as_documented();
   ad.b_k = b_k;
   ad.b_v = b_v;
   if (!stream_handle(a[9], &st)) return nullptr;
@@ -444,6 +453,7 @@ PyMODINIT_FUNC PyInit__lra_pycall() {
   s_stride = PyUnicode_InternFromString("stride");
   s_dtype = PyUnicode_InternFromString("dtype");
   s_sizes = PyUnicode_InternFromString("_sizes");
-  if (!s_data_ptr || !s_size || !s_nbytes || !s_cuda_stream || !s_zero || !s_one || !s_shape || !s_stride || !s_dtype || !s_sizes) return nullptr;
+  s_n_seqs = PyUnicode_InternFromString("_n_seqs");
+  if (!s_data_ptr || !s_size || !s_nbytes || !s_cuda_stream || !s_zero || !s_one || !s_shape || !s_stride || !s_dtype || !s_sizes || !s_n_seqs) return nullptr;
   return PyModule_Create(&module);
 }

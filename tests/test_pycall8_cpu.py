@@ -154,3 +154,17 @@ def test_rows_are_read_back_into_what_has_room_for_them(noted):
     by_hand = B.LraCache(1 << 12, 1 << 12, 1 << 12, 64, 1024, 2048, 16, 2, 4, 2, 8, 0, 1 << 12, 1 << 12, 32)
     lra.lra_cache8_gather(sh, c, by_hand, stream=STREAM)
     assert [n for n, _ in noted] == ["gather"] * 4
+
+
+def test_a_batch_has_the_sequences_of_its_cache(noted):
+    """Two sequences in the cache: a start vector of one would be read behind its end, one of three mean other queries."""
+    c, q = cache(), torch.zeros(2, 4, 64, dtype=torch.bfloat16)
+    sh = lra.make_shape(q, 2, 8)
+    i = lambda *v: torch.tensor(v, dtype=torch.int32)  # noqa: E731
+    for start in (i(0, 2), i(0, 1, 2, 2), i(0)):
+        with pytest.raises(lra.LraError):
+            lra.lra_attn_batch8(sh, c, None, None, 1, lra.make_batch(start, i(0, 0), 1), q, torch.empty_like(q), None, stream=STREAM)
+    assert not noted
+    lra.lra_attn_batch8(sh, c, None, None, 1, lra.make_batch(i(0, 1, 2), i(0, 0), 1), q, torch.empty_like(q), None, stream=STREAM)
+    lra.lra_attn_batch8(sh, c, None, None, 1, B.LraBatch(1 << 12, 1 << 12, 2, 1, 0, 0, 0), q, torch.empty_like(q), None, stream=STREAM)
+    assert [n for n, _ in noted] == ["attend"] * 2
