@@ -640,7 +640,7 @@ class _CtypesCalls8:
 
     def attend8(self, shape, cache, b_k, b_v, n_adapters, batch, q, out, workspace, stream):
         try:
-            _check_attend8(shape, cache, batch, q, out)
+            _check_attend8(shape, cache, b_k, b_v, n_adapters, batch, q, out)
         except LraError:
             return -1
         ad = LraAdapters(_ptr(b_k), _ptr(b_v), int(n_adapters))
@@ -689,8 +689,12 @@ def _check_gather8(shape, cache, dst, kept) -> None:
         _check_kept(dst, kept, dst.max_seq_len)
 
 
-def _check_attend8(shape, cache, batch, q, out) -> None:
+def _check_attend8(shape, cache, b_k, b_v, n_adapters, batch, q, out) -> None:
     _check_rows(batch, shape, q, out)
+    for b in (b_k, b_v):
+        want = int(n_adapters) * shape.rank * shape.n_kv_heads * shape.head_dim
+        if b is not None and (b.dim() > 4 or not b.is_contiguous() or b.numel() < want or _dtype_code(b) != shape.dtype):
+            raise LraError(2, f"b_k and b_v must be dense [{n_adapters}][{shape.rank}][{shape.n_kv_heads * shape.head_dim}] of the shape's dtype")
     _check_cache8(shape, cache)
     if batch._n_seqs is not None and batch._n_seqs != cache.n_seqs:
         raise LraError(2, f"seq_query_start must have {cache.n_seqs + 1} entries, one more than the cache has sequences")
@@ -745,10 +749,10 @@ def lra_batch8_workspace_bytes(shape: LraShape, cache: LraCache8, batch: LraBatc
 
 def lra_attn_batch8(shape: LraShape, cache: LraCache8, b_k: Optional[torch.Tensor], b_v: Optional[torch.Tensor], n_adapters: int,
                     batch: LraBatch, q: torch.Tensor, out: torch.Tensor, workspace: Optional[torch.Tensor], stream=None) -> None:
-    """lra_attn_batch over a cache of 8-bit codes.  q, out: [n_queries][Hq][d]."""
+    """lra_attn_batch over a cache of 8-bit codes.  b_k, b_v: [n_adapters][r][Hkv*d] (or None), q, out: [n_queries][Hq][d], all dense."""
     status = (_calls8 or _entry_points8()).attend8(shape, cache, b_k, b_v, n_adapters, batch, q, out, workspace, stream)
     if status:
-        _check8(status, _check_attend8, shape, cache, batch, q, out)
+        _check8(status, _check_attend8, shape, cache, b_k, b_v, n_adapters, batch, q, out)
 
 
 def lra_quantize_rows(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, stream=None) -> None:

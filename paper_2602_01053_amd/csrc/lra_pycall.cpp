@@ -253,6 +253,16 @@ struct View {
   bool rows(int want, int64_t n, int64_t a, int64_t b, bool dense) const {
     return dims == 3 && type == want && size[0] == n && size[1] == a && size[2] == b && stride[2] == 1 && (a == 1 || stride[1] == b) && (!dense || n <= 1 || stride[0] == a * b);
   }
+  // `elements` or more, one after the other
+  bool dense(int want, int64_t elements) const {
+    if (type != want || dims > 4) return false;
+    int64_t n = 1;
+    for (int i = dims - 1; i >= 0; --i) {
+      if (size[i] > 1 && stride[i] != n) return false;
+      n *= size[i];
+    }
+    return n >= elements;
+  }
   int64_t row_stride(int64_t row) const { return size[0] > 1 ? stride[0] : row; }
 };
 
@@ -379,19 +389,20 @@ PyObject* gather8(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* attend8(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Struct sh, c, b;
   lra_adapters ad{};
-  View q, out;
-  void *b_k, *b_v, *ws, *st;
+  View q, out, b_k, b_v;
+  void *ws, *st;
   size_t bytes;
   bool yes, same;
-  if (!arity(n, 10) || !sh.open(a[0], g_shape_type) || !c.open(a[1], g_cache8_type) || !address(a[2], &b_k) || !address(a[3], &b_v) || !int32(a[4], &ad.n_adapters) ||
-      !b.open(a[5], g_batch_type) || !q.open(a[6]) || !out.open(a[7]) || !workspace(a[8], &ws, &bytes) ||
+  if (!arity(n, 10) || !sh.open(a[0], g_shape_type) || !c.open(a[1], g_cache8_type) || (a[2] != Py_None && !b_k.open(a[2])) || (a[3] != Py_None && !b_v.open(a[3])) ||
+      !int32(a[4], &ad.n_adapters) || !b.open(a[5], g_batch_type) || !q.open(a[6]) || !out.open(a[7]) || !workspace(a[8], &ws, &bytes) ||
       !fits(a[1], sh.as<lra_shape>(), yes) || !same_sequences(a[5], c.as<lra_cache8>()->n_seqs, same))
     return nullptr;
   const lra_shape* s = sh.as<lra_shape>();
-  const int64_t queries = b.as<lra_batch>()->n_queries;
+  const int64_t queries = b.as<lra_batch>()->n_queries, table = static_cast<int64_t>(ad.n_adapters) * s->rank * s->n_kv_heads * s->head_dim;
+  if ((a[2] != Py_None && !b_k.dense(s->dtype, table)) || (a[3] != Py_None && !b_v.dense(s->dtype, table))) return not_as_documented();
   if (!yes || !same || !q.rows(s->dtype, queries, s->n_q_heads, s->head_dim, true) || !out.rows(s->dtype, queries, s->n_q_heads, s->head_dim, true)) return not_as_documented();
-  ad.b_k = b_k;
-  ad.b_v = b_v;
+  ad.b_k = b_k.data;
+  ad.b_v = b_v.data;
   if (!stream_handle(a[9], &st)) return nullptr;
   lra_status status;
   Py_BEGIN_ALLOW_THREADS

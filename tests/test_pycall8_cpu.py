@@ -168,3 +168,25 @@ def test_a_batch_has_the_sequences_of_its_cache(noted):
     lra.lra_attn_batch8(sh, c, None, None, 1, lra.make_batch(i(0, 1, 2), i(0, 0), 1), q, torch.empty_like(q), None, stream=STREAM)
     lra.lra_attn_batch8(sh, c, None, None, 1, B.LraBatch(1 << 12, 1 << 12, 2, 1, 0, 0, 0), q, torch.empty_like(q), None, stream=STREAM)
     assert [n for n, _ in noted] == ["attend"] * 2
+
+
+def test_adapters_are_as_large_as_they_are_said_to_be(noted):
+    """B_K and B_V of fewer adapters, of another type or with gaps would be read behind their end."""
+    c, q = cache(), torch.zeros(2, 4, 64, dtype=torch.bfloat16)
+    sh = lra.make_shape(q, 2, 8)
+    i = lambda *v: torch.tensor(v, dtype=torch.int32)  # noqa: E731
+    batch = lra.make_batch(i(0, 1, 2), i(0, 0), 1)
+    call = lambda b_k, b_v, n=3: lra.lra_attn_batch8(sh, c, b_k, b_v, n, batch, q, torch.empty_like(q), None, stream=STREAM)  # noqa: E731
+    good = torch.zeros(3, 8, 128, dtype=torch.bfloat16)
+    for bad in (good[:2], good[:, :7].contiguous(), good.float(), good.half(), good[:, :, ::2], torch.zeros(3, 16, 128, dtype=torch.bfloat16)[:, :8],
+                good.transpose(1, 2), good.view(1, 1, 3, 8, 128)):
+        for args in ((bad, good), (good, bad), (None, bad), (bad, None)):
+            with pytest.raises(lra.LraError):
+                call(*args)
+    with pytest.raises(lra.LraError):
+        call(good, good, 4)
+    assert not noted
+    call(good, good)
+    call(good.view(3, 8, 2, 64), good[:2], 2)
+    call(None, torch.zeros(5, 8, 128, dtype=torch.bfloat16)[1:4])
+    assert [n for n, _ in noted] == ["attend"] * 3
