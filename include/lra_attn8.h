@@ -100,6 +100,9 @@ lra_status lra_cache8_append(const lra_shape* shape, const lra_cache8* cache, co
  * src length - dst length + i; where dst's lengths are src's, the whole sequence.  dst is a cache of lra_attn.h (contiguous or
  * paged, any strides) whose k_base / v_base / l are WRITTEN although declared const; adapter 0's L rows are written.  bf16
  * values are exact.  Rows behind, and those whose source is not in [0, src length), are left as they are.
+ * With the rotary key side (key_rope_theta > 0) a row must keep its index, by which lra_attn_batch rotates its adapter part: kept is
+ * LRA_ERR_UNSUPPORTED then, as in lra_cache_gather, and without it dst's lengths must be src's, which is not checked (the last rows
+ * alone would be attended to at other positions).  A caller that wants rows for something else leaves key_rope_theta 0.
  *   kept  DEVICE int32 [n_seqs][kept_stride], kept_stride >= dst->max_seq_len
  */
 lra_status lra_cache8_gather(const lra_shape* shape, const lra_cache8* src, const int32_t* kept, int64_t kept_stride,

@@ -479,6 +479,8 @@ lra_status lra_cache8_gather(const lra_shape* shape, const lra_cache8* src, cons
   if (dst->n_seqs != src->n_seqs) return LRA_ERR_SHAPE;
   if (kept && kept_stride < dst->max_seq_len) return LRA_ERR_SHAPE;
   if (reinterpret_cast<uintptr_t>(kept) & 3) return LRA_ERR_SHAPE;
+  // (a row's index is the position by which its adapter part is rotated)
+  if (shape->key_rope_theta > 0.f && kept) return LRA_ERR_UNSUPPORTED;
   if (dst->k_base == src->k || dst->k_base == src->v || dst->v_base == src->k || dst->v_base == src->v || dst->l == src->l) return LRA_ERR_SHAPE;
   Gather8Params p{};
   p.kc = static_cast<const uint8_t*>(src->k);

@@ -243,3 +243,14 @@ int main(void) {
     got = [int(v) for v in subprocess.run([str(exe)], capture_output=True, text=True, check=True, env=dict(os.environ, LD_PRELOAD="")).stdout.split()]
     assert got == [ctypes.sizeof(LraCache8), LraCache8.max_seq_len.offset, ctypes.sizeof(LraNewRows), LraNewRows.rope_theta.offset,
                    ctypes.sizeof(LraI8Operands), LraI8Operands.k.offset]
+
+
+def test_gather_of_kept_rows_with_the_rotary_key_side(lib):
+    """A row's adapter part is rotated by its index: rows that move are refused, as lra_cache_gather refuses them."""
+    sh, c, _, _ = good()
+    sh.key_rope_theta = 10000.0
+    page = LraCache(2 * FAKE, 2 * FAKE, 2 * FAKE, 128, 2048, 16384, 16, 512, 600, 3, 0, 0, FAKE, FAKE, 8192)
+    assert lib.lra_cache8_gather(ref(sh), ref(c), FAKE, 8192, ref(page), None) == UNSUP
+    assert lib.lra_cache8_gather(ref(sh), ref(c), FAKE, 8191, ref(page), None) == SHAPE
+    other = LraCache(3 * FAKE, 3 * FAKE, 3 * FAKE, 128, 2048, 16384, 16, 512, 600, 3, 0, 0, FAKE, FAKE, 8192)
+    assert lib.lra_cache_gather(ref(sh), ref(page), 1, FAKE, 8192, ref(other), None, 0, None, 0, None) == UNSUP

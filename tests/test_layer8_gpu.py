@@ -196,3 +196,26 @@ def test_answer_tokens_in_a_graph(code):
         assert torch.equal(steps[0].out, want) and bool(torch.isfinite(want).all())
     for a, b in zip((layers[0].k, layers[0].v, layers[0].k_scale, layers[0].v_scale), (layers[1].k, layers[1].v, layers[1].k_scale, layers[1].v_scale)):
         assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+def test_rotary_key_side_on_whole_sequences_read_back():
+    """The adapters' part of a key is rotated by its row's index: whole sequences keep theirs, kept rows are refused."""
+    heads, rank = (6, 3, 64), 5
+    layer = Layer(2, 160, heads, rank, "e4m3", F32, seed=4)
+    g = torch.Generator().manual_seed(9)
+    layer.lens.copy_(torch.tensor([150, 33], dtype=torch.int32))
+    layer.step(layer.hold([150, 33], [1, 2]), torch.randn(183, layer.dm, generator=g).cuda())
+    layer.shape = lra.make_shape(torch.empty(1, 6, 64), 3, rank, key_rope_theta=THETA)
+    cache, k, v, l = layer.read()
+    batch = lra.make_batch(torch.tensor([0, 2, 3], dtype=torch.int32, device="cuda"), torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda"), 2)
+    q = torch.randn(3, 6, 64, generator=g)
+    out = torch.empty_like(q.cuda())
+    ws = torch.empty(max(lra.lra_batch_workspace_bytes(layer.shape, cache, batch), 256), dtype=torch.uint8, device="cuda")
+    lra.lra_attn_batch(layer.shape, cache, layer.b_k, layer.b_v, 3, batch, q.cuda(), out, ws)
+    torch.cuda.synchronize()
+    case = Case8([150, 33], [2, 1], heads=heads, rank=rank, dtype=F32, rope=THETA)
+    # (angles in fp32 turns: 1e-6 of a key's adapter part at most, a fifth of what the bound has for its sums)
+    want, bound = attention_with_bound(ref.Inputs(case, q, k, v, l[None], layer.b_k.cpu(), layer.b_v.cpu(), torch.tensor([0, 2, 3]), torch.tensor([0, 1, 2])))
+    close_enough(out, want, bound)
+    with pytest.raises(lra.LraError):
+        lra.lra_cache8_gather(layer.shape, layer.cache, cache, torch.zeros(2, 160, dtype=torch.int32, device="cuda"))
