@@ -22,7 +22,8 @@ extern "C" {
  * 448, no infinities), or LRA_INT8, two's complement integers.  A code c stands for
  *     c * 2^(s - 127),
  * s the byte that its block of 16 tokens and its kv head have in k_scale or v_scale (255: not a number).  With a power of two
- * every value is a bf16 number exactly.  Integers are the closer ones where the values of a block are of similar size,
+ * every value is a bf16 number exactly, for bytes from 3 (LRA_E4M3) or 0 (LRA_INT8) to 246: below, the smallest e4m3 codes lie
+ * between bf16's denormal numbers and are rounded to them, above, the largest codes are beyond its range.  Integers are the closer ones where the values of a block are of similar size,
  * e4m3 where some channels are far larger than the others.
  */
 typedef enum { LRA_E4M3 = 0, LRA_INT8 = 1 } lra_code;
@@ -87,7 +88,8 @@ typedef struct {
  * tokens are rounded anew.  Rounding is to nearest, ties to even; rotation and scaling are done in fp32 before it.  Slots past
  * the end of a sequence are left as they were, and blocks without new tokens are not touched.  A block that receives tokens
  * belongs to one sequence (blocks that are full may be shared).  Calling again with the same rows changes nothing.
- * K and V must be finite: a value that is not makes the block's rows of that head unspecified.
+ * K and V must be finite: a value that is not makes the block's rows of that head unspecified.  (Above 3.29e38 the code may stand
+ * for 2^128, which is read as infinite.)
  * Nothing is written for a sequence whose device-side length exceeds max_seq_len; tokens before the sequence's first (c_t
  * larger than its length) and blocks whose table entry is out of range are passed over.  More than 2^31 (block with new tokens,
  * pair of kv heads) of a sequence are LRA_ERR_UNSUPPORTED, and so are as many (sixteen rows, pair) in lra_cache8_gather.
@@ -99,7 +101,7 @@ lra_status lra_cache8_append(const lra_shape* shape, const lra_cache8* cache, co
  * what lra_evict_select keeps, or any choice.  kept NULL: the last rows of src, row i the token
  * src length - dst length + i; where dst's lengths are src's, the whole sequence.  dst is a cache of lra_attn.h (contiguous or
  * paged, any strides) whose k_base / v_base / l are WRITTEN although declared const; adapter 0's L rows are written.  bf16
- * values are exact.  Rows behind, and those whose source is not in [0, src length), are left as they are.
+ * values are exact where the scale byte allows it (lra_code), and the nearest elsewhere.  Rows behind, and those whose source is not in [0, src length), are left as they are.
  * With the rotary key side (key_rope_theta > 0) a row must keep its index, by which lra_attn_batch rotates its adapter part: kept is
  * LRA_ERR_UNSUPPORTED then, as in lra_cache_gather, and without it dst's lengths must be src's, which is not checked (the last rows
  * alone would be attended to at other positions).  A caller that wants rows for something else leaves key_rope_theta 0.

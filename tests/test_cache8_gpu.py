@@ -352,3 +352,29 @@ def test_appends_and_gathers_on_two_streams():
     torch.cuda.synchronize()
     for pool, twin in zip(pools[:2], pools[2:]):
         assert all(torch.equal(a, b) for a, b in zip(pool.bytes(), twin.bytes()))
+
+
+@pytest.mark.parametrize("code", ["e4m3", "int8"])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_values_over_all_scales(code, dtype):
+    """Every code at every scale byte: exact from byte 3 (e4m3) or 0 (integers) to 246, the nearest number elsewhere."""
+    d, n = 64, 255
+    codes = [c for c in range(256) if code == "int8" or c & 127 != 127]
+    every = torch.tensor((codes * 5)[:BLOCK * d], dtype=torch.uint8)
+    k = every.view(1, 1, BLOCK, d).expand(n, 1, BLOCK, d).contiguous().cuda().view(TORCH[code])
+    v = every.view(1, 1, d, BLOCK).expand(n, 1, d, BLOCK).contiguous().cuda().view(TORCH[code])
+    scale = torch.arange(n, dtype=torch.uint8)[:, None]
+    dev = scale.cuda()
+    l, lens = torch.zeros(n, BLOCK, 8, dtype=dtype, device="cuda"), torch.tensor([n * BLOCK], dtype=torch.int32, device="cuda")
+    out = [torch.full((n * BLOCK, 1, d), 7.0, dtype=dtype, device="cuda") for _ in range(2)] + [torch.zeros(n * BLOCK, 8, dtype=dtype, device="cuda")]
+    shape = lra.make_shape(out[0], 1, 8)
+    lra.lra_cache8_gather(shape, lra.make_cache8(k, v, dev, dev, l, lens, n * BLOCK), lra.make_cache(*out, lens, n * BLOCK))
+    torch.cuda.synchronize()
+    rows = every.view(TORCH[code]).view(1, BLOCK, d), every.view(TORCH[code]).view(1, d, BLOCK).transpose(1, 2)
+    for got, c in zip(out, rows):
+        want = values_of(c, scale[..., None])
+        got = got.view(n, BLOCK, d).cpu()
+        # (a double's way to bf16 is by fp32, which holds these values exactly, or as infinite)
+        assert torch.equal(got, want.float().to(dtype))
+        exact = slice(3 if code == "e4m3" and dtype == BF16 else 0, 247)
+        assert torch.equal(got[exact].double(), want[exact])
