@@ -48,9 +48,9 @@ typedef struct {
   uint8_t* k_scale;           /* DEVICE */
   uint8_t* v_scale;           /* DEVICE */
   void* l;                    /* DEVICE */
-  int64_t kv_block_stride;    /* bytes, multiples of 16 */
+  int64_t kv_block_stride;    /* bytes, multiples of 16, at most 2^40 */
   int64_t kv_head_stride;
-  int64_t scale_block_stride; /* bytes, >= Hkv; 0: Hkv */
+  int64_t scale_block_stride; /* bytes, >= Hkv; 0: Hkv; at most 2^31 */
   int64_t l_row_stride;       /* elements; 0: rank.  A multiple of 8, or the rank; at most 2^24 */
   int32_t code;               /* lra_code */
   int32_t max_blocks_per_seq; /* row length of block_table (of no effect without one) */
@@ -69,7 +69,7 @@ typedef struct {
   const void* k;             /* DEVICE [n_new][Hkv][head_dim], tokens k_token_stride elements apart; in lra_shape's type */
   const void* v;             /* DEVICE, alike */
   const void* l;             /* DEVICE [n_new][rank], or NULL: the L rows are left as they are */
-  int64_t k_token_stride;    /* elements; k_ and v_token_stride, like the addresses of k and v, multiples of 16 bytes */
+  int64_t k_token_stride;    /* elements, at most 2^31; k_ and v_token_stride, like the addresses of k and v, multiples of 16 bytes */
   int64_t v_token_stride;
   int64_t l_token_stride;
   const int32_t* seq_start;  /* DEVICE int32 [n_seqs+1], non-decreasing, [0] = 0, [n_seqs] = n_new */
@@ -113,7 +113,8 @@ lra_status lra_cache8_gather(const lra_shape* shape, const lra_cache8* src, cons
 /*
  * lra_attn_batch (same batches, windows and sinks, adapters, outputs) over such a cache: the result is that of lra_attn_batch
  * on the values that the codes stand for.  bf16 with a rank that is a multiple of 8 runs on MFMA kernels, everything else on
- * vector-ALU kernels.  A rotated key-side adapter (key_rope_theta > 0 with a b_k) is LRA_ERR_UNSUPPORTED.
+ * vector-ALU kernels.  A rotated key-side adapter (key_rope_theta > 0 with a b_k) is LRA_ERR_UNSUPPORTED, and 2^24 query rows (queries
+ * times n_q_heads) or more may be.
  *   workspace  DEVICE, 256-byte aligned, >= lra_batch8_workspace_bytes(...), as for lra_attn_batch
  *   tuning     kernel_variant (1: vector-ALU kernels, 2: no kernel of its own for few query rows)
  */
@@ -130,7 +131,8 @@ size_t lra_batch8_workspace_bytes(const lra_shape* shape, const lra_cache8* cach
  *   x      DEVICE [rows][cols] of dtype (lra_dtype), rows x_stride elements apart; x and the stride multiples of 16 bytes
  *   codes  DEVICE int8 [rows][cols], rows codes_stride bytes apart; both multiples of 16 bytes
  *   scales DEVICE float [rows]
- * cols a multiple of 16, at most 2^17; rows below 2^24.
+ * cols a multiple of 16, at most 2^17; rows below 2^24 (a product takes 2^20 of them and fewer than 2^17 columns); strides at most
+ * 2^40.
  */
 lra_status lra_quantize_rows(const void* x, int32_t dtype, int64_t x_stride, int32_t rows, int32_t cols, int8_t* codes,
                              int64_t codes_stride, float* scales, void* stream);
@@ -141,14 +143,14 @@ typedef struct {
   const int8_t* w;       /* DEVICE [n][k], rows w_stride bytes apart: a linear layer's weight, one feature per row */
   const float* x_scale;  /* DEVICE [m] */
   const float* w_scale;  /* DEVICE [n] */
-  int64_t x_stride;      /* strides and the addresses of x and w: multiples of 16 bytes */
+  int64_t x_stride;      /* strides and the addresses of x and w: multiples of 16 bytes; strides at most 2^31 */
   int64_t w_stride;
-  int32_t m, n, k;       /* k a multiple of 16, below 2^17 (sums stay in 32 bits) */
+  int32_t m, n, k;       /* m and n at most 2^20; k a multiple of 16, below 2^17 (sums stay in 32 bits) */
 } lra_i8_operands;
 
 /*
- * y[i][j] = x_scale[i] * w_scale[j] * sum_c x[i][c] w[j][c]: the sum exact in 32-bit integers, scaled in fp32, rounded once.
- *   y          DEVICE [m][n] of dtype (lra_dtype), rows y_stride elements apart, 16-byte aligned; any n and y_stride >= n
+ * y[i][j] = x_scale[i] * w_scale[j] * sum_c x[i][c] w[j][c]: the sum exact in 32-bit integers, scaled in fp32 (by x_scale first), rounded once.
+ *   y          DEVICE [m][n] of dtype (lra_dtype), rows y_stride elements apart, 16-byte aligned; y_stride from n to 2^31
  *   workspace  as many bytes as lra_matmul_i8_workspace_bytes says: none for any size so far, NULL and 0 will do
  */
 lra_status lra_matmul_i8(const lra_i8_operands* ops, void* y, int32_t dtype, int64_t y_stride, void* workspace,

@@ -254,3 +254,26 @@ def test_gather_of_kept_rows_with_the_rotary_key_side(lib):
     assert lib.lra_cache8_gather(ref(sh), ref(c), FAKE, 8191, ref(page), None) == SHAPE
     other = LraCache(3 * FAKE, 3 * FAKE, 3 * FAKE, 128, 2048, 16384, 16, 512, 600, 3, 0, 0, FAKE, FAKE, 8192)
     assert lib.lra_cache_gather(ref(sh), ref(page), 1, FAKE, 8192, ref(other), None, 0, None, 0, None) == UNSUP
+
+
+def test_sizes_at_the_documented_limits(lib):
+    size = lib.lra_matmul_i8_workspace_bytes
+    assert size(1 << 20, 1 << 20, (1 << 17) - 16, 0) < REFUSED
+    for m, n, k in (((1 << 20) + 1, 16, 16), (16, (1 << 20) + 1, 16), (16, 16, 1 << 17)):
+        assert size(m, n, k, 0) == REFUSED
+    far = (1 << 31) + 16
+    for field in ("x_stride", "w_stride"):
+        ops = LraI8Operands(FAKE, FAKE, FAKE, FAKE, 256, 256, 4, 64, 256)
+        setattr(ops, field, far)
+        assert lib.lra_matmul_i8(ref(ops), FAKE, 0, 64, None, 0, None) == UNSUP, field
+    ops = LraI8Operands(FAKE, FAKE, FAKE, FAKE, 256, 256, 4, 64, 256)
+    assert lib.lra_matmul_i8(ref(ops), FAKE, 0, far, None, 0, None) == UNSUP
+    assert lib.lra_quantize_rows(FAKE, 0, 256, 4, 256, FAKE, (1 << 40) + 16, FAKE, None) == UNSUP
+    sh, c, ad, b = good()
+    c.scale_block_stride = far
+    assert lib.lra_batch8_workspace_bytes(ref(sh), ref(c), ref(b), None) == REFUSED
+    for field in ("k_token_stride", "v_token_stride", "l_token_stride"):
+        sh, c, _, _ = good()
+        new = rows()
+        setattr(new, field, far)
+        assert lib.lra_cache8_append(ref(sh), ref(c), ref(new), None) == UNSUP, field
