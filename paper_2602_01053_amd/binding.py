@@ -581,9 +581,9 @@ def make_cache8(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale
     if any(k.size(i) > 1 and v.stride(i) != k.stride(i) for i in (0, 1)):
         raise LraError(2, "k and v must share the strides of blocks and heads")
     for s in (k_scale, v_scale):
-        if s.dtype != torch.uint8 or tuple(s.shape) != (blocks, heads) or (heads > 1 and s.stride(1) != 1) or s.stride(0) != k_scale.stride(0):
+        if s.dtype != torch.uint8 or tuple(s.shape) != (blocks, heads) or (heads > 1 and s.stride(1) != 1) or (blocks > 1 and s.stride(0) != k_scale.stride(0)):
             raise LraError(2, f"scales must be uint8 [{blocks}][{heads}], unit stride on the heads, one stride on the blocks")
-    if l.dim() != 3 or l.shape[:2] != (blocks, 16) or l.stride(-1) != 1 or l.stride(0) != 16 * l.stride(1):
+    if l.dim() != 3 or l.shape[:2] != (blocks, 16) or (l.size(2) > 1 and l.stride(2) != 1) or (blocks > 1 and l.stride(0) != 16 * l.stride(1)):
         raise LraError(2, "l must be [num_blocks][16][r] with the rows one row stride apart")
     n_seqs = 1 if block_table is None else block_table.size(0)
     if block_table is not None and (block_table.dtype != torch.int32 or block_table.dim() != 2 or not block_table.is_contiguous()):

@@ -277,3 +277,19 @@ def test_sizes_at_the_documented_limits(lib):
         new = rows()
         setattr(new, field, far)
         assert lib.lra_cache8_append(ref(sh), ref(c), ref(new), None) == UNSUP, field
+
+
+def test_binding_takes_a_cache_of_one_block():
+    """Strides of a dimension of one mean nothing: scales and L rows of one block cut from wider tensors."""
+    one = dict(k=torch.zeros(1, 2, 16, 64, dtype=torch.int8), v=torch.zeros(1, 2, 64, 16, dtype=torch.int8), k_scale=torch.zeros(1, 2, dtype=torch.uint8),
+               v_scale=torch.zeros(1, 6, dtype=torch.uint8)[:, 2:4], l=torch.zeros(1, 40, 8, dtype=torch.bfloat16)[:, 16:32], seq_lens=torch.zeros(1, dtype=torch.int32),
+               max_seq_len=16)
+    c = lra.make_cache8(**one)
+    assert (c.num_blocks, c.scale_block_stride, c.l_row_stride) == (1, 2, 8)
+    two = {n: torch.cat((t, t)) if n in ("k", "v", "k_scale") else t for n, t in one.items()}
+    two.update(v_scale=torch.zeros(2, 6, dtype=torch.uint8)[:, 2:4], l=torch.zeros(2, 16, 8, dtype=torch.bfloat16))
+    with pytest.raises(lra.LraError):
+        lra.make_cache8(**two)
+    two.update(v_scale=torch.zeros(2, 2, dtype=torch.uint8), l=torch.zeros(2, 40, 8, dtype=torch.bfloat16)[:, 16:32])
+    with pytest.raises(lra.LraError):
+        lra.make_cache8(**two)
