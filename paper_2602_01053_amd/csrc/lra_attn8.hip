@@ -10,7 +10,7 @@ namespace lra {
 // wave's lanes share a token's score (a quarter of its K row, of its L row each), a thread then sums one dimension of V over the
 // tokens of some of the four blocks, sixteen codes a load, and one rank of L over sixteen tokens.  For fp32, ranks that are no
 // multiple of 8, and as a second opinion on the MFMA kernels.  16 rows that see 260 keys take 7.5 us, the chain of a tile two to three times;
-// long contexts are bound by the vector units, every row decoding its keys anew: 32 rows over 64 k tokens in fp32 167 us.
+// long contexts are bound by the vector units, every row decoding its keys anew: 32 rows over 64 k tokens in fp32 167 to 173 us.
 template <typename T, int D, int CODE>
 __global__ __launch_bounds__(256) void attn8_vector_kernel(Batch8Params p) {
   constexpr int DQ = D / 4;             // dimensions of a K row per lane
@@ -110,7 +110,7 @@ __global__ __launch_bounds__(256) void attn8_vector_kernel(Batch8Params p) {
     const float pj = s == -INFINITY || (m_new == -INFINITY && s == s) ? 0.f : expf(s - m_new);
     m = m_new;
     ell = ell * alpha + pj;  // (of this lane's tokens)
-    p_s[piece][lane] = pj;  // (by lanes' exchange instead, sixteen at a time, 200 rows over 2 k tokens took 733 us instead of 565)
+    p_s[piece][lane] = pj;  // (by lanes' exchange instead, sixteen at a time, 200 queries of 32 heads over 2 k tokens took 733 us instead of 565)
     wave_fence();
     o *= alpha;
     olr *= alpha;

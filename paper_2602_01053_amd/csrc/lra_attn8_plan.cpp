@@ -121,8 +121,9 @@ static bool plan_few_rows(Attn8Plan& pl, const lra_shape* sh, const lra_cache8* 
 // A workgroup of attn8_tiles_kernel takes 128 rows of one sequence.  The key tiles of a q tile are shared where there are fewer q tiles
 // than the chip has places, two per compute unit, and then so that they fill the places once; a share walks two tiles at least.  Those of
 // several sequences are shared out by their lengths, on the device (attn8_tiles_per_share), into some three and a half to a unit: 12 chunks of 1 to 256
-// tokens over 1 k to 8 k tokens take 179 us, 184 in twice as many equal shares for each q tile as fill the places and 206 in as many; over 0.5 k to
-// 32 k 405, 474 and 657; 4 of 256 over 16 k 171 and 189.  In 2.7, 4.7 and 7 to a unit the first take 194, 193 and 197.
+// tokens over 1 k to 8 k tokens took 179 us (170 with the wave priorities that came later), 184 in twice as many equal shares for each q tile as fill
+// the places and 206 in as many; over 1 k to 32 k 395, 474 and 657; 4 of 256 over 16 k 171 and 189.  In 2.7, 4.7 and 7 to a unit the first took
+// 194, 193 and 197.
 // Where the q tiles need no shares, those of eight sequences and more go in the order of what they see: 32 chunks of up to 512 tokens over 0.5 k
 // to 16 k (28 q heads on 4) take 799 us instead of 999, 60 of up to 128 over 1 k to 30 k 916 instead of 1041; four chunks, of which one has
 // nearly all tiles, 1585 instead of 1513, and tiles in shares 2 to 10 % longer.

@@ -17,7 +17,7 @@ struct Attn8Plan {
   bool launchable;
   bool few_rows, tiles, states, longest_first;
   int rows, n_splits, row_tiles, tile_places;
-  int head_shares, share_least;  // few rows: shares of a kv head over all sequences (0: n_splits of each), tiles of the shortest
+  int head_shares, share_least;  // shares of a kv head over all sequences, by their lengths (0: n_splits of each); few rows: tiles of the shortest
   size_t off_ml, off_o, off_lr, off_adapter, bytes;
 };
 Attn8Plan plan_attn8(const lra_shape* sh, const lra_cache8* c, const lra_batch* b, const Tuning& tune);

@@ -11,8 +11,8 @@
 //   lane group g of the result S^T holds all sixteen tokens of block g, which is what the B operand of V^T P^T wants of it: its A
 //     operand is sixteen tokens of one dimension, the 16 bytes that the cache holds together;
 //   L is transposed by a product with the identity: the result layout of L I is the operand layout of L^T.
-// A code becomes bf16 with its block's scale in one instruction per pair (e4m3) or by itself (integers, whose scores and weights take
-// the scales instead, exactly): the codes of a tile cost a wave some 500 cycles, the 16 KB that they stand for 2000 of the memory's.
+// A code becomes bf16 with its block's scale in one instruction per pair (e4m3) or by itself (integers, whose scores take K's scale and whose
+// weights V's over a unit, powers of two both): the codes of a tile cost a wave some 500 cycles, the 16 KB that they stand for 2000 of the memory's.
 // K of a wave's next tile is requested as soon as its scores are taken, V and L as soon as the products are: with eight waves to a
 // compute unit some hundred KB are on their way.
 // Bound by HBM where the shares are long: 14 rows over 16 sequences of 4 k to 64 k tokens 141 us with the merge, 5.5 TB/s of the bytes
@@ -283,6 +283,7 @@ __global__ __launch_bounds__(256, 2) void attn8_rows_kernel(Batch8Params p) {
     for (int ks = 0; ks < KS; ++ks) qb[ks] = as_bf16x8(*reinterpret_cast<const uint4*>(qr + (ks >> 1) * 64 + (ks & 1) * 8));
   }
   // Qt^T, ranks by rows: register e of block b is rank 16b + 4g + e, the operand that L Qt^T takes (k = 16: four ranks a lane group).
+  // Rounded to bf16, as the matrix cores take it and as lra_attn_batch has it: a score is off by 2^-8 of its adapter part at most.
   // The waves divide the queries (each with its adapter, or the chunk's one) and hand the operands round in LDS.
   s16x4v qtb[HAS_BK ? RB : 1];
   if constexpr (HAS_BK) {

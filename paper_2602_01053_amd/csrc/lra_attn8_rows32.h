@@ -1,6 +1,6 @@
 // Attention over 8-bit codes for sequences with 17 to 64 query rows per kv head: attn8_rows_kernel with 32 rows to a wave
 // (v_mfma_f32_32x32x16_bf16).  Waves of 16 rows each read every key once per row tile: 16 sequences of 4 k to 64 k tokens with 28 rows took
-// 244 us so (e4m3; integers 258) and take 152 to 156 (165), 5.0 TB/s of the bytes needed; 64 rows over 32 k tokens take 38 us, as much by their
+// 244 us so (e4m3; integers 258) and take 150 to 156 (160 to 165), 5.0 TB/s of the bytes needed; 64 rows over 32 k tokens take 38 us, as much by their
 // states and products as by the reading.
 //
 // Operands straight from the cache, as there: row rho of key tile t (of two) is token 8 (rho / 16) + 4 (rho / 8 % 2) + rho % 4 of block
@@ -141,7 +141,7 @@ __global__ __launch_bounds__(256, attn8_rows32_waves(RP)) void attn8_rows32_kern
   __syncthreads();
   auto q_of = [&](int ks) __attribute__((always_inline)) -> bf16x8 { return __builtin_bit_cast(bf16x8, q_s[rt][ks][lane]); };
   // Qt^T, ranks by rows: register i of block b is rank 32b + 8 (i / 4) + 4 g2 + i % 4; the halves exchange fours, so that a lane has
-  // ranks 16 rs + 8 g2 + 0..7 of k-step rs, as it loads them of L.  The waves of a row tile divide its queries (each with its adapter, or
+  // ranks 16 rs + 8 g2 + 0..7 of k-step rs, as it loads them of L (in bf16, as in attn8_rows_kernel).  The waves of a row tile divide its queries (each with its adapter, or
   // the chunk's one) and hand the operands round in LDS.
   if constexpr (HAS_BK) {
     const int64_t ldb = static_cast<int64_t>(Hkv) * D;

@@ -234,7 +234,8 @@ __global__ __launch_bounds__(256, 2) void attn8_tiles_kernel(Batch8Params p) {
   constexpr int STAGE = 2 * K_BYTES + L_BYTES;
   // With a half-empty last 32-row block of Olr^T (rank 16 or 48 after padding), its idle
   // upper lanes read a constant [1, 0, 0, 0] instead of L, so the matrix core also
-  // accumulates the softmax row sums.
+  // accumulates the softmax row sums, of the probabilities as they are rounded to bf16: what O is divided by are the weights that
+  // it was summed with.
   constexpr bool ONES_ROW = (RP % 32) != 0;
   constexpr int ONES_AT = 2 * STAGE;
 
@@ -370,6 +371,7 @@ __global__ __launch_bounds__(256, 2) void attn8_tiles_kernel(Batch8Params p) {
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qb[ks] = pf_as_bf16x8(*reinterpret_cast<const uint4*>(qrow + ks * 16));
   }
+  // (in bf16, as in attn8_rows_kernel)
   // Qt^T[rho][row] = B_K[rho][:] . Q[row][:]: C layout lane (row l32; reg i <-> rho = 32b + 8(i/4) + 4g2 + i%4).
   // As B operand of the rank k-steps of S^T, k-step ks' takes registers 8ks'..8ks'+7 of
   // block b = ks'/2, i.e. element e <-> rho = 16ks' + 8(e/4) + 4g2 + e%4; the L operand

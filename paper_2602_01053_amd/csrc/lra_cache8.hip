@@ -33,8 +33,8 @@ __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
   return v;
 }
 
-// Sine and cosine of 2 pi x turns, |turns| <= 1/2, from their power series about the nearest quarter turn, to 1e-12: rounded to fp32
-// they are those of the exact angle but for one in 10^5, so that a key's codes do not depend on how its angle was reduced.  (The
+// Sine and cosine of 2 pi x turns, |turns| <= 1/2, from their power series about the nearest quarter turn, to 7e-12 (the sine's
+// first missing term, at an eighth of a turn): rounded to fp32 they are those of the exact angle but for one in 10^5, so that a key's codes do not depend on how its angle was reduced.  (The
 // hardware's v_sin_f32 is off by up to 1e-6, which moves one in 10^4 codes to the next.)
 __device__ __forceinline__ void sincos_turns(double turns, float& sn, float& cs) {
   const double q = rint(4.0 * turns);

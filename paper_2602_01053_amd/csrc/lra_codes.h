@@ -13,7 +13,8 @@ struct Batch8Params : BatchParams {
   int64_t scale_block_stride;
   int32_t code;
   int32_t longest_first;            // tiles kernel: q tiles in the order of what they see
-  int32_t head_shares, share_least;  // rows kernels: key shares of a kv head (0: n_splits of every sequence), tiles of the shortest
+  int32_t head_shares;              // key shares of a kv head over all sequences, formed by their lengths (0: n_splits of every sequence or q tile)
+  int32_t share_least;              // rows kernels: tiles of the shortest of those
 };
 
 // Block b of sequence t.

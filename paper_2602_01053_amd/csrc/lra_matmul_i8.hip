@@ -542,7 +542,8 @@ __global__ __launch_bounds__(256) void matmul_i8_far_kernel(I8Params p) {
 // Tiles of 32 to 256 a side by what they cost: a launch and the rounds of the chip that it takes, a compute unit holding one tile at a
 // time (two of 32, which the figures count as two rounds of half the length).  Features behind whole tiles, or behind whole rounds,
 // may get smaller tiles in a launch of their own: 8192 tokens x 6160 features are 800 tiles of 256 in four rounds, 218 us, or 768 in
-// three and a few small ones, 188; 4096 x 4640 (of 3584) 304 tiles in two rounds, 96 us, or 256 in one and 160 of 128, 76.
+// three and a few small ones, 188; 4096 x 4640 (of 3584) 304 tiles in two rounds, 96 us, or 256 in one and 160 of 128, 76.  (The figures are those of
+// k = 4096 for any k: of short rows a second launch may cost what it saves.)
 enum I8Tile { kTile32, kTile64x32, kTile32x64, kTile64, kTile128, kTile256 };  // features x tokens
 struct I8Shape {
   int features, tokens, start, round;  // time of a launch and of each round of the chip, in 0.1 us at k = 4096
