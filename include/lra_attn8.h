@@ -23,8 +23,8 @@ extern "C" {
  *     c * 2^(s - 127),
  * s the byte that its block of 16 tokens and its kv head have in k_scale or v_scale (255: not a number).  With a power of two
  * every value is a bf16 number exactly, for bytes from 3 (LRA_E4M3) or 0 (LRA_INT8) to 246: below, the smallest e4m3 codes lie
- * between bf16's denormal numbers and are rounded to them, above, the largest codes are beyond its range.  Integers are the closer ones where the values of a block are of similar size,
- * e4m3 where some channels are far larger than the others.
+ * between bf16's denormal numbers and are rounded to them, above, the largest codes are beyond its range.  Integers are the closer
+ * ones where the values of a block are of similar size, e4m3 where some channels are far larger than the others.
  */
 typedef enum { LRA_E4M3 = 0, LRA_INT8 = 1 } lra_code;
 
@@ -101,7 +101,8 @@ lra_status lra_cache8_append(const lra_shape* shape, const lra_cache8* cache, co
  * what lra_evict_select keeps, or any choice.  kept NULL: the last rows of src, row i the token
  * src length - dst length + i; where dst's lengths are src's, the whole sequence.  dst is a cache of lra_attn.h (contiguous or
  * paged, any strides) whose k_base / v_base / l are WRITTEN although declared const; adapter 0's L rows are written.  bf16
- * values are exact where the scale byte allows it (lra_code), and the nearest elsewhere.  Rows behind, and those whose source is not in [0, src length), are left as they are.
+ * values are exact where the scale byte allows it (lra_code), and the nearest elsewhere.  Rows behind, and those whose source is
+ * not in [0, src length), are left as they are.
  * With the rotary key side (key_rope_theta > 0) a row must keep its index, by which lra_attn_batch rotates its adapter part: kept is
  * LRA_ERR_UNSUPPORTED then, as in lra_cache_gather, and without it dst's lengths must be src's, which is not checked (the last rows
  * alone would be attended to at other positions).  A caller that wants rows for something else leaves key_rope_theta 0.
@@ -114,7 +115,8 @@ lra_status lra_cache8_gather(const lra_shape* shape, const lra_cache8* src, cons
  * lra_attn_batch (same batches, windows and sinks, adapters, outputs) over such a cache: the result is that of lra_attn_batch
  * on the values that the codes stand for.  bf16 with a rank that is a multiple of 8 runs on MFMA kernels, everything else on
  * vector-ALU kernels.  A rotated key-side adapter (key_rope_theta > 0 with a b_k) is LRA_ERR_UNSUPPORTED, and 2^24 query rows (queries
- * times n_q_heads) or more may be.
+ * times n_q_heads) or more may be.  LRA_INT8 with 64 query rows per kv head or fewer: a block whose v_scale is 118 or more below the
+ * largest one of its sequence (a factor of 2^118) may count as zeros.
  *   workspace  DEVICE, 256-byte aligned, >= lra_batch8_workspace_bytes(...), as for lra_attn_batch
  *   tuning     kernel_variant (1: vector-ALU kernels, 2: no kernel of its own for few query rows)
  */
